@@ -72,10 +72,15 @@ def listed():
 
 
 def _spread(rng, lo, hi):
-    """A whole number between lo and hi, even over its logarithm; half of them odd, half round."""
+    """A whole number between lo and hi, even over its logarithm; half of them odd, half
+    multiples of 64 that are none of 3 * 2^k."""
     v = int(math.exp(rng.uniform(math.log(lo), math.log(hi + 1))))
-    v = max(lo, v | 1) if rng.random() < 0.5 else max(lo, v // 64 * 64)
-    return min(v, hi)
+    if rng.random() < 0.5:
+        return min(max(lo, v | 1), hi)
+    v = max(64, v // 64 * 64)
+    if v % 3 == 0 and v // 3 & (v // 3 - 1) == 0:
+        v += 64
+    return max(lo, v) if v <= hi else hi
 
 
 def draw(rng):
@@ -114,7 +119,7 @@ def draw(rng):
     c["experts"] = rng.choice([8, 16, 60, 64, 128, 256])
     c["top_k"] = rng.choice([1, 2, 4, 6, 8])
     c["cols"] = _spread(rng, 64, 8192)
-    c["tokens"] = _spread(rng, 1, min(32 * Ki, 64 * Mi // c["cols"] // c["top_k"]))
+    c["tokens"] = _spread(rng, 1, min(32 * Ki, 128 * Mi // SIZE[c["dtype"]] // c["cols"] // c["top_k"]))
     c["masked"] = rng.choice([0.0, 0.0, 0.1])
     c["pad"] = rng.choice([0, 0, 0, 8])
     if op == "combine":
