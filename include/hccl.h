@@ -467,6 +467,158 @@ typedef struct {
 hcclResult_t hccl_comm_trace(hcclComm_t comm, hcclTileTrace_t* out, size_t capacity, size_t* count,
                              uint64_t* clock_khz);
 
+/*
+ * Mixture-of-experts operators: what a layer of experts does around its exchange. A router chooses
+ * experts for every token (hccl_moe_route), the routes are ordered by expert and counted
+ * (hccl_moe_plan: the counts of a rank's row are what hccl_alltoallv_dynamic reads), the tokens'
+ * rows are copied into that order, or quantised into it (hccl_moe_dispatch), the experts multiply
+ * them in 8-bit integers (hccl_moe_product, hccl_moe_quantize), and each token's rows are added up
+ * (hccl_moe_combine). Routing, dispatch and combine have their gradients.
+ *
+ * They work on one rank's arrays in device memory and name no rank. Unlike a collective they are no
+ * work packets: nothing is compiled or kept between calls, they take no trigger and write no
+ * program record, a device error of a collective does not stop them, and while a resident executor
+ * runs they are launched on `stream` as ever (which does not order them with its packets). So they
+ * may be captured into a HIP graph at their first call, and calls on one communicator on several
+ * streams need no order among themselves. Inside a group they fail with hcclUnsupported. On a
+ * communicator without a device their arguments are checked and nothing is enqueued.
+ *
+ * Arrays of rows have a stride (ld*, in elements, at least the row length); other arrays are
+ * packed. Every array must be aligned to its elements; rows at any such alignment keep 16-byte
+ * accesses. An array that is written may not overlap another, except for rows of two arrays of the
+ * same stride that lie side by side. `dtype` is hcclBf16, hcclFp16 or hcclFp32. Sums, softmax
+ * statistics, scores and weights are held in 32 bits, and a result is rounded to its type once. All
+ * results are the same in every call. Zero tokens, rows or columns are allowed.
+ */
+#define HCCL_MAX_EXPERTS 1024
+#define HCCL_MAX_TOP_K 32
+#define HCCL_MAX_GROUPS 32
+
+typedef enum { hcclScoreSoftmax = 0, hcclScoreSigmoid = 1 } hcclScore_t;
+
+/*
+ * A router. The score of expert e of a token with logits l is
+ *   softmax: s_e = exp(l_e - max l) / sum_i exp(l_i - max l)     sigmoid: s_e = 1 / (1 + exp(-l_e))
+ * and its choice value is s_e + bias_e with a bias (which the weights do not have in them), else
+ * l_e (the order of the scores, before any rounding). An expert whose logit, or choice value, is
+ * -inf or NaN is never chosen; its score is 0 if its logit is. Logits of +inf share a softmax among
+ * themselves.
+ * With groups > 1 the experts form groups of experts / groups consecutive ones. A group's value is
+ * the greatest choice value in it (group_top 1), or the sum of its two greatest s_e + bias_e
+ * (group_top 2; of those that may be chosen); only the top_groups greatest groups keep theirs.
+ * The top_k greatest choice values left are chosen, in descending order. Ties go to the lowest
+ * index, of groups and of experts. Where fewer are left, the last choices are -1 with weight 0.
+ * weight_k = scale * s_{e_k}, or with renormalize scale * s_{e_k} / sum_j s_{e_j} (0 if that sum is).
+ */
+typedef struct {
+    uint32_t experts;      /* 1 .. HCCL_MAX_EXPERTS */
+    uint32_t top_k;        /* 1 .. HCCL_MAX_TOP_K, and no more than the kept groups hold */
+    int32_t score;         /* hcclScore_t */
+    uint32_t groups;       /* 1 .. HCCL_MAX_GROUPS, a divisor of experts; 1 = no groups */
+    uint32_t top_groups;   /* 1 .. groups */
+    uint32_t group_top;    /* 1 or 2 */
+    int32_t renormalize;
+    float scale;
+} hcclRouter_t;
+
+/* Softmax, top 1, no groups, no renormalisation, scale 1; experts is left at 0, for the caller to set. */
+hcclResult_t hccl_router_init(hcclRouter_t* router);
+
+/*
+ * Routing. logits: tokens rows of router->experts. bias (fp32[experts]) may be NULL. mask
+ * (uint8[tokens]) may be NULL; a token with mask 0 is not routed: its choices are -1, its weights 0.
+ * index: int32[tokens * top_k], weight: fp32[tokens * top_k] (written).
+ */
+hcclResult_t hccl_moe_route(hcclComm_t comm, const hcclRouter_t* router, const void* logits, size_t ld,
+                            hcclDataType_t dtype, size_t tokens, const float* bias, const uint8_t* mask, int32_t* index,
+                            float* weight, void* stream);
+
+/*
+ * Gradient of the weights with respect to the logits, for the choices in `index` (as hccl_moe_route
+ * wrote them; an entry outside 0 .. experts - 1 adds nothing). With u_k = s_{e_k} and r = sum u (or 1):
+ *   du_k = scale * (g_k - sum_j g_j u_j / r) / r      (the second term only with renormalize)
+ *   softmax: dl_e = s_e * (du_e - sum_k du_k u_k)      sigmoid: dl_e = du_e * s_e * (1 - s_e)
+ * where du_e is 0 for an expert not chosen. The choice itself, and so the bias, has no gradient.
+ * grad_weight: fp32[tokens * top_k]; grad_logits: tokens rows of experts in dtype (written).
+ */
+hcclResult_t hccl_moe_route_backward(hcclComm_t comm, const hcclRouter_t* router, const void* logits, size_t ld,
+                                     hcclDataType_t dtype, size_t tokens, const int32_t* index, const float* grad_weight,
+                                     void* grad_logits, size_t ldg, void* stream);
+
+/* *bytes = the workspace that hccl_moe_plan needs for these sizes (0 for up to 4 096 routes). */
+hcclResult_t hccl_moe_plan_bytes(size_t tokens, uint32_t top_k, uint32_t experts, size_t* bytes);
+
+/*
+ * Order of the routes by expert. index: int32[tokens * top_k]; entries outside 0 .. experts - 1 are
+ * no route. row[t * top_k + k] (written) = the row of that route where all are ordered by expert,
+ * then token, then k; -1 without a route, and where that row is `capacity` or more.
+ * offsets: int64[experts + 1] (written): rows [offsets[e], offsets[e + 1]) are expert e's (clipped
+ * to capacity). rank_counts: int64[nranks] (written) or NULL: rows of the experts that rank d holds,
+ * experts / nranks consecutive ones: this rank's row of hccl_alltoallv_dynamic's sendcounts.
+ * workspace: hccl_moe_plan_bytes bytes, 4-byte aligned, free again once the call's work is done.
+ */
+hcclResult_t hccl_moe_plan(hcclComm_t comm, const int32_t* index, size_t tokens, uint32_t top_k, uint32_t experts,
+                           size_t capacity, int32_t* row, int64_t* offsets, int64_t* rank_counts, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
+/*
+ * Dispatch: out[row[t * top_k + k]] = x[t] for every k; rows outside 0 .. capacity - 1 are skipped,
+ * and rows that none names keep what they held. x: tokens rows of cols; out: capacity rows.
+ * With scale NULL, out has dtype. Else out is int8 and scale fp32[capacity] (written), and the rows
+ * are quantised as by hccl_moe_quantize.
+ * Its gradient is hccl_moe_combine without weights.
+ */
+hcclResult_t hccl_moe_dispatch(hcclComm_t comm, const void* x, size_t ldx, hcclDataType_t dtype, size_t tokens,
+                               size_t cols, const int32_t* row, uint32_t top_k, void* out, size_t ldo, size_t capacity,
+                               float* scale, void* stream);
+
+/*
+ * Combine: out[t] = sum_k weight[t * top_k + k] * z[row[t * top_k + k]], added up in fp32 in
+ * ascending k; rows outside 0 .. capacity - 1 add nothing, and a token without any gets zeros.
+ * weight (fp32[tokens * top_k]) may be NULL: all 1.
+ */
+hcclResult_t hccl_moe_combine(hcclComm_t comm, const void* z, size_t ldz, hcclDataType_t dtype, size_t capacity,
+                              const int32_t* row, uint32_t top_k, const float* weight, size_t tokens, size_t cols,
+                              void* out, size_t ldo, void* stream);
+
+/*
+ * Gradients of hccl_moe_combine for the gradient `grad` of its result (tokens rows of cols):
+ *   grad_z[row] = weight * grad[t]   (capacity rows; rows that none names keep what they held)
+ *   grad_weight[t * top_k + k] = sum_c grad[t, c] * z[row, c]   (fp32; 0 where there is no row)
+ * Either may be NULL; z is read for grad_weight only. No two routes may have the same row.
+ */
+hcclResult_t hccl_moe_combine_backward(hcclComm_t comm, const void* grad, size_t ldg, hcclDataType_t dtype,
+                                       size_t tokens, size_t cols, const void* z, size_t ldz, size_t capacity,
+                                       const int32_t* row, uint32_t top_k, const float* weight, void* grad_z,
+                                       size_t ldgz, float* grad_weight, void* stream);
+
+/*
+ * Rows to 8-bit codes: codes[i, c] = the whole number nearest to v * (127 / m), ties to even, scale[i] =
+ * m / 127, with m = max_c |v| (quotients and product in fp32). v = x[i, c], or with `gated`, where x
+ * has 2 * cols columns, silu(x[i, c]) * x[i, cols + c] (in fp32, not rounded in between). A row whose
+ * m is below 2^-119 has codes and scale 0; one with an infinity or NaN has codes 0 and that as its
+ * scale, so that every product with it is NaN. limit (int64, device) may be NULL: only the first
+ * *limit rows are read and written.
+ */
+hcclResult_t hccl_moe_quantize(hcclComm_t comm, const void* x, size_t ldx, hcclDataType_t dtype, size_t rows,
+                               size_t cols, int gated, const int64_t* limit, int8_t* codes, size_t ldq, float* scale,
+                               void* stream);
+
+/*
+ * The experts' product: out[m, n] = scale[m] * weight_scale[e, n] * sum_k codes[m, k] * weights[e, n, k],
+ * the sum exact in 32 bits (inner is at most 131 071), then one rounding to dtype.
+ * codes: rows rows of inner; weights: experts * cols rows of inner (ldb apart).
+ * offsets (int64[segments + 1], device, ascending): rows [offsets[s], offsets[s + 1]) are segment
+ * s's and use expert s % experts, so that the rows that an exchange brought in, ordered by source and
+ * then by expert, are segments as they lie. segments is a multiple of experts; segments may be empty.
+ * Offsets outside 0 .. rows are clipped, and rows in no segment are left as they are. offsets may be
+ * NULL with one expert: every row uses it.
+ */
+hcclResult_t hccl_moe_product(hcclComm_t comm, const int8_t* codes, size_t lda, const float* scale, size_t rows,
+                              size_t inner, const int8_t* weights, size_t ldb, const float* weight_scale, size_t cols,
+                              size_t experts, const int64_t* offsets, size_t segments, void* out, size_t ldo,
+                              hcclDataType_t dtype, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

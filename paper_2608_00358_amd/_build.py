@@ -25,8 +25,10 @@ OBJDIR = os.path.join(PKG, "_build")
 ARCH = "gfx950"
 
 HOST_SOURCES = ["compiler.cpp", "validate.cpp"]
-EXECUTOR_SOURCES = ["executor_generic.hip", "executor_resident.hip", "executor.hip", "executor_uniform.hip", "executor_dynamic.hip"]
-HIP_SOURCES = EXECUTOR_SOURCES + ["api.cpp"]
+# every source with kernels: the executor's and the mixture-of-experts operators'
+EXECUTOR_SOURCES = ["executor_generic.hip", "executor_resident.hip", "executor.hip", "executor_uniform.hip", "executor_dynamic.hip",
+                    "moe_route.hip", "moe_rows.hip", "moe_product.hip"]
+HIP_SOURCES = EXECUTOR_SOURCES + ["api.cpp", "moe_api.cpp"]
 
 HIPCC_FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-Wall",

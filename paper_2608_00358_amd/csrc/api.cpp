@@ -24,6 +24,7 @@
 
 #include "compiler.h"
 #include "hccl.h"
+#include "moe.h"
 #include "program.h"
 
 namespace hccl {
@@ -925,6 +926,26 @@ hcclResult_t check_ptr_arrays(const void* a, const void* b) {
 }
 
 }  // namespace
+
+// The mixture-of-experts operators' side of a communicator (moe_api.cpp).
+namespace hccl {
+
+hcclResult_t api_fail(hcclResult_t code, const char* msg) { return fail(code, msg); }
+hcclResult_t api_hip_fail(hipError_t e, const char* what) { return hip_fail(e, what); }
+
+hcclResult_t operator_device(hcclComm_t comm, int* device) {
+    hcclResult_t r;
+    if ((r = check_comm(comm))) return r;
+    // A group's collectives run at its end, so an operator inside it would overtake those called before it.
+    if (comm->group_depth > 0) return fail(hcclUnsupported, "operators cannot be called inside a group");
+    *device = comm->device;
+    return hcclSuccess;
+}
+
+int api_ranks(hcclComm_t comm) { return comm->nranks; }
+int api_cus(hcclComm_t comm) { return comm->cus; }
+
+}  // namespace hccl
 
 extern "C" {
 

@@ -1,0 +1,318 @@
+// moe_route.hip -- routing: logits to chosen experts and weights, and the logits' gradient.
+//
+// A token's experts lie in the registers of L neighbouring lanes, N consecutive ones each, so a wave
+// routes 64 / L tokens and nothing is exchanged beyond those lanes. One round of the top k is a
+// maximum over N registers and L lanes; the maximum of the exponentials' argument, their sum and the
+// chosen weights' sum are reductions over the same lanes. All of it is held in 32 bits.
+//
+//   s_e = exp(l_e - max l) / sum, or 1 / (1 + exp(-l_e))
+//   w_k = scale * s_{i_k} (/ sum_j s_{i_j})
+#include "moe_device.h"
+
+namespace hccl {
+namespace {
+
+constexpr int kRouteThreads = 256;
+
+// N logits of a lane, the first of them expert e0; experts past the end, and those whose logit is
+// minus infinity or no number, are -inf: never chosen, with score 0.
+template <int DT, int N>
+__device__ __forceinline__ void load_logits(const char* row, uint32_t e0, uint32_t experts, bool on, float (&l)[N]) {
+    constexpr int ES = kSize<DT>;
+#pragma unroll
+    for (int j = 0; j < N; ++j) l[j] = -kInf;
+    if (!on || e0 >= experts) return;
+    if (e0 + N <= experts) {
+        constexpr int V = kVecOf<DT>;
+        if constexpr (N >= V) {
+#pragma unroll
+            for (int q = 0; q < N / V; ++q) {
+                float x[V];
+                widen<DT>(load16<ES>(row + (uint64_t)(e0 + q * V) * ES), x);
+#pragma unroll
+                for (int i = 0; i < V; ++i) l[q * V + i] = x[i];
+            }
+        } else {
+            static_assert(N * ES == 8, "four 16-bit logits");
+            const typename Loose<ES>::x2 r = *gptr<typename Loose<ES>::x2>(row + (uint64_t)e0 * ES);
+#pragma unroll
+            for (int j = 0; j < N; ++j) l[j] = widen1<DT>((r[j / 2] >> (16 * (j & 1))) & 0xffffu);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (e0 + j < experts) l[j] = widen1<DT>(load1<ES>(row + (uint64_t)(e0 + j) * ES));
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) l[j] = l[j] > -kInf ? l[j] : -kInf;
+}
+
+// exp(l - m) with m the greatest logit: logits of +inf share the weight among themselves.
+__device__ __forceinline__ float exp_below(float l, float m) {
+    return l == -kInf ? 0.0f : l == m ? 1.0f : expf(l - m);
+}
+__device__ __forceinline__ float sigmoid(float l) { return 1.0f / (1.0f + expf(-l)); }
+
+// The order of a 16-bit float as an unsigned number (0 is none of them), and back.
+template <int DT>
+__device__ __forceinline__ uint32_t order16(float l) {
+    const uint32_t b = narrow1<DT>(l + 0.0f);  // (-0 counts as 0; l came from 16 bits, so nothing is rounded)
+    return b & 0x8000u ? (~b & 0xffffu) : (b | 0x8000u);
+}
+template <int DT>
+__device__ __forceinline__ float value16(uint32_t o) { return widen1<DT>(o & 0x8000u ? o & 0x7fffu : ~o & 0xffffu); }
+
+// PACK: the choice is by 16-bit logits, so logit and expert fit one 32-bit key, greater for the
+// lower expert among equals: a round is one maximum. Otherwise a round is the greatest choice score,
+// then the lowest expert that has it.
+template <int DT, int L, int N, bool PACK, bool GROUPED>
+__global__ __launch_bounds__(kRouteThreads) void hccl_moe_route_kernel(RouteArgs a) {
+    constexpr int ES = kSize<DT>;
+    const uint32_t sub = threadIdx.x & (L - 1), slot = threadIdx.x / L;
+    const uint64_t t = (uint64_t)blockIdx.x * (kRouteThreads / L) + slot;
+    const bool on = t < a.tokens;
+    const char* row = (const char*)a.logits + t * a.ld * ES;
+    const uint32_t e0 = sub * N;
+    float l[N];
+    load_logits<DT, N>(row, e0, a.experts, on, l);
+
+    float m = -kInf, total = 1.0f;
+    if (!a.sigmoid) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) m = fmaxf(m, l[j]);
+        m = max_lanes<L>(m);
+        total = 0.0f;
+#pragma unroll
+        for (int j = 0; j < N; ++j) total += exp_below(l[j], m);
+        total = sum_lanes<L>(total);
+    }
+    auto score = [&](float x) { return x == -kInf ? 0.0f : a.sigmoid ? sigmoid(x) : exp_below(x, m) / total; };
+
+    uint32_t mine = ~0u;   // lane k keeps choice k
+    float logit = -kInf;
+    if constexpr (PACK) {
+        uint32_t key[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) key[j] = l[j] == -kInf ? 0u : order16<DT>(l[j]) << 16 | (0xffffu - (e0 + j));
+        for (uint32_t k = 0; k < a.top_k; ++k) {
+            uint32_t best = key[0];
+#pragma unroll
+            for (int j = 1; j < N; ++j) best = best > key[j] ? best : key[j];
+            best = maxu_lanes<L>(best);
+            if (sub == k && best) {
+                mine = 0xffffu - (best & 0xffffu);
+                logit = value16<DT>(best >> 16);
+            }
+#pragma unroll
+            for (int j = 0; j < N; ++j) key[j] = key[j] == best ? 0u : key[j];
+        }
+    } else {
+        float c[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            c[j] = l[j];
+            if (a.bias && l[j] > -kInf) {
+                const float v = score(l[j]) + a.bias[e0 + j];
+                c[j] = v > -kInf ? v : -kInf;
+            }
+        }
+        if constexpr (GROUPED) {
+            __shared__ float seen[kRouteThreads * N];
+            float* part = seen + slot * (L * N);
+#pragma unroll
+            for (int j = 0; j < N; ++j) part[e0 + j] = a.group_top == 2 && !a.bias && l[j] > -kInf ? score(l[j]) : c[j];
+            __syncthreads();
+            // lane g: the greatest one or two scores of group g, of those that may be chosen
+            float one = -kInf, two = -kInf;
+            if (sub < a.groups) {
+                uint32_t i = sub % a.group_size;  // (lanes begin apart from each other: different banks)
+                for (uint32_t n = 0; n < a.group_size; ++n) {
+                    const float v = part[sub * a.group_size + i];
+                    two = fmaxf(two, fminf(one, v));
+                    one = fmaxf(one, v);
+                    if (++i == a.group_size) i = 0;
+                }
+            }
+            float left = a.group_top == 2 && two > -kInf ? one + two : one;
+            uint32_t kept = 0;
+            for (uint32_t k = 0; k < a.top_groups; ++k) {
+                const float best = max_lanes<L>(left);
+                const uint32_t g = minu_lanes<L>(best > -kInf && left == best ? sub : 255u);
+                if (g < 32u) kept |= 1u << g;
+                if (sub == g) left = -kInf;
+            }
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const uint32_t g = ((e0 + j) * a.group_magic) >> 20;
+                if (g < 32u && !((kept >> g) & 1u)) c[j] = -kInf;
+            }
+        }
+        for (uint32_t k = 0; k < a.top_k; ++k) {
+            float best = c[0];
+#pragma unroll
+            for (int j = 1; j < N; ++j) best = fmaxf(best, c[j]);
+            best = max_lanes<L>(best);
+            uint32_t e = ~0u;
+#pragma unroll
+            for (int j = N - 1; j >= 0; --j) e = c[j] == best ? e0 + j : e;
+            e = minu_lanes<L>(e);
+            if (best == -kInf) e = ~0u;  // none is left
+            if (sub == k) mine = e;
+#pragma unroll
+            for (int j = 0; j < N; ++j) c[j] = e0 + j == e ? -kInf : c[j];
+        }
+        if (on && mine != ~0u) logit = widen1<DT>(load1<ES>(row + (uint64_t)mine * ES));
+    }
+
+    if (on && a.mask && !a.mask[t]) {
+        mine = ~0u;
+        logit = -kInf;
+    }
+    float w = score(logit);
+    if (a.renormalize) {
+        const float sum = sum_lanes<L>(w);
+        w = sum > 0.0f ? w / sum : 0.0f;
+    }
+    if (on && sub < a.top_k) {
+        a.index[t * a.top_k + sub] = (int32_t)mine;
+        a.weight[t * a.top_k + sub] = w * a.scale;
+    }
+}
+
+// With r = sum_k u_k (or 1), u_k = s_{i_k}, w_k = scale u_k / r:
+//   du_k = scale (g_k - sum_j g_j u_j / r) / r (the second term only with the sum)
+//   softmax: dl_e = s_e (du_e - sum_k du_k u_k)     sigmoid: dl_e = du_e s_e (1 - s_e)
+// Scores are computed again from the logits: reading them costs less than storing them would.
+// The chosen experts' du go to the lanes that hold those experts through LDS.
+template <int DT, int L, int N>
+__global__ __launch_bounds__(kRouteThreads) void hccl_moe_route_backward_kernel(RouteBackwardArgs a) {
+    constexpr int ES = kSize<DT>;
+    __shared__ float slope[kRouteThreads * N];
+    const uint32_t sub = threadIdx.x & (L - 1), slot = threadIdx.x / L;
+    const uint64_t t = (uint64_t)blockIdx.x * (kRouteThreads / L) + slot;
+    const bool on = t < a.tokens;
+    const char* row = (const char*)a.logits + t * a.ld * ES;
+    const uint32_t e0 = sub * N;
+    float* part = slope + slot * (L * N);
+    uint32_t mine = ~0u;
+    float g = 0.0f, logit = -kInf;
+    if (on && sub < a.top_k) {
+        mine = (uint32_t)a.index[t * a.top_k + sub];
+        if (mine < a.experts) {
+            g = a.grad_weight[t * a.top_k + sub] * a.scale;
+            logit = widen1<DT>(load1<ES>(row + (uint64_t)mine * ES));
+            logit = logit > -kInf ? logit : -kInf;
+        }
+    }
+    float l[N];
+    load_logits<DT, N>(row, e0, a.experts, on, l);
+#pragma unroll
+    for (int j = 0; j < N; ++j) part[e0 + j] = 0.0f;
+    float m = -kInf, total = 1.0f;
+    if (!a.sigmoid) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) m = fmaxf(m, l[j]);
+        m = max_lanes<L>(m);
+#pragma unroll
+        for (int j = 0; j < N; ++j) l[j] = exp_below(l[j], m);
+        total = 0.0f;
+#pragma unroll
+        for (int j = 0; j < N; ++j) total += l[j];
+        total = sum_lanes<L>(total);
+    }
+    const float u = logit == -kInf ? 0.0f : a.sigmoid ? sigmoid(logit) : exp_below(logit, m) / total;
+    float du = g, common = 0.0f;
+    if (a.renormalize) {
+        // (the weights' sum is fixed, so sum_k du_k u_k is nothing)
+        const float r = sum_lanes<L>(u), mean = sum_lanes<L>(g * u);
+        du = r > 0.0f ? (g - mean / r) / r : 0.0f;
+    } else if (!a.sigmoid) {
+        common = sum_lanes<L>(g * u);
+    }
+    __syncthreads();
+    if (mine < a.experts) atomicAdd(&part[mine], du);  // (a router names an expert once)
+    __syncthreads();
+    if (!on || e0 >= a.experts) return;
+    float d[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        if (a.sigmoid) {
+            const float s = l[j] == -kInf ? 0.0f : sigmoid(l[j]);
+            d[j] = part[e0 + j] * s * (1.0f - s);
+        } else {
+            d[j] = l[j] == 0.0f ? 0.0f : l[j] / total * (part[e0 + j] - common);
+        }
+    }
+    char* out = (char*)a.grad_logits + t * a.ldg * ES;
+    if (e0 + N <= a.experts) {
+        constexpr int V = kVecOf<DT>;
+        if constexpr (N >= V) {
+#pragma unroll
+            for (int q = 0; q < N / V; ++q) {
+                float x[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) x[i] = d[q * V + i];
+                store16<ES>(out + (uint64_t)(e0 + q * V) * ES, narrow<DT>(x));
+            }
+            return;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+        if (e0 + j < a.experts) store1<ES>(out + (uint64_t)(e0 + j) * ES, narrow1<DT>(d[j]));
+}
+
+// Lanes for a token: enough for its experts at N each, its k choices and its groups. 16 lanes with
+// 4 or 8 experts each take up to 128 experts, then 32 and 64 lanes with 8, then 64 with 16.
+template <typename F>
+hipError_t by_lanes(uint32_t experts, uint32_t across, F f) {
+    if (across <= 16 && experts <= 64) return f(std::integral_constant<int, 16>(), std::integral_constant<int, 4>());
+    if (across <= 16 && experts <= 128) return f(std::integral_constant<int, 16>(), std::integral_constant<int, 8>());
+    if (experts <= 256) return f(std::integral_constant<int, 32>(), std::integral_constant<int, 8>());
+    if (experts <= 512) return f(std::integral_constant<int, 64>(), std::integral_constant<int, 8>());
+    return f(std::integral_constant<int, 64>(), std::integral_constant<int, 16>());
+}
+
+// A launch's threads are counted in 32 bits.
+bool too_many(uint64_t tokens, uint32_t lanes) { return (tokens + kRouteThreads) * lanes > 0xffffffffull; }
+
+template <int DT>
+hipError_t route_type(const RouteArgs& a, hipStream_t s) {
+    const bool grouped = a.top_groups < a.groups;
+    return by_lanes(a.experts, a.top_k > a.groups ? a.top_k : a.groups, [&](auto lanes, auto each) {
+        constexpr int L = decltype(lanes)::value, N = decltype(each)::value;
+        if (too_many(a.tokens, L)) return hipErrorInvalidConfiguration;
+        const dim3 grid((uint32_t)((a.tokens + kRouteThreads / L - 1) / (kRouteThreads / L))), block(kRouteThreads);
+        if (grouped) {
+            hipLaunchKernelGGL((hccl_moe_route_kernel<DT, L, N, false, true>), grid, block, 0, s, a);
+        } else if (DT != hcclFp32 && !a.bias) {
+            hipLaunchKernelGGL((hccl_moe_route_kernel<DT, L, N, DT != hcclFp32, false>), grid, block, 0, s, a);
+        } else {
+            hipLaunchKernelGGL((hccl_moe_route_kernel<DT, L, N, false, false>), grid, block, 0, s, a);
+        }
+        return hipGetLastError();
+    });
+}
+
+template <int DT>
+hipError_t backward_type(const RouteBackwardArgs& a, hipStream_t s) {
+    return by_lanes(a.experts, a.top_k, [&](auto lanes, auto each) {
+        constexpr int L = decltype(lanes)::value, N = decltype(each)::value;
+        if (too_many(a.tokens, L)) return hipErrorInvalidConfiguration;
+        const dim3 grid((uint32_t)((a.tokens + kRouteThreads / L - 1) / (kRouteThreads / L))), block(kRouteThreads);
+        hipLaunchKernelGGL((hccl_moe_route_backward_kernel<DT, L, N>), grid, block, 0, s, a);
+        return hipGetLastError();
+    });
+}
+
+}  // namespace
+
+hipError_t launch_route(const RouteArgs& a, hcclDataType_t dt, hipStream_t s) {
+    return dt == hcclBf16 ? route_type<hcclBf16>(a, s) : dt == hcclFp16 ? route_type<hcclFp16>(a, s) : route_type<hcclFp32>(a, s);
+}
+
+hipError_t launch_route_backward(const RouteBackwardArgs& a, hcclDataType_t dt, hipStream_t s) {
+    return dt == hcclBf16 ? backward_type<hcclBf16>(a, s) : dt == hcclFp16 ? backward_type<hcclFp16>(a, s) : backward_type<hcclFp32>(a, s);
+}
+
+}  // namespace hccl

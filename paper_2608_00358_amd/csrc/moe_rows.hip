@@ -1,0 +1,479 @@
+// moe_rows.hip -- the rows of a mixture-of-experts layer: their order by expert (plan), the tokens'
+// rows copied there (dispatch), quantised to 8 bits (quantize, dispatch), and the experts' rows added
+// up for each token (combine) with its gradients. All of them are bound by memory.
+#include "moe_device.h"
+
+namespace hccl {
+namespace {
+
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+
+// ------------------------------------------------------------------------------------------ plan
+// Routes are ordered by expert, then as they come (token, slot). The row of a route is the number of
+// routes of lower experts, plus that of earlier routes of its own. Blocks take consecutive routes;
+// the first kernel counts every block's routes per expert, and in the second a block adds up the
+// counts before its own and ranks its routes among themselves: wave by wave, a lane's peers (equal
+// expert) are found by one ballot for each bit of the expert's number. Only sums of whole numbers
+// are taken in no fixed order.
+
+__global__ __launch_bounds__(kPlanThreads) void hccl_moe_count_kernel(PlanArgs a) {
+    __shared__ uint32_t n[HCCL_MAX_EXPERTS];
+    for (uint32_t e = threadIdx.x; e < a.experts; e += kPlanThreads) n[e] = 0;
+    __syncthreads();
+    for (uint32_t s = 0; s < a.steps; ++s) {
+        const uint64_t i = ((uint64_t)blockIdx.x * a.steps + s) * kPlanThreads + threadIdx.x;
+        const uint32_t e = i < a.routes ? (uint32_t)a.index[i] : ~0u;
+        if (e < a.experts) atomicAdd(&n[e], 1u);
+    }
+    __syncthreads();
+    for (uint32_t e = threadIdx.x; e < a.experts; e += kPlanThreads) a.hist[(uint64_t)blockIdx.x * a.experts + e] = n[e];
+}
+
+static_assert(kPlanThreads == HCCL_MAX_EXPERTS, "the second kernel has a thread for every expert");
+
+__global__ __launch_bounds__(kPlanThreads) void hccl_moe_plan_kernel(PlanArgs a) {
+    constexpr uint32_t kPlanWaves = kPlanThreads / 64;
+    __shared__ uint32_t before[HCCL_MAX_EXPERTS];   // routes of an expert in earlier blocks, then its next row
+    __shared__ uint32_t first[HCCL_MAX_EXPERTS + 1];  // routes of an expert, then its first row
+    __shared__ uint16_t seen[kPlanWaves][HCCL_MAX_EXPERTS];
+    __shared__ uint32_t sums[kPlanWaves];
+    const uint32_t tid = threadIdx.x, lane = tid & 63, w = tid >> 6, E = a.experts;
+    before[tid] = 0;
+    first[tid] = 0;
+    __syncthreads();
+    if (a.blocks == 1) {
+        for (uint32_t s = 0; s < a.steps; ++s) {
+            const uint64_t i = (uint64_t)s * kPlanThreads + tid;
+            const uint32_t e = i < a.routes ? (uint32_t)a.index[i] : ~0u;
+            if (e < E) atomicAdd(&first[e], 1u);
+        }
+    } else {
+        uint32_t width = 64;
+        while (width < E) width *= 2;
+        const uint32_t e = tid & (width - 1), stride = kPlanThreads / width;
+        if (e < E) {
+            uint32_t all = 0, mine = 0;
+            for (uint32_t b = tid / width; b < a.blocks; b += stride) {
+                const uint32_t v = a.hist[(uint64_t)b * E + e];
+                all += v;
+                if (b < blockIdx.x) mine += v;
+            }
+            atomicAdd(&first[e], all);
+            atomicAdd(&before[e], mine);
+        }
+    }
+    __syncthreads();
+    // exclusive sum over the experts, one per thread
+    const uint32_t n = first[tid];
+    uint32_t incl = n;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const uint32_t v = (uint32_t)__shfl_up((int)incl, d);
+        if (lane >= (uint32_t)d) incl += v;
+    }
+    if (lane == 63) sums[w] = incl;
+    __syncthreads();
+    uint32_t base = 0;
+#pragma unroll
+    for (uint32_t q = 0; q < kPlanWaves; ++q)
+        if (q < w) base += sums[q];
+    const uint32_t at = base + incl - n;
+    first[tid] = at;  // (nobody else reads it before the barrier)
+    if (tid == kPlanThreads - 1) first[kPlanThreads] = at + n;
+    before[tid] += at;
+    __syncthreads();
+    if (blockIdx.x == 0) {
+        auto clip = [&](uint32_t v) { return (int64_t)(v < a.capacity ? v : a.capacity); };
+        for (uint32_t e = tid; e <= E; e += kPlanThreads) a.offsets[e] = clip(first[e]);
+        if (a.rank_counts && tid < a.ranks) {
+            const uint32_t each = E / a.ranks;
+            a.rank_counts[tid] = clip(first[(tid + 1) * each]) - clip(first[tid * each]);
+        }
+    }
+    const uint32_t bits = 32 - __builtin_clz(E);  // (E itself stands for no expert)
+    for (uint32_t s = 0; s < a.steps; ++s) {
+        const uint64_t i = ((uint64_t)blockIdx.x * a.steps + s) * kPlanThreads + tid;
+        for (uint32_t e = lane; e < E; e += 64) seen[w][e] = 0;
+        __syncthreads();
+        uint32_t e = i < a.routes ? (uint32_t)a.index[i] : E;
+        if (e > E) e = E;
+        uint64_t peers = ~0ull;
+        for (uint32_t b = 0; b < bits; ++b) {
+            const uint64_t set = __ballot((e >> b) & 1u);
+            peers &= ((e >> b) & 1u) ? set : ~set;
+        }
+        const uint32_t rank = (uint32_t)__popcll(peers & ((1ull << lane) - 1));
+        if (e < E && rank == 0) seen[w][e] = (uint16_t)__popcll(peers);
+        __syncthreads();
+        uint32_t run = 0;
+        if (tid < E) {
+#pragma unroll
+            for (uint32_t q = 0; q < kPlanWaves; ++q) {
+                const uint32_t c = seen[q][tid];
+                seen[q][tid] = (uint16_t)run;
+                run += c;
+            }
+        }
+        __syncthreads();
+        if (i < a.routes) {
+            int32_t r = -1;
+            if (e < E) {
+                const uint32_t at_row = before[e] + seen[w][e] + rank;
+                if (at_row < a.capacity) r = (int32_t)at_row;
+            }
+            a.row[i] = r;
+        }
+        __syncthreads();
+        if (tid < E) before[tid] += run;
+    }
+}
+
+// -------------------------------------------------------------------------------------- dispatch
+// A wave copies a piece of a token's row to every row that the token has: it is read once. Pieces of
+// kPieceVecs vectors per lane keep loads in flight and give few tokens enough waves.
+constexpr uint32_t kPieceVecs = 4;
+
+template <int ES>
+__global__ __launch_bounds__(kThreads) void hccl_moe_dispatch_kernel(DispatchArgs a, uint32_t pieces) {
+    constexpr uint64_t V = 16 / ES;
+    const uint32_t lane = threadIdx.x & 63;
+    const uint64_t id = (uint64_t)blockIdx.x * kWaves + first_lane(threadIdx.x >> 6);
+    const uint64_t t = id / pieces, c0 = (id % pieces) * (kPieceVecs * kWave * V);
+    if (t >= a.tokens) return;
+    const uint32_t mine = lane < a.top_k ? (uint32_t)a.row[t * a.top_k + lane] : ~0u;
+    const char* src = (const char*)a.x + t * a.ldx * ES;
+    v4u v[kPieceVecs];
+#pragma unroll
+    for (uint32_t u = 0; u < kPieceVecs; ++u) v[u] = load_row<ES>(src, c0 + (u * kWave + lane) * V, a.cols);
+    for (uint32_t k = 0; k < a.top_k; ++k) {
+        const uint32_t r = at_lane(mine, k);
+        if (r >= a.capacity || (int32_t)r < 0) continue;
+        char* dst = (char*)a.out + (uint64_t)r * a.ldo * ES;
+#pragma unroll
+        for (uint32_t u = 0; u < kPieceVecs; ++u) store_row<ES>(dst, c0 + (u * kWave + lane) * V, a.cols, v[u]);
+    }
+}
+
+// -------------------------------------------------------------------------------------- quantize
+// code = rint(x * (127 / max|x|)), scale = max|x| / 127: the quotient once for a row. The maximum is
+// taken of the values' bits without their sign, which orders infinities and NaN above the rest: such
+// a row gets codes of 0 and that scale, so that its products are NaN. Rows below 2^-119 count as 0
+// (127 over them would overflow).
+__device__ __forceinline__ void row_scale(uint32_t top, float& inv, float& scale) {
+    const float m = __uint_as_float(top);
+    const bool none = top < 0x04000000u;  // 2^-119
+    const bool finite = top < 0x7f800000u;
+    inv = none || !finite ? 0.0f : 127.0f / m;
+    scale = none ? 0.0f : finite ? m / 127.0f : m;
+}
+
+__device__ __forceinline__ uint32_t code4(float a, float b, float c, float d, float inv) {
+    const int32_t i = (int32_t)rintf(a * inv), j = (int32_t)rintf(b * inv), k = (int32_t)rintf(c * inv), l = (int32_t)rintf(d * inv);
+    return ((uint32_t)i & 0xffu) | ((uint32_t)j & 0xffu) << 8 | ((uint32_t)k & 0xffu) << 16 | (uint32_t)l << 24;
+}
+
+// Values of vector e of a row: x, or silu(x) * (the row's second half).
+template <int DT, bool GATED>
+__device__ __forceinline__ void row_values(const char* src, uint64_t e, uint64_t cols, float (&x)[kVecOf<DT>]) {
+    constexpr int ES = kSize<DT>, V = kVecOf<DT>;
+    widen<DT>(load_row<ES>(src, e, cols), x);
+    if constexpr (GATED) {
+        float up[V];
+        widen<DT>(load_row<ES>(src + cols * ES, e, cols), up);
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] = x[i] * (1.0f / (1.0f + expf(-x[i]))) * up[i];
+    }
+}
+
+// W waves a row; a lane keeps up to kKeep vectors between the two passes and reads longer rows twice.
+constexpr int kKeep = 8;
+
+template <int DT, bool GATED, int W>
+__global__ __launch_bounds__(kThreads) void hccl_moe_quantize_kernel(QuantizeArgs a) {
+    constexpr int V = kVecOf<DT>, ES = kSize<DT>;
+    __shared__ uint32_t tops[kWaves];
+    const uint32_t lane = threadIdx.x & 63, w = first_lane(threadIdx.x >> 6);
+    const uint64_t t = (uint64_t)blockIdx.x * (kWaves / W) + w / W;
+    const uint32_t at = W == 1 ? lane : threadIdx.x;
+    constexpr uint64_t step = (uint64_t)W * kWave * V;
+    const bool on = t < a.rows && (!a.limit || (int64_t)t < *a.limit);
+    const char* src = (const char*)a.x + t * a.ldx * ES;
+    float x[kKeep][V];
+    uint32_t top = 0;
+    if (on) {
+#pragma unroll
+        for (int u = 0; u < kKeep; ++u) {
+            const uint64_t e = u * step + at * V;
+#pragma unroll
+            for (int i = 0; i < V; ++i) x[u][i] = 0.0f;
+            if (e < a.cols) row_values<DT, GATED>(src, e, a.cols, x[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < kKeep; ++u)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const uint32_t b = __float_as_uint(x[u][i]) & 0x7fffffffu;
+                top = top > b ? top : b;
+            }
+        for (uint64_t e = kKeep * step + at * V; e < a.cols; e += step) {
+            float y[V];
+            row_values<DT, GATED>(src, e, a.cols, y);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const uint32_t b = __float_as_uint(y[i]) & 0x7fffffffu;
+                top = top > b ? top : b;
+            }
+        }
+    }
+    top = maxu_lanes<64>(top);
+    if constexpr (W > 1) {
+        if (lane == 0) tops[w] = top;
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < kWaves; ++q) top = top > tops[q] ? top : tops[q];
+    }
+    if (!on) return;
+    float inv, scale;
+    row_scale(top, inv, scale);
+    const uint32_t copies = a.row ? a.top_k : 1u;
+    const uint32_t mine = !a.row ? (uint32_t)t : lane < copies ? (uint32_t)a.row[t * a.top_k + lane] : ~0u;
+    auto store = [&](uint64_t e, const float (&y)[V]) {
+        uint32_t lo, hi = 0;
+        // (a row of infinities times 0 is no number, and no number has no code)
+        if (inv == 0.0f) lo = 0;
+        else {
+            lo = code4(y[0], y[1], y[2], y[3], inv);
+            if constexpr (V == 8) hi = code4(y[4], y[5], y[6], y[7], inv);
+        }
+        for (uint32_t k = 0; k < copies; ++k) {
+            const uint32_t r = a.row ? at_lane(mine, k) : (uint32_t)t;
+            if (r >= a.capacity || (int32_t)r < 0) continue;
+            char* dst = (char*)a.codes + (uint64_t)r * a.ldq + e;
+            if (e + V <= a.cols) {
+                if constexpr (V == 8) *gptr<typename Loose<1>::x2>(dst) = typename Loose<1>::x2{lo, hi};
+                else *gptr<typename Loose<1>::x1>(dst) = lo;
+            } else {
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    if (e + i < a.cols) *gptr<uint8_t>(dst + i) = (uint8_t)((i < 4 ? lo : hi) >> (8 * (i & 3)));
+            }
+        }
+    };
+#pragma unroll
+    for (int u = 0; u < kKeep; ++u) {
+        const uint64_t e = u * step + at * V;
+        if (e < a.cols) store(e, x[u]);
+    }
+    for (uint64_t e = kKeep * step + at * V; e < a.cols; e += step) {
+        float y[V];
+        row_values<DT, GATED>(src, e, a.cols, y);
+        store(e, y);
+    }
+    if (at == 0) {
+        for (uint32_t k = 0; k < copies; ++k) {
+            const uint32_t r = a.row ? (uint32_t)a.row[t * a.top_k + k] : (uint32_t)t;
+            if (r < a.capacity && (int32_t)r >= 0) a.scale[r] = scale;
+        }
+    }
+}
+
+// --------------------------------------------------------------------------------------- combine
+// y_t = sum_k w_k z_{row k}, added up in 32 bits in the order of the slots. A wave takes a piece of a
+// token; the loads of kBatch rows are in flight together.
+constexpr int kBatch = 4;
+constexpr int kCombineVecs = 2;
+
+template <int DT>
+__global__ __launch_bounds__(kThreads) void hccl_moe_combine_kernel(CombineArgs a, uint32_t pieces) {
+    constexpr int V = kVecOf<DT>, ES = kSize<DT>;
+    const uint32_t lane = threadIdx.x & 63;
+    const uint64_t id = (uint64_t)blockIdx.x * kWaves + first_lane(threadIdx.x >> 6);
+    const uint64_t t = id / pieces, c0 = (id % pieces) * (kCombineVecs * kWave * V);
+    if (t >= a.tokens) return;
+    uint32_t mine = lane < a.top_k ? (uint32_t)a.row[t * a.top_k + lane] : ~0u;
+    if (mine >= a.capacity) mine = ~0u;
+    const float weight = a.weight && lane < a.top_k ? a.weight[t * a.top_k + lane] : 1.0f;
+    float acc[kCombineVecs][V];
+#pragma unroll
+    for (int u = 0; u < kCombineVecs; ++u)
+#pragma unroll
+        for (int i = 0; i < V; ++i) acc[u][i] = 0.0f;
+    for (uint32_t k = 0; k < a.top_k; k += kBatch) {
+        v4u z[kBatch][kCombineVecs];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            const uint32_t r = k + j < a.top_k ? at_lane(mine, k + j) : ~0u;
+            if ((int32_t)r < 0) continue;
+            const char* src = (const char*)a.z + (uint64_t)r * a.ldz * ES;
+#pragma unroll
+            for (int u = 0; u < kCombineVecs; ++u) z[j][u] = load_row<ES>(src, c0 + (u * kWave + lane) * V, a.cols);
+        }
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            const uint32_t r = k + j < a.top_k ? at_lane(mine, k + j) : ~0u;
+            if ((int32_t)r < 0) continue;
+            const float w = __uint_as_float(at_lane(__float_as_uint(weight), k + j));
+#pragma unroll
+            for (int u = 0; u < kCombineVecs; ++u) {
+                float x[V];
+                widen<DT>(z[j][u], x);
+#pragma unroll
+                for (int i = 0; i < V; ++i) acc[u][i] += w * x[i];
+            }
+        }
+    }
+    char* dst = (char*)a.out + t * a.ldo * ES;
+#pragma unroll
+    for (int u = 0; u < kCombineVecs; ++u) store_row<ES>(dst, c0 + (u * kWave + lane) * V, a.cols, narrow<DT>(acc[u]));
+}
+
+// dz_{row k} = w_k dy_t, dw_k = <dy_t, z_{row k}>. A block of W waves takes a token: the products are
+// added up in a lane, over the lanes and then over the waves, always in the same order.
+template <int DT, int W>
+__global__ __launch_bounds__(W * 64) void hccl_moe_combine_backward_kernel(CombineBackwardArgs a) {
+    constexpr int V = kVecOf<DT>, ES = kSize<DT>;
+    __shared__ float parts[W][kBatch];
+    const uint32_t lane = threadIdx.x & 63, w = first_lane(threadIdx.x >> 6);
+    const uint64_t t = blockIdx.x;
+    uint32_t mine = lane < a.top_k ? (uint32_t)a.row[t * a.top_k + lane] : ~0u;
+    if (mine >= a.capacity) mine = ~0u;
+    const float weight = lane < a.top_k ? a.weight[t * a.top_k + lane] : 0.0f;
+    const char* dy = (const char*)a.grad + t * a.ldg * ES;
+    for (uint32_t k = 0; k < a.top_k; k += kBatch) {
+        uint32_t r[kBatch];
+        float wk[kBatch], dot[kBatch];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            r[j] = k + j < a.top_k ? at_lane(mine, k + j) : ~0u;
+            wk[j] = __uint_as_float(at_lane(__float_as_uint(weight), k + j));
+            dot[j] = 0.0f;
+        }
+        for (uint64_t e = threadIdx.x * V; e < a.cols; e += W * 64 * V) {
+            const v4u g = load_row<ES>(dy, e, a.cols);
+            v4u z[kBatch];
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j)
+                if ((int32_t)r[j] >= 0 && a.grad_weight) z[j] = load_row<ES>((const char*)a.z + (uint64_t)r[j] * a.ldz * ES, e, a.cols);
+            float x[V];
+            widen<DT>(g, x);
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {
+                if ((int32_t)r[j] < 0) continue;
+                if (a.grad_z) {
+                    float d[V];
+#pragma unroll
+                    for (int i = 0; i < V; ++i) d[i] = wk[j] * x[i];
+                    store_row<ES>((char*)a.grad_z + (uint64_t)r[j] * a.ldo * ES, e, a.cols, narrow<DT>(d));
+                }
+                if (a.grad_weight) {
+                    float y[V];
+                    widen<DT>(z[j], y);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) dot[j] += x[i] * y[i];
+                }
+            }
+        }
+        if (!a.grad_weight) continue;
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) dot[j] = sum_lanes<64>(dot[j]);
+        if constexpr (W > 1) {
+            if (lane == 0) {
+#pragma unroll
+                for (int j = 0; j < kBatch; ++j) parts[w][j] = dot[j];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {
+                dot[j] = parts[0][j];
+#pragma unroll
+                for (int q = 1; q < W; ++q) dot[j] += parts[q][j];
+            }
+            __syncthreads();
+        }
+        if (threadIdx.x == 0) {
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j)
+                if (k + j < a.top_k) a.grad_weight[t * a.top_k + k + j] = (int32_t)r[j] < 0 ? 0.0f : dot[j];
+        }
+    }
+}
+
+// A launch's threads are counted in 32 bits.
+bool too_many(uint64_t blocks, uint32_t threads) { return blocks * threads > 0xffffffffull; }
+
+template <typename F>
+hipError_t by_type(hcclDataType_t dt, F f) {
+    if (dt == hcclBf16) f(std::integral_constant<int, hcclBf16>());
+    else if (dt == hcclFp16) f(std::integral_constant<int, hcclFp16>());
+    else f(std::integral_constant<int, hcclFp32>());
+    return hipGetLastError();
+}
+
+}  // namespace
+
+void plan_shape(uint64_t routes, uint32_t* blocks, uint32_t* steps) {
+    // One launch for up to 4 096 routes, then two with at most 128 blocks: a block of the second
+    // reads every block's counts.
+    const uint64_t n = (routes + kPlanThreads - 1) / kPlanThreads;
+    if (n <= 4) {
+        *blocks = 1;
+        *steps = (uint32_t)n;
+    } else {
+        *steps = (uint32_t)((n + 127) / 128);
+        *blocks = (uint32_t)((n + *steps - 1) / *steps);
+    }
+}
+
+hipError_t launch_plan(const PlanArgs& a, hipStream_t s) {
+    if (a.blocks > 1) hipLaunchKernelGGL(hccl_moe_count_kernel, dim3(a.blocks), dim3(kPlanThreads), 0, s, a);
+    hipLaunchKernelGGL(hccl_moe_plan_kernel, dim3(a.blocks), dim3(kPlanThreads), 0, s, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_dispatch(const DispatchArgs& a, hcclDataType_t dt, hipStream_t s) {
+    const uint32_t es = dt == hcclFp32 ? 4 : 2, per = kPieceVecs * kWave * 16 / es;
+    const uint32_t pieces = (uint32_t)((a.cols + per - 1) / per);
+    const uint64_t blocks = (a.tokens * pieces + kWaves - 1) / kWaves;
+    if (too_many(blocks, kThreads)) return hipErrorInvalidConfiguration;
+    const dim3 grid((uint32_t)blocks), block(kThreads);
+    if (es == 2) hipLaunchKernelGGL(hccl_moe_dispatch_kernel<2>, grid, block, 0, s, a, pieces);
+    else hipLaunchKernelGGL(hccl_moe_dispatch_kernel<4>, grid, block, 0, s, a, pieces);
+    return hipGetLastError();
+}
+
+hipError_t launch_quantize(const QuantizeArgs& a, hcclDataType_t dt, bool gated, hipStream_t s) {
+    if (too_many(a.rows, kThreads)) return hipErrorInvalidConfiguration;
+    return by_type(dt, [&](auto type) {
+        constexpr int DT = decltype(type)::value;
+        // a wave a row where that fills the chip and the row stays in its registers
+        const bool narrow_rows = a.cols <= kKeep * kWave * kVecOf<DT> && a.rows >= 2048;
+        const dim3 grid((uint32_t)(narrow_rows ? (a.rows + kWaves - 1) / kWaves : a.rows)), block(kThreads);
+        if (narrow_rows && gated) hipLaunchKernelGGL((hccl_moe_quantize_kernel<DT, true, 1>), grid, block, 0, s, a);
+        else if (narrow_rows) hipLaunchKernelGGL((hccl_moe_quantize_kernel<DT, false, 1>), grid, block, 0, s, a);
+        else if (gated) hipLaunchKernelGGL((hccl_moe_quantize_kernel<DT, true, kWaves>), grid, block, 0, s, a);
+        else hipLaunchKernelGGL((hccl_moe_quantize_kernel<DT, false, kWaves>), grid, block, 0, s, a);
+    });
+}
+
+hipError_t launch_combine(const CombineArgs& a, hcclDataType_t dt, hipStream_t s) {
+    const uint32_t per = kCombineVecs * kWave * (dt == hcclFp32 ? 4 : 8), pieces = (uint32_t)((a.cols + per - 1) / per);
+    const uint64_t blocks = (a.tokens * pieces + kWaves - 1) / kWaves;
+    if (too_many(blocks, kThreads)) return hipErrorInvalidConfiguration;
+    return by_type(dt, [&](auto type) {
+        constexpr int DT = decltype(type)::value;
+        const dim3 grid((uint32_t)blocks);
+        hipLaunchKernelGGL(hccl_moe_combine_kernel<DT>, grid, dim3(kThreads), 0, s, a, pieces);
+    });
+}
+
+hipError_t launch_combine_backward(const CombineBackwardArgs& a, hcclDataType_t dt, hipStream_t s) {
+    if (too_many(a.tokens, 256)) return hipErrorInvalidConfiguration;
+    return by_type(dt, [&](auto type) {
+        constexpr int DT = decltype(type)::value;
+        const dim3 grid((uint32_t)a.tokens);
+        if (a.cols <= kWave * kVecOf<DT>) hipLaunchKernelGGL((hccl_moe_combine_backward_kernel<DT, 1>), grid, dim3(64), 0, s, a);
+        else hipLaunchKernelGGL((hccl_moe_combine_backward_kernel<DT, 4>), grid, dim3(256), 0, s, a);
+    });
+}
+
+}  // namespace hccl

@@ -18,6 +18,7 @@ OPS = {"sum": 0, "max": 1, "min": 2}
 ALGOS = {"auto": 0, "direct": 1, "ring": 2, "two_level": 3, "rhd": 4}
 ORDERS = {"ascending": 0, "ring": 1, "halving": 2}
 PHASES = {"auto": 0, "one": 1, "levels": 2}
+SCORES = {"softmax": 0, "sigmoid": 1}
 RESULTS = {0: "hcclSuccess", 1: "hcclInvalidArgument", 2: "hcclUnsupported", 3: "hcclHipError",
            4: "hcclOutOfMemory", 5: "hcclTimeout", 6: "hcclInternalError"}
 NO_DEVICE = -1
@@ -31,6 +32,8 @@ EXPORTS = [
     "hccl_group_start", "hccl_group_end", "hccl_alltoallv_dynamic", "hccl_set_trigger",
     "hccl_resident_start", "hccl_resident_stop", "hccl_resident_wait", "hccl_resident_last_seq",
     "hccl_allreduce_noalloc", "hccl_comm_trace", "hccl_comm_program_image",
+    "hccl_router_init", "hccl_moe_route", "hccl_moe_route_backward", "hccl_moe_plan_bytes", "hccl_moe_plan",
+    "hccl_moe_dispatch", "hccl_moe_combine", "hccl_moe_combine_backward", "hccl_moe_quantize", "hccl_moe_product",
 ]
 CMPS = {"eq": 0, "ne": 1, "ge": 2, "gt": 3, "le": 4, "lt": 5}
 
@@ -55,6 +58,14 @@ class hcclTrigger_t(ctypes.Structure):
     _fields_ = [
         ("wait_addr", ctypes.c_void_p), ("wait_value", ctypes.c_uint64), ("wait_cmp", ctypes.c_int32),
         ("reserved", ctypes.c_int32), ("done_addr", ctypes.c_void_p), ("done_value", ctypes.c_uint64),
+    ]
+
+
+class hcclRouter_t(ctypes.Structure):
+    _fields_ = [
+        ("experts", ctypes.c_uint32), ("top_k", ctypes.c_uint32), ("score", ctypes.c_int32), ("groups", ctypes.c_uint32),
+        ("top_groups", ctypes.c_uint32), ("group_top", ctypes.c_uint32), ("renormalize", ctypes.c_int32),
+        ("scale", ctypes.c_float),
     ]
 
 
@@ -120,6 +131,17 @@ def load(path: str = LIB_PATH):
     lib.hccl_resident_stop.argtypes = [vp]
     lib.hccl_resident_wait.argtypes = [vp, ctypes.c_uint64, ctypes.c_uint32]
     lib.hccl_resident_last_seq.argtypes = [vp, ctypes.POINTER(ctypes.c_uint64)]
+    rp, u32 = ctypes.POINTER(hcclRouter_t), ctypes.c_uint32
+    lib.hccl_router_init.argtypes = [rp]
+    lib.hccl_moe_route.argtypes = [vp, rp, vp, sz, i32, sz, vp, vp, vp, vp, vp]
+    lib.hccl_moe_route_backward.argtypes = [vp, rp, vp, sz, i32, sz, vp, vp, vp, sz, vp]
+    lib.hccl_moe_plan_bytes.argtypes = [sz, u32, u32, szp]
+    lib.hccl_moe_plan.argtypes = [vp, vp, sz, u32, u32, sz, vp, vp, vp, vp, sz, vp]
+    lib.hccl_moe_dispatch.argtypes = [vp, vp, sz, i32, sz, sz, vp, u32, vp, sz, sz, vp, vp]
+    lib.hccl_moe_combine.argtypes = [vp, vp, sz, i32, sz, vp, u32, vp, sz, sz, vp, sz, vp]
+    lib.hccl_moe_combine_backward.argtypes = [vp, vp, sz, i32, sz, sz, vp, sz, sz, vp, u32, vp, vp, sz, vp, vp]
+    lib.hccl_moe_quantize.argtypes = [vp, vp, sz, i32, sz, sz, i32, vp, vp, sz, vp, vp]
+    lib.hccl_moe_product.argtypes = [vp, vp, sz, vp, sz, sz, vp, sz, vp, sz, sz, vp, sz, vp, sz, i32, vp]
     for name in EXPORTS:
         if name not in ("hccl_get_last_error", "hccl_result_string"):
             getattr(lib, name).restype = res
@@ -316,6 +338,191 @@ def hccl_resident_last_seq(comm) -> int:
     return int(out.value)
 
 
+def hccl_router_init(**kw) -> hcclRouter_t:
+    router = hcclRouter_t()
+    _check(load().hccl_router_init(ctypes.byref(router)))
+    for k, v in kw.items():
+        if k == "score" and isinstance(v, str):
+            v = SCORES[v]
+        setattr(router, k, float(v) if k == "scale" else int(v))
+    return router
+
+
+def hccl_moe_plan_bytes(tokens: int, top_k: int, experts: int) -> int:
+    """Bytes of the workspace that moe_plan needs for these sizes."""
+    out = ctypes.c_size_t(0)
+    _check(load().hccl_moe_plan_bytes(tokens, top_k, experts, ctypes.byref(out)))
+    return int(out.value)
+
+
+# The operators' C calls, as (function, arguments): the hccl_moe_* functions below make them at once, the
+# bind_moe_* methods of Comm as often as they are called. Arrays of rows are 2-D tensors whose rows may be
+# any distance apart; the others are packed. Sizes come from the tensors, which must agree.
+
+def _rows(t, rows, cols, what):
+    """Address and row stride of a tensor of `rows` rows of `cols` neighbouring elements."""
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+        raise ValueError(f"{what} must have shape ({rows}, {cols}), not {tuple(t.shape)}")
+    step, inner = t.stride()
+    if inner != 1 and cols > 1:
+        raise ValueError(f"the elements of a row of {what} must be neighbours")
+    return t.data_ptr(), (step if rows > 1 else cols)
+
+
+def _list(t, n, dtype, what):
+    """Address of a packed tensor of n elements of the named type (None stays None)."""
+    if t is None:
+        return None
+    if t.numel() != n or not t.is_contiguous() or str(t.dtype) != "torch." + dtype:
+        raise ValueError(f"{what} must be {n} packed {dtype} elements, not {tuple(t.shape)} {t.dtype}")
+    return t.data_ptr()
+
+
+def _same_type(t, like, what):
+    if t.dtype != like.dtype:
+        raise ValueError(f"{what} must be {like.dtype}, not {t.dtype}")
+
+
+def _codes(t, what):
+    if str(t.dtype) != "torch.int8":
+        raise ValueError(f"{what} must be int8, not {t.dtype}")
+
+
+def _call_moe_route(comm, router, logits, index, weight, bias=None, mask=None, stream=None):
+    T, E, K = logits.shape[0], router.experts, router.top_k
+    at, ld = _rows(logits, T, E, "logits")
+    return load().hccl_moe_route, (comm, ctypes.byref(router), at, ld, _dtype_code(logits.dtype), T, _list(bias, E, "float32", "bias"),
+                                   _list(mask, T, "uint8", "mask"), _list(index, T * K, "int32", "index"),
+                                   _list(weight, T * K, "float32", "weight"), _stream_handle(stream))
+
+
+def _call_moe_route_backward(comm, router, logits, index, grad_weight, grad_logits, stream=None):
+    T, E, K = logits.shape[0], router.experts, router.top_k
+    at, ld = _rows(logits, T, E, "logits")
+    out, ldg = _rows(grad_logits, T, E, "grad_logits")
+    _same_type(grad_logits, logits, "grad_logits")
+    return load().hccl_moe_route_backward, (comm, ctypes.byref(router), at, ld, _dtype_code(logits.dtype), T,
+                                            _list(index, T * K, "int32", "index"),
+                                            _list(grad_weight, T * K, "float32", "grad_weight"), out, ldg, _stream_handle(stream))
+
+
+def _call_moe_plan(comm, index, experts, row, offsets, capacity, rank_counts=None, workspace=None, stream=None):
+    T, K = index.shape
+    counts = None
+    if rank_counts is not None:
+        counts = _list(rank_counts, rank_counts.numel(), "int64", "rank_counts")
+    size = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    return load().hccl_moe_plan, (comm, _list(index, T * K, "int32", "index"), T, K, experts, capacity,
+                                  _list(row, T * K, "int32", "row"), _list(offsets, experts + 1, "int64", "offsets"), counts,
+                                  _addr_or_null(workspace), size, _stream_handle(stream))
+
+
+def _call_moe_dispatch(comm, x, row, out, scale=None, stream=None):
+    (T, C), R, K = x.shape, out.shape[0], row.shape[1]
+    at, ldx = _rows(x, T, C, "x")
+    to, ldo = _rows(out, R, C, "out")
+    _same_type(out, x, "out") if scale is None else _codes(out, "out")
+    return load().hccl_moe_dispatch, (comm, at, ldx, _dtype_code(x.dtype), T, C, _list(row, T * K, "int32", "row"), K, to, ldo, R,
+                                      _list(scale, R, "float32", "scale"), _stream_handle(stream))
+
+
+def _call_moe_combine(comm, z, row, out, weight=None, stream=None):
+    (T, C), R, K = out.shape, z.shape[0], row.shape[1]
+    at, ldz = _rows(z, R, C, "z")
+    to, ldo = _rows(out, T, C, "out")
+    _same_type(out, z, "out")
+    return load().hccl_moe_combine, (comm, at, ldz, _dtype_code(z.dtype), R, _list(row, T * K, "int32", "row"), K,
+                                     _list(weight, T * K, "float32", "weight"), T, C, to, ldo, _stream_handle(stream))
+
+
+def _call_moe_combine_backward(comm, grad, z, row, weight, grad_z=None, grad_weight=None, stream=None):
+    (T, C), R, K = grad.shape, z.shape[0], row.shape[1]
+    at, ldg = _rows(grad, T, C, "grad")
+    rows, ldz = _rows(z, R, C, "z")
+    to, ldgz = (None, 0) if grad_z is None else _rows(grad_z, R, C, "grad_z")
+    _same_type(z, grad, "z")
+    if grad_z is not None:
+        _same_type(grad_z, grad, "grad_z")
+    return load().hccl_moe_combine_backward, (comm, at, ldg, _dtype_code(grad.dtype), T, C, rows, ldz, R,
+                                              _list(row, T * K, "int32", "row"), K, _list(weight, T * K, "float32", "weight"), to, ldgz,
+                                              _list(grad_weight, T * K, "float32", "grad_weight"), _stream_handle(stream))
+
+
+def _call_moe_quantize(comm, x, codes, scale, gated=False, limit=None, stream=None):
+    R, C = codes.shape
+    at, ldx = _rows(x, R, 2 * C if gated else C, "x")
+    to, ldq = _rows(codes, R, C, "codes")
+    _codes(codes, "codes")
+    return load().hccl_moe_quantize, (comm, at, ldx, _dtype_code(x.dtype), R, C, int(bool(gated)), _list(limit, 1, "int64", "limit"), to, ldq,
+                                      _list(scale, R, "float32", "scale"), _stream_handle(stream))
+
+
+def _call_moe_product(comm, codes, scale, weights, weight_scale, out, offsets=None, stream=None):
+    (R, D), (E, N) = codes.shape, weights.shape[:2]
+    at, lda = _rows(codes, R, D, "codes")
+    # the experts' rows follow each other at one stride
+    ldb = weights.stride(1) if N > 1 else weights.stride(0) if E > 1 else D
+    if weights.dim() != 3 or weights.shape[2] != D or (D > 1 and weights.stride(2) != 1) or (E > 1 and weights.stride(0) != N * ldb):
+        raise ValueError(f"weights must be (experts, columns, {D}) with rows one distance apart, not {tuple(weights.shape)}")
+    to, ldo = _rows(out, R, N, "out")
+    _codes(codes, "codes")
+    _codes(weights, "weights")
+    S = 0 if offsets is None else offsets.numel() - 1
+    return load().hccl_moe_product, (comm, at, lda, _list(scale, R, "float32", "scale"), R, D, weights.data_ptr(), ldb,
+                                     _list(weight_scale, E * N, "float32", "weight_scale"), N, E,
+                                     None if offsets is None else _list(offsets, S + 1, "int64", "offsets"), S, to, ldo,
+                                     _dtype_code(out.dtype), _stream_handle(stream))
+
+
+def hccl_moe_route(*args, **kw) -> None:
+    """(comm, router, logits, index, weight, bias=None, mask=None, stream=None)"""
+    fn, a = _call_moe_route(*args, **kw)
+    _check(fn(*a))
+
+
+def hccl_moe_route_backward(*args, **kw) -> None:
+    """(comm, router, logits, index, grad_weight, grad_logits, stream=None)"""
+    fn, a = _call_moe_route_backward(*args, **kw)
+    _check(fn(*a))
+
+
+def hccl_moe_plan(*args, **kw) -> None:
+    """(comm, index, experts, row, offsets, capacity, rank_counts=None, workspace=None, stream=None)"""
+    fn, a = _call_moe_plan(*args, **kw)
+    _check(fn(*a))
+
+
+def hccl_moe_dispatch(*args, **kw) -> None:
+    """(comm, x, row, out, scale=None, stream=None): int8 rows with a scale"""
+    fn, a = _call_moe_dispatch(*args, **kw)
+    _check(fn(*a))
+
+
+def hccl_moe_combine(*args, **kw) -> None:
+    """(comm, z, row, out, weight=None, stream=None)"""
+    fn, a = _call_moe_combine(*args, **kw)
+    _check(fn(*a))
+
+
+def hccl_moe_combine_backward(*args, **kw) -> None:
+    """(comm, grad, z, row, weight, grad_z=None, grad_weight=None, stream=None)"""
+    fn, a = _call_moe_combine_backward(*args, **kw)
+    _check(fn(*a))
+
+
+def hccl_moe_quantize(*args, **kw) -> None:
+    """(comm, x, codes, scale, gated=False, limit=None, stream=None)"""
+    fn, a = _call_moe_quantize(*args, **kw)
+    _check(fn(*a))
+
+
+def hccl_moe_product(*args, **kw) -> None:
+    """(comm, codes, scale, weights, weight_scale, out, offsets=None, stream=None): codes (rows, inner),
+    weights (experts, columns, inner)"""
+    fn, a = _call_moe_product(*args, **kw)
+    _check(fn(*a))
+
+
 def hccl_comm_last_program(comm) -> dict:
     info = hcclProgramInfo_t()
     _check(load().hccl_comm_last_program(comm, ctypes.byref(info)))
@@ -353,6 +560,16 @@ def _bound(fn, *args):
     def call():
         _check(fn(*args))
 
+    return call
+
+
+def _bound_operator(comm, made, *keep):
+    fn, args = made
+
+    def call():
+        _check(fn(*args))
+
+    call.keep = (comm, keep)
     return call
 
 
@@ -443,6 +660,70 @@ class Comm:
                       _addr_or_null(sdispls), _ptr_array(recv), _addr_or_null(recvcounts), _addr_or_null(rdispls),
                       row_elems, self._capacity(send, row_elems), self._capacity(recv, row_elems),
                       _dtype_code(send[0].dtype), _stream_handle(stream))
+
+    # Mixture-of-experts operators: one rank's tensors, no list of them (see include/hccl.h). The bind_*
+    # forms keep their tensors alive and the stream that is current when they are made.
+    def moe_route(self, router, logits, index, weight, bias=None, mask=None, stream=None):
+        hccl_moe_route(self.handle, router, logits, index, weight, bias, mask, stream)
+
+    def bind_moe_route(self, router, logits, index, weight, bias=None, mask=None, stream=None):
+        return _bound_operator(self, _call_moe_route(self.handle, router, logits, index, weight, bias, mask, stream),
+                               router, logits, index, weight, bias, mask)
+
+    def moe_route_backward(self, router, logits, index, grad_weight, grad_logits, stream=None):
+        hccl_moe_route_backward(self.handle, router, logits, index, grad_weight, grad_logits, stream)
+
+    def bind_moe_route_backward(self, router, logits, index, grad_weight, grad_logits, stream=None):
+        return _bound_operator(self, _call_moe_route_backward(self.handle, router, logits, index, grad_weight, grad_logits, stream),
+                               router, logits, index, grad_weight, grad_logits)
+
+    def moe_plan(self, index, experts, row, offsets, capacity, rank_counts=None, workspace=None, stream=None):
+        hccl_moe_plan(self.handle, index, experts, row, offsets, capacity, self._rank_counts(rank_counts), workspace, stream)
+
+    def bind_moe_plan(self, index, experts, row, offsets, capacity, rank_counts=None, workspace=None, stream=None):
+        return _bound_operator(self, _call_moe_plan(self.handle, index, experts, row, offsets, capacity, self._rank_counts(rank_counts),
+                                                 workspace, stream),
+                               index, row, offsets, rank_counts, workspace)
+
+    def _rank_counts(self, rank_counts):
+        if rank_counts is not None and rank_counts.numel() != self.nranks:
+            raise ValueError(f"rank_counts must be {self.nranks} packed int64 elements")
+        return rank_counts
+
+    def moe_dispatch(self, x, row, out, scale=None, stream=None):
+        hccl_moe_dispatch(self.handle, x, row, out, scale, stream)
+
+    def bind_moe_dispatch(self, x, row, out, scale=None, stream=None):
+        return _bound_operator(self, _call_moe_dispatch(self.handle, x, row, out, scale, stream),
+                               x, row, out, scale)
+
+    def moe_combine(self, z, row, out, weight=None, stream=None):
+        hccl_moe_combine(self.handle, z, row, out, weight, stream)
+
+    def bind_moe_combine(self, z, row, out, weight=None, stream=None):
+        return _bound_operator(self, _call_moe_combine(self.handle, z, row, out, weight, stream),
+                               z, row, out, weight)
+
+    def moe_combine_backward(self, grad, z, row, weight, grad_z=None, grad_weight=None, stream=None):
+        hccl_moe_combine_backward(self.handle, grad, z, row, weight, grad_z, grad_weight, stream)
+
+    def bind_moe_combine_backward(self, grad, z, row, weight, grad_z=None, grad_weight=None, stream=None):
+        return _bound_operator(self, _call_moe_combine_backward(self.handle, grad, z, row, weight, grad_z, grad_weight, stream),
+                               grad, z, row, weight, grad_z, grad_weight)
+
+    def moe_quantize(self, x, codes, scale, gated=False, limit=None, stream=None):
+        hccl_moe_quantize(self.handle, x, codes, scale, gated, limit, stream)
+
+    def bind_moe_quantize(self, x, codes, scale, gated=False, limit=None, stream=None):
+        return _bound_operator(self, _call_moe_quantize(self.handle, x, codes, scale, gated, limit, stream),
+                               x, codes, scale, limit)
+
+    def moe_product(self, codes, scale, weights, weight_scale, out, offsets=None, stream=None):
+        hccl_moe_product(self.handle, codes, scale, weights, weight_scale, out, offsets, stream)
+
+    def bind_moe_product(self, codes, scale, weights, weight_scale, out, offsets=None, stream=None):
+        return _bound_operator(self, _call_moe_product(self.handle, codes, scale, weights, weight_scale, out, offsets, stream),
+                               codes, scale, weights, weight_scale, out, offsets)
 
     def triggered(self, wait=None, done=None):
         """Context manager: the next work packet called inside waits for ``wait`` =
