@@ -12,6 +12,7 @@ namespace hccl {
 namespace {
 
 typedef int32_t v4i __attribute__((ext_vector_type(4)));
+typedef int32_t v16i __attribute__((ext_vector_type(16)));
 
 // Rows [first, end) of tile `tile` of BM rows, and its expert; false where there are fewer tiles.
 // One lane a segment: tiles of a segment, their running sum, and the segment that holds the tile.
@@ -19,6 +20,13 @@ struct Rows {
     uint64_t first, end;
     uint32_t expert;
 };
+// (offsets outside 0 .. rows are clipped, and a segment that ends before it begins is empty)
+__device__ __forceinline__ void segment(const ProductArgs& a, uint32_t s, uint64_t& first, uint64_t& end) {
+    const int64_t lo = a.offsets[s], hi = a.offsets[s + 1];
+    first = lo < 0 ? 0 : (uint64_t)lo < a.rows ? (uint64_t)lo : a.rows;
+    end = hi < (int64_t)first ? first : (uint64_t)hi < a.rows ? (uint64_t)hi : a.rows;
+}
+
 template <uint32_t BM>
 __device__ __forceinline__ bool find_rows(const ProductArgs& a, uint32_t tile, Rows& out) {
     if (!a.offsets) {
@@ -32,11 +40,7 @@ __device__ __forceinline__ bool find_rows(const ProductArgs& a, uint32_t tile, R
     for (uint32_t s0 = 0; s0 < a.segments; s0 += kWave) {
         const uint32_t s = s0 + lane;
         uint64_t first = 0, end = 0;
-        if (s < a.segments) {
-            const int64_t lo = a.offsets[s], hi = a.offsets[s + 1];
-            first = lo < 0 ? 0 : (uint64_t)lo < a.rows ? (uint64_t)lo : a.rows;
-            end = hi < (int64_t)first ? first : (uint64_t)hi < a.rows ? (uint64_t)hi : a.rows;
-        }
+        if (s < a.segments) segment(a, s, first, end);
         const uint32_t n = (uint32_t)((end - first + BM - 1) / BM);
         uint32_t incl = n;
 #pragma unroll
@@ -58,14 +62,41 @@ __device__ __forceinline__ bool find_rows(const ProductArgs& a, uint32_t tile, R
     return false;
 }
 
-// 16 bytes of a row at k; bytes from `inner` on are zero.
+// Tiles that the segments have.
+template <uint32_t BM>
+__device__ __forceinline__ uint32_t count_tiles(const ProductArgs& a) {
+    if (!a.offsets) return (uint32_t)((a.rows + BM - 1) / BM);
+    const uint32_t lane = threadIdx.x & 63;
+    uint32_t n = 0;
+    for (uint32_t s = lane; s < a.segments; s += kWave) {
+        uint64_t first, end;
+        segment(a, s, first, end);
+        n += (uint32_t)((end - first + BM - 1) / BM);
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) n += (uint32_t)__shfl_xor((int)n, d);
+    return first_lane(n);
+}
+
+// 16 bytes of a row at k; bytes from `inner` on are zero: the row's last 16 bytes, shifted down.
 __device__ __forceinline__ v4i load_k(const int8_t* row, uint32_t k, uint32_t inner) {
     if (k + 16 <= inner) return (v4i)load16<1>(row + k);
     v4i r = {0, 0, 0, 0};
-    if (k < inner) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-            if (k + i < inner) r[i / 4] |= (int32_t)((uint32_t)(uint8_t)*gptr<int8_t>(row + k + i) << (8 * (i & 3)));
+    if (k >= inner) return r;
+    if (inner >= 16) {
+        const v4u t = load16<1>(row + inner - 16);
+        uint64_t lo = (uint64_t)t[1] << 32 | t[0], hi = (uint64_t)t[3] << 32 | t[2];
+        const uint32_t bits = 8 * (k + 16 - inner);  // 8 .. 120
+        lo = bits < 64 ? lo >> bits | hi << (64 - bits) : hi >> (bits - 64);
+        hi = bits < 64 ? hi >> bits : 0;
+        return v4i{(int32_t)lo, (int32_t)(lo >> 32), (int32_t)hi, (int32_t)(hi >> 32)};
+    }
+    for (uint32_t i = 0; k + i < inner; ++i) {  // (a row of fewer than 16 bytes; k is 0)
+        const uint32_t v = (uint32_t)(uint8_t)*gptr<int8_t>(row + k + i) << (8 * (i & 3));
+        r[0] |= i / 4 == 0 ? v : 0;
+        r[1] |= i / 4 == 1 ? v : 0;
+        r[2] |= i / 4 == 2 ? v : 0;
+        r[3] |= i / 4 == 3 ? v : 0;
     }
     return r;
 }
@@ -154,8 +185,145 @@ __global__ __launch_bounds__(W * 64) void hccl_moe_product_few_kernel(ProductArg
     }
 }
 
+// Many rows a segment: BM rows by BN columns a block, in WM x WN waves, k in steps of 128 through two
+// LDS buffers: while one is multiplied the next is filled, by loads that go to LDS directly
+// (DIRECT: both operands' rows are 16-byte aligned) or through registers (any alignment, and the
+// last step of an inner size that is no multiple of 128, where bytes past the end are zero).
+//
+// LDS holds a row's 128 bytes as 8 chunks of 16; chunk c of row r lies in slot c ^ (r & 7), so that the
+// lanes that read one chunk of neighbouring rows use different banks. A direct load writes its 64
+// lanes one after the other, so a lane reads the chunk that belongs in its slot.
+constexpr uint32_t kStep = 128;
+
+typedef __attribute__((address_space(3))) void* lds_ptr;
+
+template <int DT, int BM, int BN, int WM, int WN, bool DIRECT>
+__global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_many_kernel(ProductArgs a, uint32_t nblocks) {
+    constexpr int W = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
+    constexpr int LA = BM / 8 / W, LB = BN / 8 / W;  // loads a wave has to make for a step: 8 rows each
+    static_assert(BM % (8 * W) == 0 && BN % (8 * W) == 0, "whole loads");
+    __shared__ __attribute__((aligned(128))) char lds[2 * (BM + BN) * kStep];
+    const uint32_t lane = threadIdx.x & 63, w = first_lane(threadIdx.x >> 6);
+
+    // Blocks go to the XCDs in turn; each XCD gets neighbouring tiles, in bands of 8 column blocks, so
+    // that the tiles it works on at a time share their rows and weights in its L2.
+    uint32_t tile, nb;
+    {
+        const uint32_t tiles = count_tiles<BM>(a);
+        const uint64_t all = (uint64_t)tiles * nblocks, share = (all + 7) / 8;
+        const uint64_t id = (blockIdx.x & 7) * share + blockIdx.x / 8;
+        if (blockIdx.x / 8 >= share || id >= all) return;
+        const uint64_t banded = (uint64_t)(nblocks / 8 * 8) * tiles;
+        const uint32_t width = id < banded ? 8 : nblocks % 8;
+        const uint64_t at = id < banded ? id % (8ull * tiles) : id - banded;
+        tile = (uint32_t)(at / width);
+        nb = (id < banded ? (uint32_t)(id / (8ull * tiles)) * 8 : nblocks / 8 * 8) + (uint32_t)(at % width);
+    }
+    Rows rows;
+    if (!find_rows<BM>(a, tile, rows)) return;
+    const uint32_t n0 = nb * BN;
+
+    // where this lane's part of each load comes from
+    const uint32_t lrow = lane >> 3, chunk = (lane & 7) ^ lrow;
+    const int8_t* src[LA + LB];
+#pragma unroll
+    for (int i = 0; i < LA; ++i) {
+        const uint64_t m = rows.first + (w * LA + i) * 8 + lrow;
+        src[i] = a.a + (m < rows.end ? m : rows.end - 1) * a.lda;
+    }
+#pragma unroll
+    for (int i = 0; i < LB; ++i) {
+        const uint32_t n = n0 + (w * LB + i) * 8 + lrow;
+        src[LA + i] = a.b + ((uint64_t)rows.expert * a.cols + (n < a.cols ? n : a.cols - 1)) * a.ldb;
+    }
+    auto buffer = [&](uint32_t s) { return lds + (s & 1) * ((BM + BN) * kStep); };
+    auto slot = [&](uint32_t s, int i) { return buffer(s) + (i < LA ? (w * LA + i) * 8 : BM + (w * LB + i - LA) * 8) * kStep; };
+
+    v16i acc[TN][TM];
+#pragma unroll
+    for (int y = 0; y < TN; ++y)
+#pragma unroll
+        for (int x = 0; x < TM; ++x)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[y][x][r] = 0;
+
+    const uint32_t steps = (a.inner + kStep - 1) / kStep, whole = a.inner / kStep;
+    const uint32_t wm = w % WM, wn = w / WM;
+    v4u held[DIRECT ? 1 : LA + LB];
+    auto fetch = [&](uint32_t s) {  // begins to fill buffer s
+        if (DIRECT && s < whole) {
+#pragma unroll
+            for (int i = 0; i < LA + LB; ++i)
+                __builtin_amdgcn_global_load_lds((const HCCL_AS1 void*)(src[i] + (uint64_t)s * kStep + chunk * 16), (lds_ptr)slot(s, i), 16, 0, 0);
+        } else if constexpr (!DIRECT) {
+#pragma unroll
+            for (int i = 0; i < LA + LB; ++i) held[i] = (v4u)load_k(src[i], s * kStep + chunk * 16, a.inner);
+        } else {
+#pragma unroll
+            for (int i = 0; i < LA + LB; ++i) *(v4u*)(slot(s, i) + lane * 16) = (v4u)load_k(src[i], s * kStep + chunk * 16, a.inner);
+        }
+    };
+    auto land = [&](uint32_t s) {  // what was fetched for buffer s is there
+        if constexpr (!DIRECT) {
+#pragma unroll
+            for (int i = 0; i < LA + LB; ++i) *(v4u*)(slot(s, i) + lane * 16) = held[i];
+        }
+        __builtin_amdgcn_s_waitcnt(0);
+        __syncthreads();
+    };
+    if (steps) fetch(0);
+    for (uint32_t s = 0; s < steps; ++s) {
+        land(s);
+        if (s + 1 < steps) fetch(s + 1);
+        const char* pa = buffer(s) + (wm * TM * 32 + (lane & 31)) * kStep;
+        const char* pb = buffer(s) + (BM + wn * TN * 32 + (lane & 31)) * kStep;
+#pragma unroll
+        for (uint32_t kk = 0; kk < 4; ++kk) {
+            const uint32_t at = ((kk * 2 + (lane >> 5)) ^ (lane & 7)) * 16;
+            v4i va[TM], vb[TN];
+#pragma unroll
+            for (int y = 0; y < TN; ++y) vb[y] = *(const v4i*)(pb + y * 32 * kStep + at);
+#pragma unroll
+            for (int x = 0; x < TM; ++x) va[x] = *(const v4i*)(pa + x * 32 * kStep + at);
+#pragma unroll
+            for (int y = 0; y < TN; ++y)
+#pragma unroll
+                for (int x = 0; x < TM; ++x) acc[y][x] = __builtin_amdgcn_mfma_i32_32x32x32_i8(vb[y], va[x], acc[y][x], 0, 0, 0);
+        }
+    }
+    const float* bs = a.b_scale + (uint64_t)rows.expert * a.cols;
+#pragma unroll
+    for (int x = 0; x < TM; ++x) {
+        const uint64_t m = rows.first + (wm * TM + x) * 32 + (lane & 31);
+        if (m >= rows.end) continue;
+        const float as = a.a_scale[m];
+#pragma unroll
+        for (int y = 0; y < TN; ++y)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const uint32_t n = n0 + (wn * TN + y) * 32 + g * 8 + (lane >> 5) * 4;
+                if (n < a.cols) store_four<DT>(a, m, n, v4i{acc[y][x][4 * g], acc[y][x][4 * g + 1], acc[y][x][4 * g + 2], acc[y][x][4 * g + 3]}, as, bs);
+            }
+    }
+}
+
+template <int DT, int BM, int BN, int WM, int WN>
+hipError_t launch_many(const ProductArgs& a, hipStream_t s) {
+    const uint32_t nblocks = (a.cols + BN - 1) / BN, threads = WM * WN * 64;
+    const uint64_t blocks = ((a.rows + BM - 1) / BM + (a.offsets ? a.segments : 0)) * nblocks;
+    if (blocks + 8 > 0xffffffffull / threads) return hipErrorInvalidConfiguration;
+    const dim3 grid((uint32_t)((blocks + 7) / 8 * 8));
+    const bool direct = ((uintptr_t)a.a | (uintptr_t)a.b | a.lda | a.ldb) % 16 == 0;
+    if (direct) hipLaunchKernelGGL((hccl_moe_product_many_kernel<DT, BM, BN, WM, WN, true>), grid, dim3(threads), 0, s, a, nblocks);
+    else hipLaunchKernelGGL((hccl_moe_product_many_kernel<DT, BM, BN, WM, WN, false>), grid, dim3(threads), 0, s, a, nblocks);
+    return hipGetLastError();
+}
+
 template <int DT>
 hipError_t product_type(const ProductArgs& a, int cus, hipStream_t s) {
+    const uint64_t each = a.rows / a.segments;
+    if (each >= 512) return launch_many<DT, 256, 256, 2, 4>(a, s);
+    if (each >= 64) return launch_many<DT, 128, 128, 2, 2>(a, s);
     const uint32_t nblocks = (a.cols + 63) / 64;
     const uint64_t tiles = (a.rows + 15) / 16 + (a.offsets ? a.segments : 0);
     if (tiles * nblocks > 0xffffffffull / 256) return hipErrorInvalidConfiguration;

@@ -72,7 +72,7 @@ def close(got, want, bound, what=""):
 def rounded(got, want, bound, what=""):
     """A value within `bound` of `want` (and the rounding to 32 bits that it has anyway), rounded to got's type."""
     want = torch.from_numpy(np.ascontiguousarray(want))
-    bound = torch.from_numpy(np.ascontiguousarray(np.broadcast_to(bound, want.shape))) + F32 * want.abs() + 1e-37
+    bound = torch.from_numpy(np.broadcast_to(bound, want.shape).copy()) + F32 * want.abs() + 1e-37
     lo, hi = ((want + s * bound).float().to(got.dtype).double().numpy() for s in (-1, 1))
     v, w = host(got), want.numpy()
     bad = ~((lo <= v) & (v <= hi)) & ~(np.isnan(v) & np.isnan(w))
