@@ -129,29 +129,50 @@ __global__ __launch_bounds__(kPlanThreads) void hccl_moe_plan_kernel(PlanArgs a)
 }
 
 // -------------------------------------------------------------------------------------- dispatch
-// A wave copies a piece of a token's row to every row that the token has: it is read once. Pieces of
-// kPieceVecs vectors per lane keep loads in flight and give few tokens enough waves.
-constexpr uint32_t kPieceVecs = 4;
+// Vectors of rows. WHOLE: every lane's vector lies inside the row, so that none looks where it ends.
+// STREAM: with the non-temporal hint, for calls that move more than the last-level cache holds. That
+// keeps their results from pushing out what the call still reads: dispatch of 8 192 x 4 096 bf16 to 4
+// rows each 67 -> 53 us, gradients of the combination of 8 192 x 4 rows of 2 048 60 -> 52 us. It costs
+// a consumer that reads the rows at once (dispatch and quantisation 151 -> 158 us), and in calls that
+// the cache holds it costs more than it gives (2 048 x 4 096 to 4 rows each, and quantised, 40 -> 45 us).
+constexpr uint64_t kLastLevelCache = 256ull << 20;
 
-template <int ES>
-__global__ __launch_bounds__(kThreads) void hccl_moe_dispatch_kernel(DispatchArgs a, uint32_t pieces) {
-    constexpr uint64_t V = 16 / ES;
-    const uint32_t lane = threadIdx.x & 63;
-    const uint64_t id = (uint64_t)blockIdx.x * kWaves + first_lane(threadIdx.x >> 6);
-    const uint64_t t = id / pieces, c0 = (id % pieces) * (kPieceVecs * kWave * V);
-    if (t >= a.tokens) return;
-    const uint32_t mine = lane < a.top_k ? (uint32_t)a.row[t * a.top_k + lane] : ~0u;
-    const char* src = (const char*)a.x + t * a.ldx * ES;
-    v4u v[kPieceVecs];
-#pragma unroll
-    for (uint32_t u = 0; u < kPieceVecs; ++u) v[u] = load_row<ES>(src, c0 + (u * kWave + lane) * V, a.cols);
+template <int ES, bool WHOLE, bool STREAM>
+__device__ __forceinline__ v4u piece_load(const char* row, uint64_t e, uint64_t cols) {
+    if constexpr (WHOLE && STREAM) return (v4u)__builtin_nontemporal_load(gptr<typename Loose<ES>::x4>(row + e * ES));
+    else if constexpr (WHOLE) return load16<ES>(row + e * ES);
+    else return load_row<ES>(row, e, cols);
+}
+template <int ES, bool WHOLE, bool STREAM>
+__device__ __forceinline__ void piece_store(char* row, uint64_t e, uint64_t cols, const v4u& v) {
+    if constexpr (WHOLE && STREAM) __builtin_nontemporal_store((typename Loose<ES>::x4)v, gptr<typename Loose<ES>::x4>(row + e * ES));
+    else if constexpr (WHOLE) store16<ES>(row + e * ES, v);
+    else store_row<ES>(row, e, cols, v);
+}
+
+// A wave copies 1 KiB of a token's row to every row that the token has: it is read once, and few
+// tokens still make many waves. Rows that begin at any alignment are read and written as they lie:
+// stores brought to 16 bytes, which read the token again at another shift for every row, took 60 us
+// against 43 (16 384 x 1 001 bf16 to 4 rows each).
+template <int ES, bool WHOLE, bool STREAM>
+__device__ __forceinline__ void dispatch_piece(const DispatchArgs& a, uint64_t t, uint64_t e, uint32_t mine) {
+    const v4u v = piece_load<ES, WHOLE, false>((const char*)a.x + t * a.ldx * ES, e, a.cols);
     for (uint32_t k = 0; k < a.top_k; ++k) {
         const uint32_t r = at_lane(mine, k);
-        if (r >= a.capacity || (int32_t)r < 0) continue;
-        char* dst = (char*)a.out + (uint64_t)r * a.ldo * ES;
-#pragma unroll
-        for (uint32_t u = 0; u < kPieceVecs; ++u) store_row<ES>(dst, c0 + (u * kWave + lane) * V, a.cols, v[u]);
+        if (r < a.capacity) piece_store<ES, WHOLE, STREAM>((char*)a.out + (uint64_t)r * a.ldo * ES, e, a.cols, v);
     }
+}
+
+template <int ES, bool STREAM>
+__global__ __launch_bounds__(kThreads) void hccl_moe_dispatch_kernel(DispatchArgs a, uint32_t pieces) {
+    constexpr uint64_t V = 16 / ES, kPiece = kWave * V;
+    const uint32_t lane = threadIdx.x & 63;
+    const uint64_t id = (uint64_t)blockIdx.x * kWaves + first_lane(threadIdx.x >> 6);
+    const uint64_t t = id / pieces, c0 = (id % pieces) * kPiece;
+    if (t >= a.tokens) return;
+    const uint32_t mine = lane < a.top_k ? (uint32_t)a.row[t * a.top_k + lane] : ~0u;
+    if (c0 + kPiece <= a.cols) dispatch_piece<ES, true, STREAM>(a, t, c0 + lane * V, mine);
+    else dispatch_piece<ES, false, STREAM>(a, t, c0 + lane * V, mine);
 }
 
 // -------------------------------------------------------------------------------------- quantize
@@ -283,15 +304,10 @@ __global__ __launch_bounds__(kThreads) void hccl_moe_quantize_kernel(QuantizeArg
 constexpr int kBatch = 4;
 constexpr int kCombineVecs = 2;
 
-template <int DT>
-__global__ __launch_bounds__(kThreads) void hccl_moe_combine_kernel(CombineArgs a, uint32_t pieces) {
+template <int DT, bool WHOLE>
+__device__ __forceinline__ void combine_piece(const CombineArgs& a, uint64_t t, uint64_t c0, uint32_t lane) {
     constexpr int V = kVecOf<DT>, ES = kSize<DT>;
-    const uint32_t lane = threadIdx.x & 63;
-    const uint64_t id = (uint64_t)blockIdx.x * kWaves + first_lane(threadIdx.x >> 6);
-    const uint64_t t = id / pieces, c0 = (id % pieces) * (kCombineVecs * kWave * V);
-    if (t >= a.tokens) return;
-    uint32_t mine = lane < a.top_k ? (uint32_t)a.row[t * a.top_k + lane] : ~0u;
-    if (mine >= a.capacity) mine = ~0u;
+    const uint32_t mine = lane < a.top_k ? (uint32_t)a.row[t * a.top_k + lane] : ~0u;
     const float weight = a.weight && lane < a.top_k ? a.weight[t * a.top_k + lane] : 1.0f;
     float acc[kCombineVecs][V];
 #pragma unroll
@@ -302,16 +318,15 @@ __global__ __launch_bounds__(kThreads) void hccl_moe_combine_kernel(CombineArgs 
         v4u z[kBatch][kCombineVecs];
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) {
-            const uint32_t r = k + j < a.top_k ? at_lane(mine, k + j) : ~0u;
-            if ((int32_t)r < 0) continue;
+            const uint32_t r = at_lane(mine, k + j);  // (lanes from top_k on have no row)
+            if (r >= a.capacity) continue;
             const char* src = (const char*)a.z + (uint64_t)r * a.ldz * ES;
 #pragma unroll
-            for (int u = 0; u < kCombineVecs; ++u) z[j][u] = load_row<ES>(src, c0 + (u * kWave + lane) * V, a.cols);
+            for (int u = 0; u < kCombineVecs; ++u) z[j][u] = piece_load<ES, WHOLE, false>(src, c0 + (u * kWave + lane) * V, a.cols);
         }
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) {
-            const uint32_t r = k + j < a.top_k ? at_lane(mine, k + j) : ~0u;
-            if ((int32_t)r < 0) continue;
+            if (at_lane(mine, k + j) >= a.capacity) continue;
             const float w = __uint_as_float(at_lane(__float_as_uint(weight), k + j));
 #pragma unroll
             for (int u = 0; u < kCombineVecs; ++u) {
@@ -324,19 +339,65 @@ __global__ __launch_bounds__(kThreads) void hccl_moe_combine_kernel(CombineArgs 
     }
     char* dst = (char*)a.out + t * a.ldo * ES;
 #pragma unroll
-    for (int u = 0; u < kCombineVecs; ++u) store_row<ES>(dst, c0 + (u * kWave + lane) * V, a.cols, narrow<DT>(acc[u]));
+    for (int u = 0; u < kCombineVecs; ++u) piece_store<ES, WHOLE, false>(dst, c0 + (u * kWave + lane) * V, a.cols, narrow<DT>(acc[u]));
 }
 
-// dz_{row k} = w_k dy_t, dw_k = <dy_t, z_{row k}>. A block of W waves takes a token: the products are
-// added up in a lane, over the lanes and then over the waves, always in the same order.
-template <int DT, int W>
-__global__ __launch_bounds__(W * 64) void hccl_moe_combine_backward_kernel(CombineBackwardArgs a) {
+template <int DT>
+__global__ __launch_bounds__(kThreads) void hccl_moe_combine_kernel(CombineArgs a, uint32_t pieces) {
+    constexpr uint64_t kPiece = kCombineVecs * kWave * kVecOf<DT>;
+    const uint32_t lane = threadIdx.x & 63;
+    const uint64_t id = (uint64_t)blockIdx.x * kWaves + first_lane(threadIdx.x >> 6);
+    const uint64_t t = id / pieces, c0 = (id % pieces) * kPiece;
+    if (t >= a.tokens) return;
+    if (c0 + kPiece <= a.cols) combine_piece<DT, true>(a, t, c0, lane);
+    else combine_piece<DT, false>(a, t, c0, lane);
+}
+
+// dz_{row k} = w_k dy_t, dw_k = <dy_t, z_{row k}>. A block of W waves takes a token, as many as its row
+// has vectors for, up to 4 (3 001 tokens x 2 rows of 1 003 fp16: 2 waves 9 us, 4 waves 12 us). The
+// products are added up in a lane, over the lanes and then over the waves, always in the same order.
+template <int DT, bool WHOLE, bool STREAM>
+__device__ __forceinline__ void backward_piece(const CombineBackwardArgs& a, const char* dy, const uint32_t (&r)[kBatch], const float (&wk)[kBatch],
+                                               uint64_t e, float (&dot)[kBatch]) {
     constexpr int V = kVecOf<DT>, ES = kSize<DT>;
+    const v4u g = piece_load<ES, WHOLE, false>(dy, e, a.cols);
+    v4u z[kBatch];
+    if (a.grad_weight) {
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+            if (r[j] < a.capacity) z[j] = piece_load<ES, WHOLE, STREAM>((const char*)a.z + (uint64_t)r[j] * a.ldz * ES, e, a.cols);
+    }
+    float x[V];
+    widen<DT>(g, x);
+    if (a.grad_z) {
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            if (r[j] >= a.capacity) continue;
+            float d[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) d[i] = wk[j] * x[i];
+            piece_store<ES, WHOLE, STREAM>((char*)a.grad_z + (uint64_t)r[j] * a.ldo * ES, e, a.cols, narrow<DT>(d));
+        }
+    }
+    if (a.grad_weight) {
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            if (r[j] >= a.capacity) continue;
+            float y[V];
+            widen<DT>(z[j], y);
+#pragma unroll
+            for (int i = 0; i < V; ++i) dot[j] += x[i] * y[i];
+        }
+    }
+}
+
+template <int DT, int W, bool STREAM>
+__global__ __launch_bounds__(W * 64) void hccl_moe_combine_backward_kernel(CombineBackwardArgs a) {
+    constexpr uint64_t V = kVecOf<DT>, ES = kSize<DT>;
     __shared__ float parts[W][kBatch];
     const uint32_t lane = threadIdx.x & 63, w = first_lane(threadIdx.x >> 6);
     const uint64_t t = blockIdx.x;
-    uint32_t mine = lane < a.top_k ? (uint32_t)a.row[t * a.top_k + lane] : ~0u;
-    if (mine >= a.capacity) mine = ~0u;
+    const uint32_t mine = lane < a.top_k ? (uint32_t)a.row[t * a.top_k + lane] : ~0u;
     const float weight = lane < a.top_k ? a.weight[t * a.top_k + lane] : 0.0f;
     const char* dy = (const char*)a.grad + t * a.ldg * ES;
     for (uint32_t k = 0; k < a.top_k; k += kBatch) {
@@ -344,34 +405,13 @@ __global__ __launch_bounds__(W * 64) void hccl_moe_combine_backward_kernel(Combi
         float wk[kBatch], dot[kBatch];
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) {
-            r[j] = k + j < a.top_k ? at_lane(mine, k + j) : ~0u;
+            r[j] = at_lane(mine, k + j);  // (lanes from top_k on have no row)
             wk[j] = __uint_as_float(at_lane(__float_as_uint(weight), k + j));
             dot[j] = 0.0f;
         }
-        for (uint64_t e = threadIdx.x * V; e < a.cols; e += W * 64 * V) {
-            const v4u g = load_row<ES>(dy, e, a.cols);
-            v4u z[kBatch];
-#pragma unroll
-            for (int j = 0; j < kBatch; ++j)
-                if ((int32_t)r[j] >= 0 && a.grad_weight) z[j] = load_row<ES>((const char*)a.z + (uint64_t)r[j] * a.ldz * ES, e, a.cols);
-            float x[V];
-            widen<DT>(g, x);
-#pragma unroll
-            for (int j = 0; j < kBatch; ++j) {
-                if ((int32_t)r[j] < 0) continue;
-                if (a.grad_z) {
-                    float d[V];
-#pragma unroll
-                    for (int i = 0; i < V; ++i) d[i] = wk[j] * x[i];
-                    store_row<ES>((char*)a.grad_z + (uint64_t)r[j] * a.ldo * ES, e, a.cols, narrow<DT>(d));
-                }
-                if (a.grad_weight) {
-                    float y[V];
-                    widen<DT>(z[j], y);
-#pragma unroll
-                    for (int i = 0; i < V; ++i) dot[j] += x[i] * y[i];
-                }
-            }
+        for (uint64_t e = w * kWave * V; e < a.cols; e += W * kWave * V) {
+            if (e + kWave * V <= a.cols) backward_piece<DT, true, STREAM>(a, dy, r, wk, e + lane * V, dot);
+            else backward_piece<DT, false, STREAM>(a, dy, r, wk, e + lane * V, dot);
         }
         if (!a.grad_weight) continue;
 #pragma unroll
@@ -393,7 +433,7 @@ __global__ __launch_bounds__(W * 64) void hccl_moe_combine_backward_kernel(Combi
         if (threadIdx.x == 0) {
 #pragma unroll
             for (int j = 0; j < kBatch; ++j)
-                if (k + j < a.top_k) a.grad_weight[t * a.top_k + k + j] = (int32_t)r[j] < 0 ? 0.0f : dot[j];
+                if (k + j < a.top_k) a.grad_weight[t * a.top_k + k + j] = r[j] < a.capacity ? dot[j] : 0.0f;
         }
     }
 }
@@ -431,13 +471,16 @@ hipError_t launch_plan(const PlanArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_dispatch(const DispatchArgs& a, hcclDataType_t dt, hipStream_t s) {
-    const uint32_t es = dt == hcclFp32 ? 4 : 2, per = kPieceVecs * kWave * 16 / es;
+    const uint32_t es = dt == hcclFp32 ? 4 : 2, per = kWave * 16 / es;
     const uint32_t pieces = (uint32_t)((a.cols + per - 1) / per);
     const uint64_t blocks = (a.tokens * pieces + kWaves - 1) / kWaves;
     if (too_many(blocks, kThreads)) return hipErrorInvalidConfiguration;
+    const bool stream = a.tokens * (a.top_k + 1) * a.cols * es > kLastLevelCache;
     const dim3 grid((uint32_t)blocks), block(kThreads);
-    if (es == 2) hipLaunchKernelGGL(hccl_moe_dispatch_kernel<2>, grid, block, 0, s, a, pieces);
-    else hipLaunchKernelGGL(hccl_moe_dispatch_kernel<4>, grid, block, 0, s, a, pieces);
+    if (es == 2 && stream) hipLaunchKernelGGL((hccl_moe_dispatch_kernel<2, true>), grid, block, 0, s, a, pieces);
+    else if (es == 2) hipLaunchKernelGGL((hccl_moe_dispatch_kernel<2, false>), grid, block, 0, s, a, pieces);
+    else if (stream) hipLaunchKernelGGL((hccl_moe_dispatch_kernel<4, true>), grid, block, 0, s, a, pieces);
+    else hipLaunchKernelGGL((hccl_moe_dispatch_kernel<4, false>), grid, block, 0, s, a, pieces);
     return hipGetLastError();
 }
 
@@ -468,11 +511,16 @@ hipError_t launch_combine(const CombineArgs& a, hcclDataType_t dt, hipStream_t s
 
 hipError_t launch_combine_backward(const CombineBackwardArgs& a, hcclDataType_t dt, hipStream_t s) {
     if (too_many(a.tokens, 256)) return hipErrorInvalidConfiguration;
+    const uint64_t es = dt == hcclFp32 ? 4 : 2, vecs = a.cols * es / (kWave * 16);
+    const uint64_t arrays = (a.grad_z ? 1 : 0) + (a.grad_weight ? 1 : 0);
+    const bool stream = a.tokens * (a.top_k * arrays + 1) * a.cols * es > kLastLevelCache;
     return by_type(dt, [&](auto type) {
         constexpr int DT = decltype(type)::value;
         const dim3 grid((uint32_t)a.tokens);
-        if (a.cols <= kWave * kVecOf<DT>) hipLaunchKernelGGL((hccl_moe_combine_backward_kernel<DT, 1>), grid, dim3(64), 0, s, a);
-        else hipLaunchKernelGGL((hccl_moe_combine_backward_kernel<DT, 4>), grid, dim3(256), 0, s, a);
+        if (vecs < 1) hipLaunchKernelGGL((hccl_moe_combine_backward_kernel<DT, 1, false>), grid, dim3(64), 0, s, a);
+        else if (vecs < 2) hipLaunchKernelGGL((hccl_moe_combine_backward_kernel<DT, 2, false>), grid, dim3(128), 0, s, a);
+        else if (stream) hipLaunchKernelGGL((hccl_moe_combine_backward_kernel<DT, 4, true>), grid, dim3(256), 0, s, a);
+        else hipLaunchKernelGGL((hccl_moe_combine_backward_kernel<DT, 4, false>), grid, dim3(256), 0, s, a);
     });
 }
 
