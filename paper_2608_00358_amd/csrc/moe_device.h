@@ -124,7 +124,7 @@ __device__ __forceinline__ void store_row(char* p, uint64_t e, uint64_t cols, co
 // ---- reductions over groups of L lanes (16, 32 or 64); every lane gets the result
 template <int CTRL>
 __device__ __forceinline__ uint32_t dpp(uint32_t v) {
-    return (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, 0xf, 0xf, false);
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);  // (every lane has a source)
 }
 constexpr int kQuadSwap = 0xB1, kQuadHalf = 0x4E, kHalfMirror = 0x141, kMirror = 0x140;
 
@@ -134,8 +134,15 @@ __device__ __forceinline__ uint32_t fold_lanes(uint32_t v, OP op) {
     v = op(v, dpp<kQuadHalf>(v));
     v = op(v, dpp<kHalfMirror>(v));  // (a quad's lanes agree by now, so mirrored lanes are as good as shifted ones)
     v = op(v, dpp<kMirror>(v));
-    if constexpr (L >= 32) v = op(v, (uint32_t)__builtin_amdgcn_ds_swizzle((int)v, 0x401F));  // lane ^ 16
-    if constexpr (L >= 64) v = op(v, (uint32_t)__shfl_xor((int)v, 32));
+    // the halves of 32 lanes, and of the wave, side by side in two registers
+    if constexpr (L >= 32) {
+        const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        v = op(r[0], r[1]);
+    }
+    if constexpr (L >= 64) {
+        const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        v = op(r[0], r[1]);
+    }
     return v;
 }
 template <int L>

@@ -24,19 +24,17 @@ __device__ __forceinline__ void load_logits(const char* row, uint32_t e0, uint32
     if (!on || e0 >= experts) return;
     if (e0 + N <= experts) {
         constexpr int V = kVecOf<DT>;
-        if constexpr (N >= V) {
 #pragma unroll
-            for (int q = 0; q < N / V; ++q) {
-                float x[V];
-                widen<DT>(load16<ES>(row + (uint64_t)(e0 + q * V) * ES), x);
+        for (int q = 0; q < N / V; ++q) {
+            float x[V];
+            widen<DT>(load16<ES>(row + (uint64_t)(e0 + q * V) * ES), x);
 #pragma unroll
-                for (int i = 0; i < V; ++i) l[q * V + i] = x[i];
-            }
-        } else {
-            static_assert(N * ES == 8, "four 16-bit logits");
-            const typename Loose<ES>::x2 r = *gptr<typename Loose<ES>::x2>(row + (uint64_t)e0 * ES);
+            for (int i = 0; i < V; ++i) l[q * V + i] = x[i];
+        }
+        if constexpr (N % V == 4) {  // four 16-bit logits
+            const typename Loose<ES>::x2 r = *gptr<typename Loose<ES>::x2>(row + (uint64_t)(e0 + N - 4) * ES);
 #pragma unroll
-            for (int j = 0; j < N; ++j) l[j] = widen1<DT>((r[j / 2] >> (16 * (j & 1))) & 0xffffu);
+            for (int j = 0; j < 4; ++j) l[N - 4 + j] = widen1<DT>((r[j / 2] >> (16 * (j & 1))) & 0xffffu);
         }
     } else {
 #pragma unroll
@@ -47,11 +45,14 @@ __device__ __forceinline__ void load_logits(const char* row, uint32_t e0, uint32
     for (int j = 0; j < N; ++j) l[j] = l[j] > -kInf ? l[j] : -kInf;
 }
 
-// exp(l - m) with m the greatest logit: logits of +inf share the weight among themselves.
-__device__ __forceinline__ float exp_below(float l, float m) {
-    return l == -kInf ? 0.0f : l == m ? 1.0f : expf(l - m);
-}
-__device__ __forceinline__ float sigmoid(float l) { return 1.0f / (1.0f + expf(-l)); }
+// e^x as 2^(x log2 e): the product's rounding makes the error |x| 2^-24 of the value, and the values that
+// count have a small x: a chosen expert is near the greatest logit.
+__device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896340736f); }
+
+// exp(l - m) with m the greatest logit: logits of +inf share the weight among themselves (inf - inf is NaN,
+// and the lesser of NaN and 0 is 0).
+__device__ __forceinline__ float exp_below(float l, float m) { return l == -kInf ? 0.0f : exp_fast(fminf(l - m, 0.0f)); }
+__device__ __forceinline__ float sigmoid(float l) { return 1.0f / (1.0f + exp_fast(-l)); }
 
 // The order of a 16-bit float as an unsigned number (0 is none of them), and back.
 template <int DT>
@@ -94,17 +95,22 @@ __global__ __launch_bounds__(kRouteThreads) void hccl_moe_route_kernel(RouteArgs
         uint32_t key[N];
 #pragma unroll
         for (int j = 0; j < N; ++j) key[j] = l[j] == -kInf ? 0u : order16<DT>(l[j]) << 16 | (0xffffu - (e0 + j));
+        // Keys already chosen are the last one and those above it. Less the last one, modulo 2^32, they
+        // come below all the others, in their order: one subtraction takes them all out.
+        uint32_t last = 0;
         for (uint32_t k = 0; k < a.top_k; ++k) {
-            uint32_t best = key[0];
+            uint32_t best = key[0] - last;
 #pragma unroll
-            for (int j = 1; j < N; ++j) best = best > key[j] ? best : key[j];
-            best = maxu_lanes<L>(best);
-            if (sub == k && best) {
-                mine = 0xffffu - (best & 0xffffu);
-                logit = value16<DT>(best >> 16);
-            }
-#pragma unroll
-            for (int j = 0; j < N; ++j) key[j] = key[j] == best ? 0u : key[j];
+            for (int j = 1; j < N; ++j) best = max(best, key[j] - last);
+            last += maxu_lanes<L>(best);
+            mine = sub == k ? last : mine;
+            if (last == 0) break;  // (in every lane of the token; the others have theirs)
+        }
+        if (mine != ~0u && mine) {
+            logit = value16<DT>(mine >> 16);
+            mine = 0xffffu - (mine & 0xffffu);
+        } else {
+            mine = ~0u;
         }
     } else {
         float c[N];
@@ -117,20 +123,34 @@ __global__ __launch_bounds__(kRouteThreads) void hccl_moe_route_kernel(RouteArgs
             }
         }
         if constexpr (GROUPED) {
+            // lane g: the greatest one or two values of group g, of those that may be chosen. Where groups
+            // are whole lanes, a lane has found its own two first.
             __shared__ float seen[kRouteThreads * N];
             float* part = seen + slot * (L * N);
-#pragma unroll
-            for (int j = 0; j < N; ++j) part[e0 + j] = a.group_top == 2 && !a.bias && l[j] > -kInf ? score(l[j]) : c[j];
-            __syncthreads();
-            // lane g: the greatest one or two scores of group g, of those that may be chosen
             float one = -kInf, two = -kInf;
+            auto take = [&](float v) {
+                two = fmaxf(two, fminf(one, v));
+                one = fmaxf(one, v);
+            };
+            uint32_t each = a.group_size;
+            if (each % N == 0) {
+                each = each / N * 2;
+#pragma unroll
+                for (int j = 0; j < N; ++j) take(a.group_top == 2 && !a.bias && l[j] > -kInf ? score(l[j]) : c[j]);
+                part[sub * 2] = one;
+                part[sub * 2 + 1] = two;
+                one = two = -kInf;
+            } else {
+#pragma unroll
+                for (int j = 0; j < N; ++j) part[e0 + j] = a.group_top == 2 && !a.bias && l[j] > -kInf ? score(l[j]) : c[j];
+            }
+            __syncthreads();
             if (sub < a.groups) {
-                uint32_t i = sub % a.group_size;  // (lanes begin apart from each other: different banks)
-                for (uint32_t n = 0; n < a.group_size; ++n) {
-                    const float v = part[sub * a.group_size + i];
-                    two = fmaxf(two, fminf(one, v));
-                    one = fmaxf(one, v);
-                    if (++i == a.group_size) i = 0;
+                uint32_t i = sub % each;  // (lanes begin apart from each other: different banks)
+#pragma unroll 4
+                for (uint32_t n = 0; n < each; ++n) {
+                    take(part[sub * each + i]);
+                    if (++i == each) i = 0;
                 }
             }
             float left = a.group_top == 2 && two > -kInf ? one + two : one;
@@ -233,6 +253,7 @@ __global__ __launch_bounds__(kRouteThreads) void hccl_moe_route_backward_kernel(
     if (mine < a.experts) atomicAdd(&part[mine], du);  // (a router names an expert once)
     __syncthreads();
     if (!on || e0 >= a.experts) return;
+    const float inv = total > 0.0f ? 1.0f / total : 0.0f;
     float d[N];
 #pragma unroll
     for (int j = 0; j < N; ++j) {
@@ -240,37 +261,45 @@ __global__ __launch_bounds__(kRouteThreads) void hccl_moe_route_backward_kernel(
             const float s = l[j] == -kInf ? 0.0f : sigmoid(l[j]);
             d[j] = part[e0 + j] * s * (1.0f - s);
         } else {
-            d[j] = l[j] == 0.0f ? 0.0f : l[j] / total * (part[e0 + j] - common);
+            d[j] = l[j] * inv * (part[e0 + j] - common);
         }
     }
     char* out = (char*)a.grad_logits + t * a.ldg * ES;
     if (e0 + N <= a.experts) {
         constexpr int V = kVecOf<DT>;
-        if constexpr (N >= V) {
 #pragma unroll
-            for (int q = 0; q < N / V; ++q) {
-                float x[V];
+        for (int q = 0; q < N / V; ++q) {
+            float x[V];
 #pragma unroll
-                for (int i = 0; i < V; ++i) x[i] = d[q * V + i];
-                store16<ES>(out + (uint64_t)(e0 + q * V) * ES, narrow<DT>(x));
-            }
-            return;
+            for (int i = 0; i < V; ++i) x[i] = d[q * V + i];
+            store16<ES>(out + (uint64_t)(e0 + q * V) * ES, narrow<DT>(x));
         }
+        if constexpr (N % V == 4) {
+            typedef typename Loose<ES>::x2 v2;
+            *gptr<v2>(out + (uint64_t)(e0 + N - 4) * ES) = v2{narrow1<DT>(d[N - 4]) | narrow1<DT>(d[N - 3]) << 16, narrow1<DT>(d[N - 2]) | narrow1<DT>(d[N - 1]) << 16};
+        }
+        return;
     }
 #pragma unroll
     for (int j = 0; j < N; ++j)
         if (e0 + j < a.experts) store1<ES>(out + (uint64_t)(e0 + j) * ES, narrow1<DT>(d[j]));
 }
 
-// Lanes for a token: enough for its experts at N each, its k choices and its groups. 16 lanes with
-// 4 or 8 experts each take up to 128 experts, then 32 and 64 lanes with 8, then 64 with 16.
+// Lanes for a token: 16 where they hold its choices and groups one each and its experts 16 each, else 32
+// or 64. Few lanes leave little to exchange between them; a wave then routes four tokens.
+template <int L, int N>
+struct Shape {
+    static constexpr int lanes = L, each = N;
+};
 template <typename F>
 hipError_t by_lanes(uint32_t experts, uint32_t across, F f) {
-    if (across <= 16 && experts <= 64) return f(std::integral_constant<int, 16>(), std::integral_constant<int, 4>());
-    if (across <= 16 && experts <= 128) return f(std::integral_constant<int, 16>(), std::integral_constant<int, 8>());
-    if (experts <= 256) return f(std::integral_constant<int, 32>(), std::integral_constant<int, 8>());
-    if (experts <= 512) return f(std::integral_constant<int, 64>(), std::integral_constant<int, 8>());
-    return f(std::integral_constant<int, 64>(), std::integral_constant<int, 16>());
+    if (across <= 16 && experts <= 64) return f(Shape<16, 4>());
+    if (across <= 16 && experts <= 128) return f(Shape<16, 8>());
+    if (across <= 16 && experts <= 192) return f(Shape<16, 12>());
+    if (across <= 16 && experts <= 256) return f(Shape<16, 16>());
+    if (experts <= 256) return f(Shape<32, 8>());
+    if (experts <= 512) return f(Shape<32, 16>());
+    return f(Shape<64, 16>());
 }
 
 // A launch's threads are counted in 32 bits.
@@ -279,8 +308,8 @@ bool too_many(uint64_t tokens, uint32_t lanes) { return (tokens + kRouteThreads)
 template <int DT>
 hipError_t route_type(const RouteArgs& a, hipStream_t s) {
     const bool grouped = a.top_groups < a.groups;
-    return by_lanes(a.experts, a.top_k > a.groups ? a.top_k : a.groups, [&](auto lanes, auto each) {
-        constexpr int L = decltype(lanes)::value, N = decltype(each)::value;
+    return by_lanes(a.experts, a.top_k > a.groups ? a.top_k : a.groups, [&](auto shape) {
+        constexpr int L = decltype(shape)::lanes, N = decltype(shape)::each;
         if (too_many(a.tokens, L)) return hipErrorInvalidConfiguration;
         const dim3 grid((uint32_t)((a.tokens + kRouteThreads / L - 1) / (kRouteThreads / L))), block(kRouteThreads);
         if (grouped) {
@@ -296,8 +325,8 @@ hipError_t route_type(const RouteArgs& a, hipStream_t s) {
 
 template <int DT>
 hipError_t backward_type(const RouteBackwardArgs& a, hipStream_t s) {
-    return by_lanes(a.experts, a.top_k, [&](auto lanes, auto each) {
-        constexpr int L = decltype(lanes)::value, N = decltype(each)::value;
+    return by_lanes(a.experts, a.top_k, [&](auto shape) {
+        constexpr int L = decltype(shape)::lanes, N = decltype(shape)::each;
         if (too_many(a.tokens, L)) return hipErrorInvalidConfiguration;
         const dim3 grid((uint32_t)((a.tokens + kRouteThreads / L - 1) / (kRouteThreads / L))), block(kRouteThreads);
         hipLaunchKernelGGL((hccl_moe_route_backward_kernel<DT, L, N>), grid, block, 0, s, a);
