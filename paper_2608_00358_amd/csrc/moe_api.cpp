@@ -172,6 +172,7 @@ hcclResult_t hccl_moe_route(hcclComm_t comm, const hcclRouter_t* router, const v
         a.group_magic = ((1u << 20) + a.group_size - 1) / a.group_size;
         a.sigmoid = router->score == hcclScoreSigmoid;
         a.renormalize = router->renormalize != 0;
+        a.whole_sum = bias || !a.renormalize || (a.top_groups < a.groups && a.group_top == 2);
         return enqueue(c, [&] { return launch_route(a, dtype, (hipStream_t)stream); });
     });
 }

@@ -42,26 +42,37 @@ __device__ __forceinline__ void load_logits(const char* row, uint32_t e0, uint32
             if (e0 + j < experts) l[j] = widen1<DT>(load1<ES>(row + (uint64_t)(e0 + j) * ES));
     }
 #pragma unroll
-    for (int j = 0; j < N; ++j) l[j] = l[j] > -kInf ? l[j] : -kInf;
+    for (int j = 0; j < N; ++j) l[j] = fmaxf(l[j], -kInf);  // (the greater of NaN and -inf is -inf)
 }
 
-// e^x as 2^(x log2 e): the product's rounding makes the error |x| 2^-24 of the value, and the values that
-// count have a small x: a chosen expert is near the greatest logit.
-__device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896340736f); }
+constexpr float kLog2e = 1.44269504088896340736f;
 
-// exp(l - m) with m the greatest logit: logits of +inf share the weight among themselves (inf - inf is NaN,
-// and the lesser of NaN and 0 is 0).
-__device__ __forceinline__ float exp_below(float l, float m) { return l == -kInf ? 0.0f : exp_fast(fminf(l - m, 0.0f)); }
-__device__ __forceinline__ float sigmoid(float l) { return 1.0f / (1.0f + exp_fast(-l)); }
+// e^(l - m), m the greatest logit, as 2^((l - m) log2 e): the product's rounding makes the error |l - m| 2^-24
+// of the value, and the values that count are near m. (One fused product l log2 e - m log2 e would be off by
+// m 2^-24, which is anything where all logits are a mask's -1e9.) Logits of +inf share the weight among
+// themselves: they count as 0 and all others as -inf.
+struct Exponential {
+    float top;
+    bool infinite;
+    __device__ __forceinline__ explicit Exponential(float m) : top(m > -kInf && m < kInf ? m : 0.0f), infinite(m == kInf) {}
+    __device__ __forceinline__ float operator()(float l) const {
+        if (infinite) l = l == kInf ? 0.0f : -kInf;
+        return __builtin_amdgcn_exp2f((l - top) * kLog2e);
+    }
+};
+__device__ __forceinline__ float sigmoid(float l) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-l * kLog2e)); }
 
-// The order of a 16-bit float as an unsigned number (0 is none of them), and back.
-template <int DT>
-__device__ __forceinline__ uint32_t order16(float l) {
-    const uint32_t b = narrow1<DT>(l + 0.0f);  // (-0 counts as 0; l came from 16 bits, so nothing is rounded)
-    return b & 0x8000u ? (~b & 0xffffu) : (b | 0x8000u);
+// A 16-bit float widened to 32 bits has its 13 lowest bits free: the order of the float as an unsigned
+// number there, and 1023 less the expert below it. -0 counts as 0. And back.
+constexpr uint32_t kFree = 0x1fffu;
+__device__ __forceinline__ uint32_t order16(float l, uint32_t e) {
+    const int32_t x = __float_as_int(l + 0.0f);
+    return ((uint32_t)x ^ (((uint32_t)(x >> 31) & 0x7fffffffu & ~kFree) | 0x80000000u)) | (HCCL_MAX_EXPERTS - 1 - e);
 }
-template <int DT>
-__device__ __forceinline__ float value16(uint32_t o) { return widen1<DT>(o & 0x8000u ? o & 0x7fffu : ~o & 0xffffu); }
+__device__ __forceinline__ float value16(uint32_t key) {
+    const uint32_t o = key & ~kFree;
+    return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o & ~kFree);
+}
 
 // PACK: the choice is by 16-bit logits, so logit and expert fit one 32-bit key, greater for the
 // lower expert among equals: a round is one maximum. Otherwise a round is the greatest choice score,
@@ -77,26 +88,32 @@ __global__ __launch_bounds__(kRouteThreads) void hccl_moe_route_kernel(RouteArgs
     float l[N];
     load_logits<DT, N>(row, e0, a.experts, on, l);
 
-    float m = -kInf, total = 1.0f;
+    float m = -kInf, inv = 1.0f;  // greatest logit, 1 / the sum of the exponentials
     if (!a.sigmoid) {
 #pragma unroll
         for (int j = 0; j < N; ++j) m = fmaxf(m, l[j]);
         m = max_lanes<L>(m);
-        total = 0.0f;
-#pragma unroll
-        for (int j = 0; j < N; ++j) total += exp_below(l[j], m);
-        total = sum_lanes<L>(total);
     }
-    auto score = [&](float x) { return x == -kInf ? 0.0f : a.sigmoid ? sigmoid(x) : exp_below(x, m) / total; };
+    const Exponential exponential(m);
+    // Renormalised weights of a choice by logit have no need of the sum over all experts: it cancels.
+    if (!a.sigmoid && a.whole_sum) {
+        float total = 0.0f;
+#pragma unroll
+        for (int j = 0; j < N; ++j) total += exponential(l[j]);
+        total = sum_lanes<L>(total);
+        inv = total > 0.0f ? 1.0f / total : 0.0f;
+    }
+    auto score = [&](float x) { return x == -kInf ? 0.0f : a.sigmoid ? sigmoid(x) : exponential(x) * inv; };
 
     uint32_t mine = ~0u;   // lane k keeps choice k
     float logit = -kInf;
     if constexpr (PACK) {
         uint32_t key[N];
 #pragma unroll
-        for (int j = 0; j < N; ++j) key[j] = l[j] == -kInf ? 0u : order16<DT>(l[j]) << 16 | (0xffffu - (e0 + j));
+        for (int j = 0; j < N; ++j) key[j] = order16(l[j], e0 + j);
         // Keys already chosen are the last one and those above it. Less the last one, modulo 2^32, they
-        // come below all the others, in their order: one subtraction takes them all out.
+        // come below all the others, in their order: one subtraction takes them all out. (-inf is chosen
+        // like any other value, behind them all, and stands for no expert.)
         uint32_t last = 0;
         for (uint32_t k = 0; k < a.top_k; ++k) {
             uint32_t best = key[0] - last;
@@ -104,13 +121,10 @@ __global__ __launch_bounds__(kRouteThreads) void hccl_moe_route_kernel(RouteArgs
             for (int j = 1; j < N; ++j) best = max(best, key[j] - last);
             last += maxu_lanes<L>(best);
             mine = sub == k ? last : mine;
-            if (last == 0) break;  // (in every lane of the token; the others have theirs)
         }
-        if (mine != ~0u && mine) {
-            logit = value16<DT>(mine >> 16);
-            mine = 0xffffu - (mine & 0xffffu);
-        } else {
-            mine = ~0u;
+        if (sub < a.top_k) {
+            logit = value16(mine);
+            mine = logit > -kInf ? HCCL_MAX_EXPERTS - 1 - (mine & kFree) : ~0u;
         }
     } else {
         float c[N];
@@ -203,8 +217,11 @@ __global__ __launch_bounds__(kRouteThreads) void hccl_moe_route_kernel(RouteArgs
 //   du_k = scale (g_k - sum_j g_j u_j / r) / r (the second term only with the sum)
 //   softmax: dl_e = s_e (du_e - sum_k du_k u_k)     sigmoid: dl_e = du_e s_e (1 - s_e)
 // Scores are computed again from the logits: reading them costs less than storing them would.
-// The chosen experts' du go to the lanes that hold those experts through LDS.
-template <int DT, int L, int N>
+// DENSE: a softmax without renormalisation, where every expert's logit moves the weights. Otherwise only
+// the chosen ones' do: with the sum, sum_k du_k u_k is nothing, and s_k / r is the weight itself, so a
+// lane needs its choice's logit and no other. The gradients of the chosen go to the lanes that hold
+// those experts through LDS.
+template <int DT, int L, int N, bool DENSE>
 __global__ __launch_bounds__(kRouteThreads) void hccl_moe_route_backward_kernel(RouteBackwardArgs a) {
     constexpr int ES = kSize<DT>;
     __shared__ float slope[kRouteThreads * N];
@@ -218,51 +235,51 @@ __global__ __launch_bounds__(kRouteThreads) void hccl_moe_route_backward_kernel(
     float g = 0.0f, logit = -kInf;
     if (on && sub < a.top_k) {
         mine = (uint32_t)a.index[t * a.top_k + sub];
-        if (mine < a.experts) {
-            g = a.grad_weight[t * a.top_k + sub] * a.scale;
-            logit = widen1<DT>(load1<ES>(row + (uint64_t)mine * ES));
-            logit = logit > -kInf ? logit : -kInf;
-        }
+        g = a.grad_weight[t * a.top_k + sub] * a.scale;
     }
-    float l[N];
-    load_logits<DT, N>(row, e0, a.experts, on, l);
+    const bool some = mine < a.experts;
+    if (some) logit = fmaxf(widen1<DT>(load1<ES>(row + (uint64_t)mine * ES)), -kInf);
+    else g = 0.0f;
+    float l[DENSE ? N : 1];
+    if constexpr (DENSE) load_logits<DT, N>(row, e0, a.experts, on, l);
 #pragma unroll
     for (int j = 0; j < N; ++j) part[e0 + j] = 0.0f;
-    float m = -kInf, total = 1.0f;
-    if (!a.sigmoid) {
+    __syncthreads();
+    float common = 0.0f;
+    if constexpr (DENSE) {
+        float m = -kInf;
 #pragma unroll
         for (int j = 0; j < N; ++j) m = fmaxf(m, l[j]);
         m = max_lanes<L>(m);
+        const Exponential exponential(m);
+        float total = 0.0f;
 #pragma unroll
-        for (int j = 0; j < N; ++j) l[j] = exp_below(l[j], m);
-        total = 0.0f;
-#pragma unroll
-        for (int j = 0; j < N; ++j) total += l[j];
+        for (int j = 0; j < N; ++j) {
+            l[j] = exponential(l[j]);
+            total += l[j];
+        }
         total = sum_lanes<L>(total);
+        const float inv = total > 0.0f ? 1.0f / total : 0.0f;
+#pragma unroll
+        for (int j = 0; j < N; ++j) l[j] *= inv;
+        common = sum_lanes<L>(g * (exponential(logit) * inv));
+    } else {
+        float u = sigmoid(logit), d = u * (1.0f - u);  // (0 at -inf)
+        if (!a.sigmoid) u = d = Exponential(max_lanes<L>(logit))(logit);
+        if (a.renormalize) {
+            const float r = sum_lanes<L>(u), mean = sum_lanes<L>(g * u);
+            g = r > 0.0f ? (g - mean / r) / r : 0.0f;
+        }
+        g *= d;
     }
-    const float u = logit == -kInf ? 0.0f : a.sigmoid ? sigmoid(logit) : exp_below(logit, m) / total;
-    float du = g, common = 0.0f;
-    if (a.renormalize) {
-        // (the weights' sum is fixed, so sum_k du_k u_k is nothing)
-        const float r = sum_lanes<L>(u), mean = sum_lanes<L>(g * u);
-        du = r > 0.0f ? (g - mean / r) / r : 0.0f;
-    } else if (!a.sigmoid) {
-        common = sum_lanes<L>(g * u);
-    }
-    __syncthreads();
-    if (mine < a.experts) atomicAdd(&part[mine], du);  // (a router names an expert once)
+    if (some) atomicAdd(&part[mine], g);  // (a router names an expert once)
     __syncthreads();
     if (!on || e0 >= a.experts) return;
-    const float inv = total > 0.0f ? 1.0f / total : 0.0f;
     float d[N];
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-        if (a.sigmoid) {
-            const float s = l[j] == -kInf ? 0.0f : sigmoid(l[j]);
-            d[j] = part[e0 + j] * s * (1.0f - s);
-        } else {
-            d[j] = l[j] * inv * (part[e0 + j] - common);
-        }
+        d[j] = part[e0 + j];
+        if constexpr (DENSE) d[j] = l[j] * (d[j] - common);
     }
     char* out = (char*)a.grad_logits + t * a.ldg * ES;
     if (e0 + N <= a.experts) {
@@ -329,7 +346,8 @@ hipError_t backward_type(const RouteBackwardArgs& a, hipStream_t s) {
         constexpr int L = decltype(shape)::lanes, N = decltype(shape)::each;
         if (too_many(a.tokens, L)) return hipErrorInvalidConfiguration;
         const dim3 grid((uint32_t)((a.tokens + kRouteThreads / L - 1) / (kRouteThreads / L))), block(kRouteThreads);
-        hipLaunchKernelGGL((hccl_moe_route_backward_kernel<DT, L, N>), grid, block, 0, s, a);
+        if (!a.sigmoid && !a.renormalize) hipLaunchKernelGGL((hccl_moe_route_backward_kernel<DT, L, N, true>), grid, block, 0, s, a);
+        else hipLaunchKernelGGL((hccl_moe_route_backward_kernel<DT, L, N, false>), grid, block, 0, s, a);
         return hipGetLastError();
     });
 }
