@@ -190,9 +190,14 @@ __global__ __launch_bounds__(W * 64) void hccl_moe_product_few_kernel(ProductArg
 // (DIRECT: both operands' rows are 16-byte aligned) or through registers (any alignment, and the
 // last step of an inner size that is no multiple of 128, where bytes past the end are zero).
 //
-// LDS holds a row's 128 bytes as 8 chunks of 16; chunk c of row r lies in slot c ^ (r & 7), so that the
-// lanes that read one chunk of neighbouring rows use different banks. A direct load writes its 64
-// lanes one after the other, so a lane reads the chunk that belongs in its slot.
+// LDS holds a row's 128 bytes as 8 chunks of 16; chunk c of row r lies in slot c ^ (r / 2 & 7), so that the
+// 16 lanes served together, which read one chunk of 16 rows, use different banks (two rows fill the 256
+// bytes of all banks; with slot c ^ (r & 7) half of LDS' time went to conflicts). A direct load writes
+// its 64 lanes one after the other, so a lane reads the chunk that belongs in its slot.
+//
+// Fragments are read one part (32 of the 128 k) ahead of the matrix instructions. The barrier stands
+// before a step's last part: by then all its fragments have been read, so the next step's buffer can be
+// read and the old one refilled while that part is still being multiplied.
 constexpr uint32_t kStep = 128;
 
 typedef __attribute__((address_space(3))) void* lds_ptr;
@@ -224,7 +229,8 @@ __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_many_kernel(Pro
     const uint32_t n0 = nb * BN;
 
     // where this lane's part of each load comes from
-    const uint32_t lrow = lane >> 3, chunk = (lane & 7) ^ lrow;
+    const uint32_t lrow = lane >> 3;
+    auto chunk = [&](int i) { return ((lane & 7) ^ (((i < LA ? w * LA + i : w * LB + i - LA) & 1) * 4 + lrow / 2)) * 16; };
     const int8_t* src[LA + LB];
 #pragma unroll
     for (int i = 0; i < LA; ++i) {
@@ -254,16 +260,17 @@ __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_many_kernel(Pro
         if (DIRECT && s < whole) {
 #pragma unroll
             for (int i = 0; i < LA + LB; ++i)
-                __builtin_amdgcn_global_load_lds((const HCCL_AS1 void*)(src[i] + (uint64_t)s * kStep + chunk * 16), (lds_ptr)slot(s, i), 16, 0, 0);
-        } else if constexpr (!DIRECT) {
-#pragma unroll
-            for (int i = 0; i < LA + LB; ++i) held[i] = (v4u)load_k(src[i], s * kStep + chunk * 16, a.inner);
+                __builtin_amdgcn_global_load_lds((const HCCL_AS1 void*)(src[i] + (uint64_t)s * kStep + chunk(i)), (lds_ptr)slot(s, i), 16, 0, 0);
         } else {
 #pragma unroll
-            for (int i = 0; i < LA + LB; ++i) *(v4u*)(slot(s, i) + lane * 16) = (v4u)load_k(src[i], s * kStep + chunk * 16, a.inner);
+            for (int i = 0; i < LA + LB; ++i) {
+                const v4u v = (v4u)load_k(src[i], s * kStep + chunk(i), a.inner);
+                if constexpr (DIRECT) *(v4u*)(slot(s, i) + lane * 16) = v;
+                else held[i] = v;
+            }
         }
     };
-    auto land = [&](uint32_t s) {  // what was fetched for buffer s is there
+    auto land = [&](uint32_t s) {  // what was fetched for buffer s is there, for all waves
         if constexpr (!DIRECT) {
 #pragma unroll
             for (int i = 0; i < LA + LB; ++i) *(v4u*)(slot(s, i) + lane * 16) = held[i];
@@ -271,25 +278,47 @@ __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_many_kernel(Pro
         __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();
     };
-    if (steps) fetch(0);
-    for (uint32_t s = 0; s < steps; ++s) {
-        land(s);
-        if (s + 1 < steps) fetch(s + 1);
-        const char* pa = buffer(s) + (wm * TM * 32 + (lane & 31)) * kStep;
-        const char* pb = buffer(s) + (BM + wn * TN * 32 + (lane & 31)) * kStep;
+    v4i va[2][TM], vb[2][TN];
+    auto read = [&](uint32_t s, uint32_t part) {
+        const uint32_t at = ((part * 2 + (lane >> 5)) ^ (lane >> 1 & 7)) * 16;
+        const char* pa = buffer(s) + (wm * TM * 32 + (lane & 31)) * kStep + at;
+        const char* pb = buffer(s) + (BM + wn * TN * 32 + (lane & 31)) * kStep + at;
 #pragma unroll
-        for (uint32_t kk = 0; kk < 4; ++kk) {
-            const uint32_t at = ((kk * 2 + (lane >> 5)) ^ (lane & 7)) * 16;
-            v4i va[TM], vb[TN];
+        for (int y = 0; y < TN; ++y) vb[part & 1][y] = *(const v4i*)(pb + y * 32 * kStep);
 #pragma unroll
-            for (int y = 0; y < TN; ++y) vb[y] = *(const v4i*)(pb + y * 32 * kStep + at);
+        for (int x = 0; x < TM; ++x) va[part & 1][x] = *(const v4i*)(pa + x * 32 * kStep);
+    };
+    constexpr int kFirst = TM * TN >= 8 ? 2 : 1;  // instructions of a part before the next one's fragments are read
+    auto multiply = [&](uint32_t part, bool first) {
 #pragma unroll
-            for (int x = 0; x < TM; ++x) va[x] = *(const v4i*)(pa + x * 32 * kStep + at);
+        for (int x = 0; x < TM; ++x)
 #pragma unroll
             for (int y = 0; y < TN; ++y)
+                if ((x * TN + y < kFirst) == first) acc[y][x] = __builtin_amdgcn_mfma_i32_32x32x32_i8(vb[part & 1][y], va[part & 1][x], acc[y][x], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    if (steps) {
+        fetch(0);
+        land(0);
+        if (steps > 1) fetch(1);
+        read(0, 0);
+    }
+    for (uint32_t s = 0; s < steps; ++s) {
 #pragma unroll
-                for (int x = 0; x < TM; ++x) acc[y][x] = __builtin_amdgcn_mfma_i32_32x32x32_i8(vb[y], va[x], acc[y][x], 0, 0, 0);
+        for (uint32_t part = 0; part < 3; ++part) {
+            multiply(part, true);
+            read(s, part + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(part, false);
         }
+        multiply(3, true);
+        if (s + 1 < steps) {
+            land(s + 1);
+            if (s + 2 < steps) fetch(s + 2);
+            read(s + 1, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(3, false);
     }
     const float* bs = a.b_scale + (uint64_t)rows.expert * a.cols;
 #pragma unroll
