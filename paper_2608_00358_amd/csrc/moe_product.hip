@@ -6,6 +6,8 @@
 //
 // The weights are the instruction's first operand: a lane then holds neighbouring columns of one row.
 // The order of k within an instruction does not matter as long as both operands have the same.
+#include <type_traits>
+
 #include "moe_device.h"
 
 namespace hccl {
@@ -185,29 +187,42 @@ __global__ __launch_bounds__(W * 64) void hccl_moe_product_few_kernel(ProductArg
     }
 }
 
-// Many rows a segment: BM rows by BN columns a block, in WM x WN waves, k in steps of 128 through two
-// LDS buffers: while one is multiplied the next is filled, by loads that go to LDS directly
+// Many rows a segment: BM rows by BN columns a block, in WM x WN waves, k in steps of 64 through four
+// LDS buffers: one is multiplied while the next three are filled, by loads that go to LDS directly
 // (DIRECT: both operands' rows are 16-byte aligned) or through registers (any alignment, and the
-// last step of an inner size that is no multiple of 128, where bytes past the end are zero).
+// last step of an inner size that is no multiple of 64, where bytes past the end are zero).
 //
-// LDS holds a row's 128 bytes as 8 chunks of 16; chunk c of row r lies in slot c ^ (r / 2 & 7), so that the
-// 16 lanes served together, which read one chunk of 16 rows, use different banks (two rows fill the 256
-// bytes of all banks; with slot c ^ (r & 7) half of LDS' time went to conflicts). A direct load writes
-// its 64 lanes one after the other, so a lane reads the chunk that belongs in its slot.
+// LDS holds a row's 64 bytes as 4 chunks of 16; chunk c of row r lies in slot c ^ (r / 4 & 3), so that the
+// 16 lanes served together, which read one chunk of 16 rows, use different banks (four rows fill the 256
+// bytes of all banks; with conflicts LDS was busy twice as long). A direct load writes its 64 lanes one
+// after the other, so a lane reads the chunk that belongs in its slot.
 //
-// Fragments are read one part (32 of the 128 k) ahead of the matrix instructions. The barrier stands
-// before a step's last part: by then all its fragments have been read, so the next step's buffer can be
+// Fragments are read one part (32 of the 64 k) ahead of the matrix instructions. The barrier stands
+// inside a step's last part: by then all its fragments have been read, so the next step's buffer can be
 // read and the old one refilled while that part is still being multiplied.
-constexpr uint32_t kStep = 128;
+constexpr uint32_t kStep = 64;
+constexpr uint32_t kBuffers = 4;
 
 typedef __attribute__((address_space(3))) void* lds_ptr;
+
+template <int N>
+__device__ __forceinline__ void wait_loads() {  // until at most N loads are on their way, and LDS is done
+    __builtin_amdgcn_s_waitcnt(0x70 | N);
+}
+// A barrier that leaves loads to LDS in flight; nothing that touches memory moves across it.
+__device__ __forceinline__ void meet() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
 
 template <int DT, int BM, int BN, int WM, int WN, bool DIRECT>
 __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_many_kernel(ProductArgs a, uint32_t nblocks) {
     constexpr int W = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
-    constexpr int LA = BM / 8 / W, LB = BN / 8 / W;  // loads a wave has to make for a step: 8 rows each
-    static_assert(BM % (8 * W) == 0 && BN % (8 * W) == 0, "whole loads");
-    __shared__ __attribute__((aligned(128))) char lds[2 * (BM + BN) * kStep];
+    constexpr int LA = BM / 16 / W, LB = BN / 16 / W, LN = LA + LB;  // loads a wave makes for a step: 16 rows each
+    static_assert(BM % (16 * W) == 0 && BN % (16 * W) == 0 && 3 * LN < 16, "whole loads, and a counter that holds them");
+    constexpr uint32_t kBuffer = (BM + BN) * kStep;
+    __shared__ __attribute__((aligned(256))) char lds[kBuffers * kBuffer];
     const uint32_t lane = threadIdx.x & 63, w = first_lane(threadIdx.x >> 6);
 
     // Blocks go to the XCDs in turn; each XCD gets neighbouring tiles, in bands of 8 column blocks, so
@@ -228,22 +243,20 @@ __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_many_kernel(Pro
     if (!find_rows<BM>(a, tile, rows)) return;
     const uint32_t n0 = nb * BN;
 
-    // where this lane's part of each load comes from
-    const uint32_t lrow = lane >> 3;
-    auto chunk = [&](int i) { return ((lane & 7) ^ (((i < LA ? w * LA + i : w * LB + i - LA) & 1) * 4 + lrow / 2)) * 16; };
-    const int8_t* src[LA + LB];
+    // where this lane's part of each load comes from, and where in a buffer each load goes
+    const uint32_t lrow = lane >> 2, chunk = ((lane & 3) ^ (lrow >> 2)) * 16;
+    const int8_t* src[LN];
 #pragma unroll
     for (int i = 0; i < LA; ++i) {
-        const uint64_t m = rows.first + (w * LA + i) * 8 + lrow;
-        src[i] = a.a + (m < rows.end ? m : rows.end - 1) * a.lda;
+        const uint64_t m = rows.first + (w * LA + i) * 16 + lrow;
+        src[i] = a.a + (m < rows.end ? m : rows.end - 1) * a.lda + chunk;
     }
 #pragma unroll
     for (int i = 0; i < LB; ++i) {
-        const uint32_t n = n0 + (w * LB + i) * 8 + lrow;
-        src[LA + i] = a.b + ((uint64_t)rows.expert * a.cols + (n < a.cols ? n : a.cols - 1)) * a.ldb;
+        const uint32_t n = n0 + (w * LB + i) * 16 + lrow;
+        src[LA + i] = a.b + ((uint64_t)rows.expert * a.cols + (n < a.cols ? n : a.cols - 1)) * a.ldb + chunk;
     }
-    auto buffer = [&](uint32_t s) { return lds + (s & 1) * ((BM + BN) * kStep); };
-    auto slot = [&](uint32_t s, int i) { return buffer(s) + (i < LA ? (w * LA + i) * 8 : BM + (w * LB + i - LA) * 8) * kStep; };
+    auto slot = [&](uint32_t s, int i) { return lds + (s % kBuffers) * kBuffer + (i < LA ? (w * LA + i) * 16 : BM + (w * LB + i - LA) * 16) * kStep; };
 
     v16i acc[TN][TM];
 #pragma unroll
@@ -255,38 +268,37 @@ __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_many_kernel(Pro
 
     const uint32_t steps = (a.inner + kStep - 1) / kStep, whole = a.inner / kStep;
     const uint32_t wm = w % WM, wn = w / WM;
-    v4u held[DIRECT ? 1 : LA + LB];
-    auto fetch = [&](uint32_t s) {  // begins to fill buffer s
-        if (DIRECT && s < whole) {
+    v4u held[2][DIRECT ? 1 : LN];  // on their way through registers: steps of either parity
+    // Begins to bring in step s. INNER: it and the steps before it are whole.
+    auto fetch = [&](uint32_t s, int parity, auto inner) {
+        if (DIRECT && (inner.value || s < whole)) {
 #pragma unroll
-            for (int i = 0; i < LA + LB; ++i)
-                __builtin_amdgcn_global_load_lds((const HCCL_AS1 void*)(src[i] + (uint64_t)s * kStep + chunk(i)), (lds_ptr)slot(s, i), 16, 0, 0);
-        } else {
+            for (int i = 0; i < LN; ++i)
+                __builtin_amdgcn_global_load_lds((const HCCL_AS1 void*)(src[i] + (uint64_t)s * kStep), (lds_ptr)slot(s, i), 16, 0, 0);
+        } else if (inner.value || s < steps) {
 #pragma unroll
-            for (int i = 0; i < LA + LB; ++i) {
-                const v4u v = (v4u)load_k(src[i], s * kStep + chunk(i), a.inner);
+            for (int i = 0; i < LN; ++i) {
+                const v4u v = inner.value ? load16<1>(src[i] + (uint64_t)s * kStep) : (v4u)load_k(src[i] - chunk, s * kStep + chunk, a.inner);
                 if constexpr (DIRECT) *(v4u*)(slot(s, i) + lane * 16) = v;
-                else held[i] = v;
+                else held[parity][i] = v;
             }
         }
     };
-    auto land = [&](uint32_t s) {  // what was fetched for buffer s is there, for all waves
+    auto put = [&](uint32_t s, int parity) {  // what registers hold of step s goes to its buffer
         if constexpr (!DIRECT) {
 #pragma unroll
-            for (int i = 0; i < LA + LB; ++i) *(v4u*)(slot(s, i) + lane * 16) = held[i];
+            for (int i = 0; i < LN; ++i) *(v4u*)(slot(s, i) + lane * 16) = held[parity][i];
         }
-        __builtin_amdgcn_s_waitcnt(0);
-        __syncthreads();
     };
     v4i va[2][TM], vb[2][TN];
     auto read = [&](uint32_t s, uint32_t part) {
-        const uint32_t at = ((part * 2 + (lane >> 5)) ^ (lane >> 1 & 7)) * 16;
-        const char* pa = buffer(s) + (wm * TM * 32 + (lane & 31)) * kStep + at;
-        const char* pb = buffer(s) + (BM + wn * TN * 32 + (lane & 31)) * kStep + at;
+        const uint32_t at = (s % kBuffers) * kBuffer + ((part * 2 + (lane >> 5)) ^ (lane >> 2 & 3)) * 16 + (lane & 31) * kStep;
+        const char* pa = lds + wm * TM * 32 * kStep + at;
+        const char* pb = lds + (BM + wn * TN * 32) * kStep + at;
 #pragma unroll
-        for (int y = 0; y < TN; ++y) vb[part & 1][y] = *(const v4i*)(pb + y * 32 * kStep);
+        for (int y = 0; y < TN; ++y) vb[part][y] = *(const v4i*)(pb + y * 32 * kStep);
 #pragma unroll
-        for (int x = 0; x < TM; ++x) va[part & 1][x] = *(const v4i*)(pa + x * 32 * kStep);
+        for (int x = 0; x < TM; ++x) va[part][x] = *(const v4i*)(pa + x * 32 * kStep);
     };
     constexpr int kFirst = TM * TN >= 8 ? 2 : 1;  // instructions of a part before the next one's fragments are read
     auto multiply = [&](uint32_t part, bool first) {
@@ -294,45 +306,111 @@ __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_many_kernel(Pro
         for (int x = 0; x < TM; ++x)
 #pragma unroll
             for (int y = 0; y < TN; ++y)
-                if ((x * TN + y < kFirst) == first) acc[y][x] = __builtin_amdgcn_mfma_i32_32x32x32_i8(vb[part & 1][y], va[part & 1][x], acc[y][x], 0, 0, 0);
+                if ((x * TN + y < kFirst) == first) acc[y][x] = __builtin_amdgcn_mfma_i32_32x32x32_i8(vb[part][y], va[part][x], acc[y][x], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
     };
-    if (steps) {
-        fetch(0);
-        land(0);
-        if (steps > 1) fetch(1);
-        read(0, 0);
-    }
-    for (uint32_t s = 0; s < steps; ++s) {
-#pragma unroll
-        for (uint32_t part = 0; part < 3; ++part) {
-            multiply(part, true);
-            read(s, part + 1);
-            __builtin_amdgcn_sched_barrier(0);
-            multiply(part, false);
-        }
-        multiply(3, true);
-        if (s + 1 < steps) {
-            land(s + 1);
-            if (s + 2 < steps) fetch(s + 2);
-            read(s + 1, 0);
-        }
+    auto step = [&](uint32_t s, int parity, auto inner) {
+        multiply(0, true);
+        read(s, 1);
         __builtin_amdgcn_sched_barrier(0);
-        multiply(3, false);
+        multiply(0, false);
+        multiply(1, true);
+        // Step s + 1 has landed for all waves, and all have read step s, whose buffer step s + 4 takes. Loads of
+        // the steps s + 2 and s + 3 stay on their way (where both are direct loads).
+        if (inner.value || s + 2 < steps) put(s + 2, parity);
+        if (!DIRECT) __builtin_amdgcn_s_waitcnt(0xc07f);  // LDS alone
+        else if (inner.value || s + 3 < whole) wait_loads<2 * LN>();
+        else wait_loads<0>();
+        meet();
+        fetch(s + 4, parity, inner);
+        if (inner.value || s + 1 < steps) read(s + 1, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(1, false);
+    };
+    if (steps) {
+        const std::false_type any;
+        if constexpr (DIRECT) {
+#pragma unroll
+            for (uint32_t s = 0; s < kBuffers; ++s) fetch(s, 0, any);
+        } else {
+            fetch(0, 0, any), fetch(1, 1, any);
+            put(0, 0);
+            if (steps > 1) put(1, 1);
+            fetch(2, 0, any), fetch(3, 1, any);
+        }
+        if (DIRECT && whole >= kBuffers) wait_loads<3 * LN>();
+        else wait_loads<0>();
+        meet();
+        read(0, 0);
+        uint32_t s = 0;
+        for (; s + 5 < whole; s += 2) {
+            step(s, 0, std::true_type());
+            step(s + 1, 1, std::true_type());
+        }
+#pragma unroll 1
+        for (; s < steps; s += 2) {
+            step(s, 0, any);
+            if (s + 1 < steps) step(s + 1, 1, any);
+        }
     }
+
+    // The wave's TM x TN blocks leave through its own part of LDS, as rows of TN * 32 results: lanes that hold
+    // four results each of 32 rows would store 16 bytes of a line at a time.
+    constexpr int ES = kSize<DT>;
+    constexpr uint32_t kLine = TN * 32 * ES, kChunks = kLine / 16;  // bytes of a row
+    constexpr int kRowsEach = kBuffers * kBuffer / W / kLine >= TM * 32 ? TM : kBuffers * kBuffer / W / kLine / 32;  // blocks of 32 rows at a time
+    static_assert(kRowsEach >= 1 && TM % kRowsEach == 0, "a block of rows fits");
+    meet();
+    char* mine = lds + w * (kBuffers * kBuffer / W);
     const float* bs = a.b_scale + (uint64_t)rows.expert * a.cols;
+    const uint32_t c0 = n0 + wn * TN * 32;
+    float scale[TN][4][4];
 #pragma unroll
-    for (int x = 0; x < TM; ++x) {
-        const uint64_t m = rows.first + (wm * TM + x) * 32 + (lane & 31);
-        if (m >= rows.end) continue;
-        const float as = a.a_scale[m];
+    for (int y = 0; y < TN; ++y)
 #pragma unroll
-        for (int y = 0; y < TN; ++y)
+        for (int g = 0; g < 4; ++g)
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const uint32_t n = n0 + (wn * TN + y) * 32 + g * 8 + (lane >> 5) * 4;
-                if (n < a.cols) store_four<DT>(a, m, n, v4i{acc[y][x][4 * g], acc[y][x][4 * g + 1], acc[y][x][4 * g + 2], acc[y][x][4 * g + 3]}, as, bs);
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t n = c0 + y * 32 + g * 8 + (lane >> 5) * 4 + i;
+                scale[y][g][i] = bs[n < a.cols ? n : a.cols - 1];
             }
+#pragma unroll
+    for (int x0 = 0; x0 < TM; x0 += kRowsEach) {
+        const uint64_t m0 = rows.first + (wm * TM + x0) * 32;
+#pragma unroll
+        for (int x = 0; x < kRowsEach; ++x) {
+            const uint64_t m = m0 + x * 32 + (lane & 31);
+            const float as = a.a_scale[m < rows.end ? m : rows.end - 1];
+            const uint32_t r = x * 32 + (lane & 31);
+#pragma unroll
+            for (int y = 0; y < TN; ++y)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    float v[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] = (float)acc[y][x0 + x][4 * g + i] * as * scale[y][g][i];
+                    // columns y * 32 + g * 8 + (lane / 32) * 4 of row r; a row's 16-byte chunks lie in another order in
+                    // each pair of rows
+                    if constexpr (ES == 2) {
+                        const uint32_t at = ((y * 4 + g) ^ (r >> 1)) % kChunks * 16 + (lane >> 5) * 8;
+                        *(v2u*)(mine + r * kLine + at) = v2u{narrow1<DT>(v[0]) | narrow1<DT>(v[1]) << 16, narrow1<DT>(v[2]) | narrow1<DT>(v[3]) << 16};
+                    } else {
+                        const uint32_t at = ((y * 8 + g * 2 + (lane >> 5)) ^ (r >> 1)) % kChunks * 16;
+                        *(v4u*)(mine + r * kLine + at) = v4u{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+                    }
+                }
+        }
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0xc07f);
+        constexpr uint32_t kRowsAtOnce = 64 / kChunks, V = 16 / ES;
+        const uint32_t c = lane % kChunks;
+#pragma unroll
+        for (uint32_t r0 = 0; r0 < kRowsEach * 32; r0 += kRowsAtOnce) {
+            const uint32_t r = r0 + lane / kChunks;
+            const v4u v = *(const v4u*)(mine + r * kLine + (c ^ (r >> 1)) % kChunks * 16);
+            if (m0 + r < rows.end) store_row<ES>((char*)a.out + (m0 + r) * a.ldo * ES, c0 + c * V, a.cols, v);
+        }
+        asm volatile("" ::: "memory");
     }
 }
 
