@@ -16,12 +16,11 @@ namespace {
 typedef int32_t v4i __attribute__((ext_vector_type(4)));
 typedef int32_t v16i __attribute__((ext_vector_type(16)));
 
-// Rows [first, end) of tile `tile` of BM rows, and its expert; false where there are fewer tiles.
-// One lane a segment: tiles of a segment, their running sum, and the segment that holds the tile.
 struct Rows {
     uint64_t first, end;
     uint32_t expert;
 };
+
 // (offsets outside 0 .. rows are clipped, and a segment that ends before it begins is empty)
 __device__ __forceinline__ void segment(const ProductArgs& a, uint32_t s, uint64_t& first, uint64_t& end) {
     const int64_t lo = a.offsets[s], hi = a.offsets[s + 1];
@@ -29,6 +28,24 @@ __device__ __forceinline__ void segment(const ProductArgs& a, uint32_t s, uint64
     end = hi < (int64_t)first ? first : (uint64_t)hi < a.rows ? (uint64_t)hi : a.rows;
 }
 
+// Tiles of BM rows that the segments have.
+template <uint32_t BM>
+__device__ __forceinline__ uint32_t count_tiles(const ProductArgs& a) {
+    if (!a.offsets) return (uint32_t)((a.rows + BM - 1) / BM);
+    const uint32_t lane = threadIdx.x & 63;
+    uint32_t n = 0;
+    for (uint32_t s = lane; s < a.segments; s += kWave) {
+        uint64_t first, end;
+        segment(a, s, first, end);
+        n += (uint32_t)((end - first + BM - 1) / BM);
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) n += (uint32_t)__shfl_xor((int)n, d);
+    return first_lane(n);
+}
+
+// Rows [first, end) of tile `tile`, and its expert; false where there are fewer tiles. One lane a segment:
+// the tiles in it, their running sum, and the segment that holds the tile.
 template <uint32_t BM>
 __device__ __forceinline__ bool find_rows(const ProductArgs& a, uint32_t tile, Rows& out) {
     if (!a.offsets) {
@@ -62,22 +79,6 @@ __device__ __forceinline__ bool find_rows(const ProductArgs& a, uint32_t tile, R
         left -= all;
     }
     return false;
-}
-
-// Tiles that the segments have.
-template <uint32_t BM>
-__device__ __forceinline__ uint32_t count_tiles(const ProductArgs& a) {
-    if (!a.offsets) return (uint32_t)((a.rows + BM - 1) / BM);
-    const uint32_t lane = threadIdx.x & 63;
-    uint32_t n = 0;
-    for (uint32_t s = lane; s < a.segments; s += kWave) {
-        uint64_t first, end;
-        segment(a, s, first, end);
-        n += (uint32_t)((end - first + BM - 1) / BM);
-    }
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) n += (uint32_t)__shfl_xor((int)n, d);
-    return first_lane(n);
 }
 
 // 16 bytes of a row at k; bytes from `inner` on are zero: the row's last 16 bytes, shifted down.
@@ -202,6 +203,7 @@ __global__ __launch_bounds__(W * 64) void hccl_moe_product_few_kernel(ProductArg
 // read and the old one refilled while that part is still being multiplied.
 constexpr uint32_t kStep = 64;
 constexpr uint32_t kBuffers = 4;
+constexpr uint32_t kBand = 4;  // (4, 8 and 16: 328, 332 and 348 us for 16 384 rows through 16 experts)
 
 typedef __attribute__((address_space(3))) void* lds_ptr;
 
@@ -225,19 +227,21 @@ __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_many_kernel(Pro
     __shared__ __attribute__((aligned(256))) char lds[kBuffers * kBuffer];
     const uint32_t lane = threadIdx.x & 63, w = first_lane(threadIdx.x >> 6);
 
-    // Blocks go to the XCDs in turn; each XCD gets neighbouring tiles, in bands of 8 column blocks, so
-    // that the tiles it works on at a time share their rows and weights in its L2.
+    // Blocks go to the XCDs in turn; each XCD gets neighbouring tiles, in bands of kBand column blocks, so
+    // that the tiles it works on at a time share their rows and weights in its L2. (Ends of segments, which are
+    // less work, in a turn of their own after the whole tiles read the weights twice: 346 us against 337 for
+    // 16 384 rows through 16 experts.)
     uint32_t tile, nb;
     {
         const uint32_t tiles = count_tiles<BM>(a);
         const uint64_t all = (uint64_t)tiles * nblocks, share = (all + 7) / 8;
         const uint64_t id = (blockIdx.x & 7) * share + blockIdx.x / 8;
         if (blockIdx.x / 8 >= share || id >= all) return;
-        const uint64_t banded = (uint64_t)(nblocks / 8 * 8) * tiles;
-        const uint32_t width = id < banded ? 8 : nblocks % 8;
-        const uint64_t at = id < banded ? id % (8ull * tiles) : id - banded;
+        const uint64_t banded = (uint64_t)(nblocks / kBand * kBand) * tiles;
+        const uint32_t width = id < banded ? kBand : nblocks % kBand;
+        const uint64_t at = id < banded ? id % ((uint64_t)kBand * tiles) : id - banded;
         tile = (uint32_t)(at / width);
-        nb = (id < banded ? (uint32_t)(id / (8ull * tiles)) * 8 : nblocks / 8 * 8) + (uint32_t)(at % width);
+        nb = (id < banded ? (uint32_t)(id / ((uint64_t)kBand * tiles)) * kBand : nblocks / kBand * kBand) + (uint32_t)(at % width);
     }
     Rows rows;
     if (!find_rows<BM>(a, tile, rows)) return;
@@ -267,7 +271,9 @@ __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_many_kernel(Pro
             for (int r = 0; r < 16; ++r) acc[y][x][r] = 0;
 
     const uint32_t steps = (a.inner + kStep - 1) / kStep, whole = a.inner / kStep;
-    const uint32_t wm = w % WM, wn = w / WM;
+    // Waves of the same rows are neighbours, and so on different SIMDs: where an end of a segment leaves
+    // waves without rows, those that have some share out the matrix units.
+    const uint32_t wm = w / WN, wn = w % WN;
     v4u held[2][DIRECT ? 1 : LN];  // on their way through registers: steps of either parity
     // Begins to bring in step s. INNER: it and the steps before it are whole.
     auto fetch = [&](uint32_t s, int parity, auto inner) {
@@ -301,12 +307,14 @@ __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_many_kernel(Pro
         for (int x = 0; x < TM; ++x) va[part][x] = *(const v4i*)(pa + x * 32 * kStep);
     };
     constexpr int kFirst = TM * TN >= 8 ? 2 : 1;  // instructions of a part before the next one's fragments are read
-    auto multiply = [&](uint32_t part, bool first) {
+    auto multiply = [&](uint32_t part, bool first) {  // ahead of the other wave's loads on the SIMD
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int x = 0; x < TM; ++x)
 #pragma unroll
             for (int y = 0; y < TN; ++y)
                 if ((x * TN + y < kFirst) == first) acc[y][x] = __builtin_amdgcn_mfma_i32_32x32x32_i8(vb[part][y], va[part][x], acc[y][x], 0, 0, 0);
+        __builtin_amdgcn_s_setprio(0);
         __builtin_amdgcn_sched_barrier(0);
     };
     auto step = [&](uint32_t s, int parity, auto inner) {
@@ -327,6 +335,26 @@ __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_many_kernel(Pro
         __builtin_amdgcn_sched_barrier(0);
         multiply(1, false);
     };
+    auto idle = [&](uint32_t s, int parity, auto inner) {  // a step of a wave without rows: brings in its part for the others
+        if (inner.value || s + 2 < steps) put(s + 2, parity);
+        if (!DIRECT) __builtin_amdgcn_s_waitcnt(0xc07f);
+        else if (inner.value || s + 3 < whole) wait_loads<2 * LN>();
+        else wait_loads<0>();
+        meet();
+        fetch(s + 4, parity, inner);
+    };
+    auto walk = [&](auto each) {
+        uint32_t s = 0;
+        for (; s + 5 < whole; s += 2) {
+            each(s, 0, std::true_type());
+            each(s + 1, 1, std::true_type());
+        }
+#pragma unroll 1
+        for (; s < steps; s += 2) {
+            each(s, 0, std::false_type());
+            if (s + 1 < steps) each(s + 1, 1, std::false_type());
+        }
+    };
     if (steps) {
         const std::false_type any;
         if constexpr (DIRECT) {
@@ -341,17 +369,12 @@ __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_many_kernel(Pro
         if (DIRECT && whole >= kBuffers) wait_loads<3 * LN>();
         else wait_loads<0>();
         meet();
+        if (rows.first + wm * TM * 32 >= rows.end) {
+            walk(idle);
+            return;
+        }
         read(0, 0);
-        uint32_t s = 0;
-        for (; s + 5 < whole; s += 2) {
-            step(s, 0, std::true_type());
-            step(s + 1, 1, std::true_type());
-        }
-#pragma unroll 1
-        for (; s < steps; s += 2) {
-            step(s, 0, any);
-            if (s + 1 < steps) step(s + 1, 1, any);
-        }
+        walk(step);
     }
 
     // The wave's TM x TN blocks leave through its own part of LDS, as rows of TN * 32 results: lanes that hold
@@ -360,7 +383,7 @@ __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_many_kernel(Pro
     constexpr uint32_t kLine = TN * 32 * ES, kChunks = kLine / 16;  // bytes of a row
     constexpr int kRowsEach = kBuffers * kBuffer / W / kLine >= TM * 32 ? TM : kBuffers * kBuffer / W / kLine / 32;  // blocks of 32 rows at a time
     static_assert(kRowsEach >= 1 && TM % kRowsEach == 0, "a block of rows fits");
-    meet();
+    // (nothing reads the buffers after the last step's barrier)
     char* mine = lds + w * (kBuffers * kBuffer / W);
     const float* bs = a.b_scale + (uint64_t)rows.expert * a.cols;
     const uint32_t c0 = n0 + wn * TN * 32;
