@@ -193,84 +193,95 @@ __device__ __forceinline__ uint32_t code4(float a, float b, float c, float d, fl
     return ((uint32_t)i & 0xffu) | ((uint32_t)j & 0xffu) << 8 | ((uint32_t)k & 0xffu) << 16 | (uint32_t)l << 24;
 }
 
-// Values of vector e of a row: x, or silu(x) * (the row's second half).
+// What a lane keeps of a vector between the two passes: its bits, or the gated values, silu(x) * (the row's
+// second half), which cost more to make than registers. silu(x) = x / (1 + 2^(-x log2 e)); the exponent's
+// rounding is |x| 2^-24 of a term that is small where |x| is large.
 template <int DT, bool GATED>
-__device__ __forceinline__ void row_values(const char* src, uint64_t e, uint64_t cols, float (&x)[kVecOf<DT>]) {
-    constexpr int ES = kSize<DT>, V = kVecOf<DT>;
-    widen<DT>(load_row<ES>(src, e, cols), x);
-    if constexpr (GATED) {
-        float up[V];
-        widen<DT>(load_row<ES>(src + cols * ES, e, cols), up);
+struct Held {
+    float x[kVecOf<DT>];
+    __device__ __forceinline__ void values(float (&y)[kVecOf<DT>]) const {
 #pragma unroll
-        for (int i = 0; i < V; ++i) x[i] = x[i] * (1.0f / (1.0f + expf(-x[i]))) * up[i];
+        for (int i = 0; i < kVecOf<DT>; ++i) y[i] = x[i];
     }
+};
+template <int DT>
+struct Held<DT, false> {
+    v4u x;
+    __device__ __forceinline__ void values(float (&y)[kVecOf<DT>]) const { widen<DT>(x, y); }
+};
+template <int DT, bool GATED, bool WHOLE>
+__device__ __forceinline__ Held<DT, GATED> hold(const char* src, uint64_t e, uint64_t cols) {
+    constexpr int ES = kSize<DT>;
+    Held<DT, GATED> h;
+    if constexpr (GATED) {
+        float up[kVecOf<DT>];
+        const v4u g = piece_load<ES, WHOLE, false>(src, e, cols), u = piece_load<ES, WHOLE, false>(src + cols * ES, e, cols);
+        widen<DT>(g, h.x);
+        widen<DT>(u, up);
+#pragma unroll
+        for (int i = 0; i < kVecOf<DT>; ++i) h.x[i] *= __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(h.x[i] * -1.44269504088896340736f)) * up[i];
+    } else {
+        h.x = piece_load<ES, WHOLE, false>(src, e, cols);
+    }
+    return h;
 }
 
-// W waves a row; a lane keeps up to kKeep vectors between the two passes and reads longer rows twice.
-constexpr int kKeep = 8;
+// The greatest magnitude's bits among the values of a vector.
+template <int DT, bool GATED>
+__device__ __forceinline__ uint32_t top_of(const Held<DT, GATED>& h, uint32_t top) {
+    float x[kVecOf<DT>];
+    h.values(x);
+#pragma unroll
+    for (int i = 0; i < kVecOf<DT>; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+    return top;
+}
 
-template <int DT, bool GATED, int W>
-__global__ __launch_bounds__(kThreads) void hccl_moe_quantize_kernel(QuantizeArgs a) {
+constexpr int kKeep = 4;
+
+// A row that lane `at` of `step / V` shares: its vectors are at e = at * V, + step, ...; the first kKeep of them
+// stay in registers between the two passes, those of longer rows are read twice.
+template <int DT, bool GATED, int W, bool WHOLE>
+__device__ __forceinline__ void quantize_row(const QuantizeArgs& a, uint64_t t, uint32_t at, uint32_t* tops, bool on) {
     constexpr int V = kVecOf<DT>, ES = kSize<DT>;
-    __shared__ uint32_t tops[kWaves];
-    const uint32_t lane = threadIdx.x & 63, w = first_lane(threadIdx.x >> 6);
-    const uint64_t t = (uint64_t)blockIdx.x * (kWaves / W) + w / W;
-    const uint32_t at = W == 1 ? lane : threadIdx.x;
     constexpr uint64_t step = (uint64_t)W * kWave * V;
-    const bool on = t < a.rows && (!a.limit || (int64_t)t < *a.limit);
+    const uint32_t lane = threadIdx.x & 63, w = first_lane(threadIdx.x >> 6);
     const char* src = (const char*)a.x + t * a.ldx * ES;
-    float x[kKeep][V];
+    Held<DT, GATED> x[kKeep];
+    const uint32_t copies = a.row ? a.top_k : 1u;
+    const uint32_t mine = !a.row ? (uint32_t)t : on && lane < copies ? (uint32_t)a.row[t * a.top_k + lane] : ~0u;
     uint32_t top = 0;
     if (on) {
 #pragma unroll
-        for (int u = 0; u < kKeep; ++u) {
-            const uint64_t e = u * step + at * V;
-#pragma unroll
-            for (int i = 0; i < V; ++i) x[u][i] = 0.0f;
-            if (e < a.cols) row_values<DT, GATED>(src, e, a.cols, x[u]);
-        }
+        for (int u = 0; u < kKeep; ++u)
+            if (u * step + at * V < a.cols) x[u] = hold<DT, GATED, WHOLE>(src, u * step + at * V, a.cols);
 #pragma unroll
         for (int u = 0; u < kKeep; ++u)
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const uint32_t b = __float_as_uint(x[u][i]) & 0x7fffffffu;
-                top = top > b ? top : b;
-            }
-        for (uint64_t e = kKeep * step + at * V; e < a.cols; e += step) {
-            float y[V];
-            row_values<DT, GATED>(src, e, a.cols, y);
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const uint32_t b = __float_as_uint(y[i]) & 0x7fffffffu;
-                top = top > b ? top : b;
-            }
-        }
+            if (u * step + at * V < a.cols) top = top_of<DT, GATED>(x[u], top);
+        for (uint64_t e = kKeep * step + at * V; e < a.cols; e += step) top = top_of<DT, GATED>(hold<DT, GATED, WHOLE>(src, e, a.cols), top);
     }
     top = maxu_lanes<64>(top);
     if constexpr (W > 1) {
         if (lane == 0) tops[w] = top;
         __syncthreads();
 #pragma unroll
-        for (int q = 0; q < kWaves; ++q) top = top > tops[q] ? top : tops[q];
+        for (int q = 0; q < W; ++q) top = max(top, tops[w / W * W + q]);
     }
     if (!on) return;
     float inv, scale;
     row_scale(top, inv, scale);
-    const uint32_t copies = a.row ? a.top_k : 1u;
-    const uint32_t mine = !a.row ? (uint32_t)t : lane < copies ? (uint32_t)a.row[t * a.top_k + lane] : ~0u;
-    auto store = [&](uint64_t e, const float (&y)[V]) {
-        uint32_t lo, hi = 0;
-        // (a row of infinities times 0 is no number, and no number has no code)
-        if (inv == 0.0f) lo = 0;
-        else {
+    auto store = [&](uint64_t e, const Held<DT, GATED>& h) {
+        float y[V];
+        h.values(y);
+        uint32_t lo = 0, hi = 0;
+        if (inv != 0.0f) {  // (infinity times 0 is no number, and no number has no code)
             lo = code4(y[0], y[1], y[2], y[3], inv);
             if constexpr (V == 8) hi = code4(y[4], y[5], y[6], y[7], inv);
         }
         for (uint32_t k = 0; k < copies; ++k) {
             const uint32_t r = a.row ? at_lane(mine, k) : (uint32_t)t;
-            if (r >= a.capacity || (int32_t)r < 0) continue;
+            if (r >= a.capacity) continue;
             char* dst = (char*)a.codes + (uint64_t)r * a.ldq + e;
-            if (e + V <= a.cols) {
+            if (WHOLE || e + V <= a.cols) {
                 if constexpr (V == 8) *gptr<typename Loose<1>::x2>(dst) = typename Loose<1>::x2{lo, hi};
                 else *gptr<typename Loose<1>::x1>(dst) = lo;
             } else {
@@ -281,21 +292,23 @@ __global__ __launch_bounds__(kThreads) void hccl_moe_quantize_kernel(QuantizeArg
         }
     };
 #pragma unroll
-    for (int u = 0; u < kKeep; ++u) {
-        const uint64_t e = u * step + at * V;
-        if (e < a.cols) store(e, x[u]);
+    for (int u = 0; u < kKeep; ++u)
+        if (u * step + at * V < a.cols) store(u * step + at * V, x[u]);
+    for (uint64_t e = kKeep * step + at * V; e < a.cols; e += step) store(e, hold<DT, GATED, WHOLE>(src, e, a.cols));
+    if (at < copies && w % W == 0) {
+        const uint32_t r = a.row ? mine : (uint32_t)t;
+        if (r < a.capacity) a.scale[r] = scale;
     }
-    for (uint64_t e = kKeep * step + at * V; e < a.cols; e += step) {
-        float y[V];
-        row_values<DT, GATED>(src, e, a.cols, y);
-        store(e, y);
-    }
-    if (at == 0) {
-        for (uint32_t k = 0; k < copies; ++k) {
-            const uint32_t r = a.row ? (uint32_t)a.row[t * a.top_k + k] : (uint32_t)t;
-            if (r < a.capacity && (int32_t)r >= 0) a.scale[r] = scale;
-        }
-    }
+}
+
+template <int DT, bool GATED, int W>
+__global__ __launch_bounds__(kThreads) void hccl_moe_quantize_kernel(QuantizeArgs a) {
+    __shared__ uint32_t tops[kWaves];
+    const uint64_t t = (uint64_t)blockIdx.x * (kWaves / W) + first_lane(threadIdx.x >> 6) / W;
+    const bool on = t < a.rows && (!a.limit || (int64_t)t < *a.limit);
+    const uint32_t at = threadIdx.x & (W * kWave - 1);
+    if (a.cols % kVecOf<DT> == 0) quantize_row<DT, GATED, W, true>(a, t, at, tops, on);
+    else quantize_row<DT, GATED, W, false>(a, t, at, tops, on);
 }
 
 // --------------------------------------------------------------------------------------- combine
@@ -484,17 +497,28 @@ hipError_t launch_dispatch(const DispatchArgs& a, hcclDataType_t dt, hipStream_t
     return hipGetLastError();
 }
 
+template <int DT, bool GATED, int W>
+void launch_quantize_rows(const QuantizeArgs& a, hipStream_t s) {
+    hipLaunchKernelGGL((hccl_moe_quantize_kernel<DT, GATED, W>), dim3((uint32_t)((a.rows * W + kWaves - 1) / kWaves)), dim3(kThreads), 0, s, a);
+}
+
+template <int DT, bool GATED>
+void quantize_type(const QuantizeArgs& a, hipStream_t s) {
+    // As many waves a row as leave its lanes at most kKeep vectors, up to 4; one for up to 2 vectors a lane
+    // (16 384 rows of bf16: 512 columns 1 / 2 / 4 waves 7.3 / 9.9 / 14 us, 4 096 columns 50 / 37 / 38 us, 8 192
+    // columns 106 / 87 / 71 us).
+    const uint64_t vecs = (a.cols + kWave * kVecOf<DT> - 1) / (kWave * kVecOf<DT>);
+    if (vecs <= 2) launch_quantize_rows<DT, GATED, 1>(a, s);
+    else if (vecs <= 2 * kKeep) launch_quantize_rows<DT, GATED, 2>(a, s);
+    else launch_quantize_rows<DT, GATED, 4>(a, s);
+}
+
 hipError_t launch_quantize(const QuantizeArgs& a, hcclDataType_t dt, bool gated, hipStream_t s) {
     if (too_many(a.rows, kThreads)) return hipErrorInvalidConfiguration;
     return by_type(dt, [&](auto type) {
         constexpr int DT = decltype(type)::value;
-        // a wave a row where that fills the chip and the row stays in its registers
-        const bool narrow_rows = a.cols <= kKeep * kWave * kVecOf<DT> && a.rows >= 2048;
-        const dim3 grid((uint32_t)(narrow_rows ? (a.rows + kWaves - 1) / kWaves : a.rows)), block(kThreads);
-        if (narrow_rows && gated) hipLaunchKernelGGL((hccl_moe_quantize_kernel<DT, true, 1>), grid, block, 0, s, a);
-        else if (narrow_rows) hipLaunchKernelGGL((hccl_moe_quantize_kernel<DT, false, 1>), grid, block, 0, s, a);
-        else if (gated) hipLaunchKernelGGL((hccl_moe_quantize_kernel<DT, true, kWaves>), grid, block, 0, s, a);
-        else hipLaunchKernelGGL((hccl_moe_quantize_kernel<DT, false, kWaves>), grid, block, 0, s, a);
+        if (gated) quantize_type<DT, true>(a, s);
+        else quantize_type<DT, false>(a, s);
     });
 }
 
