@@ -128,8 +128,9 @@ __device__ __forceinline__ void store_four(const ProductArgs& a, uint64_t m, uin
 
 // Few rows a segment: 16 MB rows by 16 NB columns a block, whose W waves share out the k axis in
 // steps of 128 and join their sums through LDS. Weights go from memory to registers: each is used
-// by one block only. A lane reads 32 neighbouring bytes of a row, four lanes the 128 of a step.
-template <int DT, int MB, int NB, int W>
+// by one block only. A lane reads 32 neighbouring bytes of a row, four lanes the 128 of a step; the loads
+// of U steps are on their way together.
+template <int DT, int MB, int NB, int W, int U>
 __global__ __launch_bounds__(W * 64) void hccl_moe_product_few_kernel(ProductArgs a, uint32_t nblocks) {
     constexpr uint32_t BM = 16 * MB, BN = 16 * NB;
     __shared__ v4i part[W][MB * NB][64];
@@ -155,22 +156,38 @@ __global__ __launch_bounds__(W * 64) void hccl_moe_product_few_kernel(ProductArg
     for (int x = 0; x < MB; ++x)
 #pragma unroll
         for (int y = 0; y < NB; ++y) acc[x][y] = v4i{0, 0, 0, 0};
-    for (uint32_t k0 = w * 128; k0 < a.inner; k0 += W * 128) {
+    v4i va[U][MB][2], vb[U][NB][2];
+    auto fetch = [&](int u, uint32_t k0, auto inner) {  // INNER: the step lies inside the rows
         const uint32_t k = k0 + q * 32;
-        v4i va[MB][2], vb[NB][2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
 #pragma unroll
-            for (int y = 0; y < NB; ++y) vb[y][h] = load_k(pb[y], k + 16 * h, a.inner);
+            for (int y = 0; y < NB; ++y) vb[u][y][h] = inner.value ? (v4i)load16<1>(pb[y] + k + 16 * h) : load_k(pb[y], k + 16 * h, a.inner);
 #pragma unroll
-            for (int x = 0; x < MB; ++x) va[x][h] = load_k(pa[x], k + 16 * h, a.inner);
+            for (int x = 0; x < MB; ++x) va[u][x][h] = inner.value ? (v4i)load16<1>(pa[x] + k + 16 * h) : load_k(pa[x], k + 16 * h, a.inner);
         }
+    };
+    auto multiply = [&](int u) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int x = 0; x < MB; ++x)
 #pragma unroll
-                for (int y = 0; y < NB; ++y) acc[x][y] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vb[y][h], va[x][h], acc[x][y], 0, 0, 0);
+                for (int y = 0; y < NB; ++y) acc[x][y] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vb[u][y][h], va[u][x][h], acc[x][y], 0, 0, 0);
+    };
+    uint32_t k0 = w * 128;
+    for (; k0 + (U - 1) * (W * 128) + 128 <= a.inner; k0 += U * (W * 128)) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) fetch(u, k0 + u * (W * 128), std::true_type());
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int u = 0; u < U; ++u) multiply(u);
+    }
+#pragma unroll 1
+    for (; k0 < a.inner; k0 += W * 128) {
+        if (k0 + 128 <= a.inner) fetch(0, k0, std::true_type());
+        else fetch(0, k0, std::false_type());
+        multiply(0);
     }
 #pragma unroll
     for (int x = 0; x < MB; ++x)
@@ -449,16 +466,50 @@ hipError_t launch_many(const ProductArgs& a, hipStream_t s) {
     return hipGetLastError();
 }
 
+template <int DT, int MB, int NB, int W, int U>
+hipError_t launch_few(const ProductArgs& a, hipStream_t s) {
+    const uint64_t nblocks = (a.cols + 16 * NB - 1) / (16 * NB), tiles = (a.rows + 16 * MB - 1) / (16 * MB) + (a.offsets ? a.segments : 0);
+    if (tiles * nblocks > 0xffffffffull / (W * 64)) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL((hccl_moe_product_few_kernel<DT, MB, NB, W, U>), dim3((uint32_t)(tiles * nblocks)), dim3(W * 64), 0, s, a, (uint32_t)nblocks);
+    return hipGetLastError();
+}
+
+// The largest tiles that leave at least 3/4 of the CUs a block and are not mostly empty: a tile is at most
+// twice as high as a segment has rows on average. us, in bf16 (rows x inner x columns x experts):
+//                            256 x 256   128 x 128   64 x 128   64 x 64    few rows
+//   16384 x 4096 x 4096 x 16    329          -          -         -           -
+//   12000 x 1024 x 1024 x 16     25         30         31        37           -
+//    2999 x 1408 x 2050 x 12     29         23         27        32           -
+//    2048 x 2048 x 2048 x 64     65         60         60        67          76
+//    1024 x 2048 x 2048 x 64     63         57         56         -          58
+//     512 x 2048 x 2048 x 64     62         55         52         -          49
+//    1024 x 4096 x 4096 x 1      50         24         33        43          87
+//     256 x 4096 x 4096 x 1      49         19         16        14          24
+//      64 x 4096 x 4096 x 1      32         17         15        13          10
+// Few rows: 32 a block from 9 rows a segment on (16 where one expert has no more), and of 64, 32 and 16 columns
+// the most that leave every CU a block, with k shared out over more waves the fewer columns there are
+// (1 x 4096 x 4096: 16 columns 5.4 us, 32 columns 6.7 us, 64 columns 10.5 us; 256 x 2048 x 2048 x 64: 74, 47, 47 us).
 template <int DT>
 hipError_t product_type(const ProductArgs& a, int cus, hipStream_t s) {
-    const uint64_t each = a.rows / a.segments;
-    if (each >= 512) return launch_many<DT, 256, 256, 2, 4>(a, s);
-    if (each >= 64) return launch_many<DT, 128, 128, 2, 2>(a, s);
-    const uint32_t nblocks = (a.cols + 63) / 64;
-    const uint64_t tiles = (a.rows + 15) / 16 + (a.offsets ? a.segments : 0);
-    if (tiles * nblocks > 0xffffffffull / 256) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL((hccl_moe_product_few_kernel<DT, 1, 4, 4>), dim3((uint32_t)(tiles * nblocks)), dim3(256), 0, s, a, nblocks);
-    return hipGetLastError();
+    const uint64_t each = a.rows / a.segments, spread = a.offsets ? (a.rows < a.segments ? a.rows : a.segments) : 0;
+    auto blocks = [&](uint64_t bm, uint64_t bn) {  // about; half a tile more for every segment
+        return (a.offsets ? a.rows / bm + (spread + 1) / 2 : (a.rows + bm - 1) / bm) * ((a.cols + bn - 1) / bn);
+    };
+    const uint64_t most = (uint64_t)cus * 3 / 4;
+    if (each >= 128 && blocks(256, 256) >= most) return launch_many<DT, 256, 256, 2, 4>(a, s);
+    if (each >= 32 && blocks(128, 128) >= most) return launch_many<DT, 128, 128, 2, 2>(a, s);
+    if (each >= 16 && blocks(64, 128) >= most) return launch_many<DT, 64, 128, 1, 4>(a, s);
+    if (each > 64) return launch_many<DT, 64, 64, 1, 2>(a, s);
+    if (a.offsets ? each <= 8 : a.rows <= 16) {
+        const uint64_t tiles = a.offsets ? a.rows / 16 + spread : 1, cols16 = (a.cols + 15) / 16;
+        if (tiles * (cols16 / 4) >= (uint64_t)cus) return launch_few<DT, 1, 4, 4, 2>(a, s);
+        if (tiles * (cols16 / 2) >= (uint64_t)cus) return launch_few<DT, 1, 2, 4, 4>(a, s);
+        return launch_few<DT, 1, 1, 16, 2>(a, s);
+    }
+    const uint64_t tiles = a.offsets ? a.rows / 32 + spread : (a.rows + 31) / 32, cols16 = (a.cols + 15) / 16;
+    if (tiles * (cols16 / 4) >= (uint64_t)cus) return launch_few<DT, 2, 4, 4, 2>(a, s);
+    if (tiles * (cols16 / 2) >= (uint64_t)cus) return launch_few<DT, 2, 2, 8, 2>(a, s);
+    return launch_few<DT, 2, 1, 16, 2>(a, s);
 }
 
 }  // namespace
