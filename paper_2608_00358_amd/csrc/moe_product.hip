@@ -292,20 +292,19 @@ __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_many_kernel(Pro
     // waves without rows, those that have some share out the matrix units.
     const uint32_t wm = w / WN, wn = w % WN;
     v4u held[2][DIRECT ? 1 : LN];  // on their way through registers: steps of either parity
-    // Begins to bring in step s. INNER: it and the steps before it are whole.
-    auto fetch = [&](uint32_t s, int parity, auto inner) {
+    // Load i of those that bring in step s. INNER: it and the steps before it are whole.
+    auto fetch = [&](uint32_t s, int parity, auto inner, int i) {
         if (DIRECT && (inner.value || s < whole)) {
-#pragma unroll
-            for (int i = 0; i < LN; ++i)
-                __builtin_amdgcn_global_load_lds((const HCCL_AS1 void*)(src[i] + (uint64_t)s * kStep), (lds_ptr)slot(s, i), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((const HCCL_AS1 void*)(src[i] + (uint64_t)s * kStep), (lds_ptr)slot(s, i), 16, 0, 0);
         } else if (inner.value || s < steps) {
-#pragma unroll
-            for (int i = 0; i < LN; ++i) {
-                const v4u v = inner.value ? load16<1>(src[i] + (uint64_t)s * kStep) : (v4u)load_k(src[i] - chunk, s * kStep + chunk, a.inner);
-                if constexpr (DIRECT) *(v4u*)(slot(s, i) + lane * 16) = v;
-                else held[parity][i] = v;
-            }
+            const v4u v = inner.value ? load16<1>(src[i] + (uint64_t)s * kStep) : (v4u)load_k(src[i] - chunk, s * kStep + chunk, a.inner);
+            if constexpr (DIRECT) *(v4u*)(slot(s, i) + lane * 16) = v;
+            else held[parity][i] = v;
         }
+    };
+    auto fetch_all = [&](uint32_t s, int parity, auto inner) {
+#pragma unroll
+        for (int i = 0; i < LN; ++i) fetch(s, parity, inner, i);
     };
     auto put = [&](uint32_t s, int parity) {  // what registers hold of step s goes to its buffer
         if constexpr (!DIRECT) {
@@ -314,32 +313,39 @@ __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_many_kernel(Pro
         }
     };
     v4i va[2][TM], vb[2][TN];
-    auto read = [&](uint32_t s, uint32_t part) {
+    auto read = [&](uint32_t s, uint32_t part, int i) {  // fragment i of a part, in the order of their use
         const uint32_t at = (s % kBuffers) * kBuffer + ((part * 2 + (lane >> 5)) ^ (lane >> 2 & 3)) * 16 + (lane & 31) * kStep;
-        const char* pa = lds + wm * TM * 32 * kStep + at;
-        const char* pb = lds + (BM + wn * TN * 32) * kStep + at;
-#pragma unroll
-        for (int y = 0; y < TN; ++y) vb[part][y] = *(const v4i*)(pb + y * 32 * kStep);
-#pragma unroll
-        for (int x = 0; x < TM; ++x) va[part][x] = *(const v4i*)(pa + x * 32 * kStep);
+        if (i == 0) va[part][0] = *(const v4i*)(lds + wm * TM * 32 * kStep + at);
+        else if (i <= TN) vb[part][i - 1] = *(const v4i*)(lds + (BM + (wn * TN + i - 1) * 32) * kStep + at);
+        else va[part][i - TN] = *(const v4i*)(lds + (wm * TM + i - TN) * 32 * kStep + at);
     };
-    constexpr int kFirst = TM * TN >= 8 ? 2 : 1;  // instructions of a part before the next one's fragments are read
-    auto multiply = [&](uint32_t part, bool first) {  // ahead of the other wave's loads on the SIMD
-        __builtin_amdgcn_s_setprio(1);
+    // A part's matrix instructions, one after the other, each followed by a load or a read or two: a wave
+    // that makes its loads in one go waits for the units that take them, and its SIMD with it.
+    constexpr int kMfmas = TM * TN, kReads = TM + TN, kFirst = kMfmas >= 8 ? 2 : 1;
+    auto multiply = [&](uint32_t part, int from, int to, auto between) {
 #pragma unroll
-        for (int x = 0; x < TM; ++x)
-#pragma unroll
-            for (int y = 0; y < TN; ++y)
-                if ((x * TN + y < kFirst) == first) acc[y][x] = __builtin_amdgcn_mfma_i32_32x32x32_i8(vb[part][y], va[part][x], acc[y][x], 0, 0, 0);
-        __builtin_amdgcn_s_setprio(0);
-        __builtin_amdgcn_sched_barrier(0);
+        for (int i = from; i < to; ++i) {
+            acc[i % TN][i / TN] = __builtin_amdgcn_mfma_i32_32x32x32_i8(vb[part][i % TN], va[part][i / TN], acc[i % TN][i / TN], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            between(i);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     };
+    // Those of n operations that go behind instruction i, spread over `slots` of them from `from` on.
+    auto spread = [](int i, int from, int slots, int n, auto f) {
+        const int at = i - from;
+        if (at < 0 || at >= slots) return;
+#pragma unroll
+        for (int r = at * n / slots; r < (at + 1) * n / slots; ++r) f(r);
+    };
+    // reads end two instructions before the part does, so that they are there when the next one begins
+    constexpr int kReadSlots = kMfmas >= 8 ? kMfmas - kFirst - 2 : kMfmas >= 4 ? 2 : 1;
     auto step = [&](uint32_t s, int parity, auto inner) {
-        multiply(0, true);
-        read(s, 1);
-        __builtin_amdgcn_sched_barrier(0);
-        multiply(0, false);
-        multiply(1, true);
+        multiply(0, 0, kMfmas, [&](int i) {
+            spread(i, kFirst - 1, kReadSlots, kReads, [&](int r) { read(s, 1, r); });
+            spread(i, kFirst - 1, kMfmas - kFirst + 1, LN, [&](int r) { fetch(s + 3, parity ^ 1, inner, r); });
+        });
+        multiply(1, 0, kFirst, [](int) {});
         // Step s + 1 has landed for all waves, and all have read step s, whose buffer step s + 4 takes. Loads of
         // the steps s + 2 and s + 3 stay on their way (where both are direct loads).
         if (inner.value || s + 2 < steps) put(s + 2, parity);
@@ -347,22 +353,22 @@ __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_many_kernel(Pro
         else if (inner.value || s + 3 < whole) wait_loads<2 * LN>();
         else wait_loads<0>();
         meet();
-        fetch(s + 4, parity, inner);
-        if (inner.value || s + 1 < steps) read(s + 1, 0);
-        __builtin_amdgcn_sched_barrier(0);
-        multiply(1, false);
+        const bool more = inner.value || s + 1 < steps;
+        multiply(1, kFirst, kMfmas, [&](int i) {
+            if (more) spread(i, kFirst, kReadSlots, kReads, [&](int r) { read(s + 1, 0, r); });
+        });
     };
     auto idle = [&](uint32_t s, int parity, auto inner) {  // a step of a wave without rows: brings in its part for the others
+        fetch_all(s + 3, parity ^ 1, inner);
         if (inner.value || s + 2 < steps) put(s + 2, parity);
         if (!DIRECT) __builtin_amdgcn_s_waitcnt(0xc07f);
         else if (inner.value || s + 3 < whole) wait_loads<2 * LN>();
         else wait_loads<0>();
         meet();
-        fetch(s + 4, parity, inner);
     };
     auto walk = [&](auto each) {
         uint32_t s = 0;
-        for (; s + 5 < whole; s += 2) {
+        for (; s + 4 < whole; s += 2) {
             each(s, 0, std::true_type());
             each(s + 1, 1, std::true_type());
         }
@@ -376,21 +382,22 @@ __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_many_kernel(Pro
         const std::false_type any;
         if constexpr (DIRECT) {
 #pragma unroll
-            for (uint32_t s = 0; s < kBuffers; ++s) fetch(s, 0, any);
+            for (uint32_t s = 0; s < kBuffers - 1; ++s) fetch_all(s, 0, any);
         } else {
-            fetch(0, 0, any), fetch(1, 1, any);
+            fetch_all(0, 0, any), fetch_all(1, 1, any);
             put(0, 0);
             if (steps > 1) put(1, 1);
-            fetch(2, 0, any), fetch(3, 1, any);
+            fetch_all(2, 0, any);
         }
-        if (DIRECT && whole >= kBuffers) wait_loads<3 * LN>();
+        if (DIRECT && whole >= kBuffers - 1) wait_loads<2 * LN>();
         else wait_loads<0>();
         meet();
         if (rows.first + wm * TM * 32 >= rows.end) {
             walk(idle);
             return;
         }
-        read(0, 0);
+#pragma unroll
+        for (int r = 0; r < kReads; ++r) read(0, 0, r);
         walk(step);
     }
 
