@@ -94,31 +94,69 @@ __device__ __forceinline__ void store1(void* p, uint32_t v) {
     else *gptr<uint32_t>(p) = v;
 }
 
-// Vector `e / V` of a row of `cols` elements that begins at p; elements past the end are zero.
+// The 16 bytes of v moved down by `bits` (0 .. 127), with zeros from above.
+__device__ __forceinline__ v4u shift_down(const v4u& v, uint32_t bits) {
+    uint64_t lo = (uint64_t)v[1] << 32 | v[0], hi = (uint64_t)v[3] << 32 | v[2];
+    if (bits >= 64) {
+        lo = hi;
+        hi = 0;
+    }
+    const uint32_t n = bits & 63;
+    if (n) {
+        lo = lo >> n | hi << (64 - n);
+        hi >>= n;
+    }
+    return v4u{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+}
+
+// The vector at element e of a row of `cols` elements (at least one) that begins at p; elements past the end
+// are zero. The row's last vector is read where the one asked for would pass the end, and moved down: one
+// load for every lane, where element by element each would wait for the one before.
 template <int ES>
 __device__ __forceinline__ v4u load_row(const char* p, uint64_t e, uint64_t cols) {
     constexpr int V = 16 / ES;
-    if (e + V <= cols) return load16<ES>(p + e * ES);
+    if (cols >= V) {
+        const uint64_t at = e + V <= cols ? e : cols - V;
+        const v4u v = load16<ES>(p + at * ES);
+        if (e == at) return v;
+        return e >= cols ? v4u{0, 0, 0, 0} : shift_down(v, (uint32_t)(e - at) * ES * 8);
+    }
     v4u r = {0, 0, 0, 0};
 #pragma unroll
-    for (int i = 0; i < V; ++i)
-        if (e + i < cols) {
-            const uint32_t b = load1<ES>(p + (e + i) * ES);
-            if constexpr (ES == 2) r[i / 2] |= b << (16 * (i & 1));
-            else r[i] = b;
-        }
+    for (int i = 0; i < V; ++i) {
+        const uint64_t at = e + i < cols ? e + i : cols - 1;
+        const uint32_t b = e + i < cols ? load1<ES>(p + at * ES) : 0u;
+        if constexpr (ES == 2) r[i / 2] |= b << (16 * (i & 1));
+        else r[i] = b;
+    }
     return r;
 }
+// The same for a store: the last elements of a row in pieces of 8, 4 and 2 bytes.
 template <int ES>
 __device__ __forceinline__ void store_row(char* p, uint64_t e, uint64_t cols, const v4u& r) {
     constexpr int V = 16 / ES;
     if (e + V <= cols) return store16<ES>(p + e * ES, r);
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-        if (e + i < cols) {
-            if constexpr (ES == 2) store1<ES>(p + (e + i) * ES, (r[i / 2] >> (16 * (i & 1))) & 0xffffu);
-            else store1<ES>(p + (e + i) * ES, r[i]);
+    if (e >= cols) return;
+    const uint32_t n = (uint32_t)(cols - e);  // 1 .. V - 1
+    char* at = p + e * ES;
+    v4u v = r;
+    if (n * ES >= 8) {
+        typedef typename Loose<ES>::x2 x2;
+        *gptr<x2>(at) = x2{v[0], v[1]};
+        v = v4u{v[2], v[3], 0, 0};
+        at += 8;
+    }
+    if constexpr (ES == 4) {
+        if (n & 1) store1<4>(at, v[0]);
+    } else {
+        typedef uint32_t x1 __attribute__((aligned(2)));
+        if (n & 2) {
+            *gptr<x1>(at) = v[0];
+            v[0] = v[1];
+            at += 4;
         }
+        if (n & 1) store1<2>(at, v[0] & 0xffffu);
+    }
 }
 
 // ---- reductions over groups of L lanes (16, 32 or 64); every lane gets the result

@@ -86,14 +86,7 @@ __device__ __forceinline__ v4i load_k(const int8_t* row, uint32_t k, uint32_t in
     if (k + 16 <= inner) return (v4i)load16<1>(row + k);
     v4i r = {0, 0, 0, 0};
     if (k >= inner) return r;
-    if (inner >= 16) {
-        const v4u t = load16<1>(row + inner - 16);
-        uint64_t lo = (uint64_t)t[1] << 32 | t[0], hi = (uint64_t)t[3] << 32 | t[2];
-        const uint32_t bits = 8 * (k + 16 - inner);  // 8 .. 120
-        lo = bits < 64 ? lo >> bits | hi << (64 - bits) : hi >> (bits - 64);
-        hi = bits < 64 ? hi >> bits : 0;
-        return v4i{(int32_t)lo, (int32_t)(lo >> 32), (int32_t)hi, (int32_t)(hi >> 32)};
-    }
+    if (inner >= 16) return (v4i)shift_down(load16<1>(row + inner - 16), 8 * (k + 16 - inner));
     for (uint32_t i = 0; k + i < inner; ++i) {  // (a row of fewer than 16 bytes; k is 0)
         const uint32_t v = (uint32_t)(uint8_t)*gptr<int8_t>(row + k + i) << (8 * (i & 3));
         r[0] |= i / 4 == 0 ? v : 0;

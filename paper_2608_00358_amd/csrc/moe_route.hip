@@ -37,9 +37,15 @@ __device__ __forceinline__ void load_logits(const char* row, uint32_t e0, uint32
             for (int j = 0; j < 4; ++j) l[N - 4 + j] = widen1<DT>((r[j / 2] >> (16 * (j & 1))) & 0xffffu);
         }
     } else {
+        constexpr int V = kVecOf<DT>;
 #pragma unroll
-        for (int j = 0; j < N; ++j)
-            if (e0 + j < experts) l[j] = widen1<DT>(load1<ES>(row + (uint64_t)(e0 + j) * ES));
+        for (int q = 0; q < (N + V - 1) / V; ++q) {
+            float x[V];
+            widen<DT>(load_row<ES>(row, e0 + q * V, experts), x);
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (q * V + i < N && e0 + q * V + i < experts) l[q * V + i] = x[i];
+        }
     }
 #pragma unroll
     for (int j = 0; j < N; ++j) l[j] = fmaxf(l[j], -kInf);  // (the greater of NaN and -inf is -inf)
