@@ -28,6 +28,7 @@ struct RouteArgs {
     uint32_t experts, top_k;
     uint32_t groups, top_groups, group_top, group_size;
     uint32_t group_magic;  // ceil(2^20 / group_size): e / group_size = e * group_magic >> 20 for e < 1024
+    uint32_t group_lanes;  // lanes of a group where groups are whole lanes, else 0 (set by launch_route)
     uint32_t sigmoid, renormalize;
     uint32_t whole_sum;    // the softmax needs its sum over all experts
 };

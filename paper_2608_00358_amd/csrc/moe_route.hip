@@ -56,16 +56,13 @@ constexpr float kLog2e = 1.44269504088896340736f;
 // e^(l - m), m the greatest logit, as 2^((l - m) log2 e): the product's rounding makes the error |l - m| 2^-24
 // of the value, and the values that count are near m. (One fused product l log2 e - m log2 e would be off by
 // m 2^-24, which is anything where all logits are a mask's -1e9.) Logits of +inf share the weight among
-// themselves: they count as 0 and all others as -inf.
+// themselves: inf - inf is NaN, and the lesser of NaN and 0 is 0. Without any logit (m = -inf) all are 0.
 struct Exponential {
     float top;
-    bool infinite;
-    __device__ __forceinline__ explicit Exponential(float m) : top(m > -kInf && m < kInf ? m : 0.0f), infinite(m == kInf) {}
-    __device__ __forceinline__ float operator()(float l) const {
-        if (infinite) l = l == kInf ? 0.0f : -kInf;
-        return __builtin_amdgcn_exp2f((l - top) * kLog2e);
-    }
+    __device__ __forceinline__ explicit Exponential(float m) : top(m > -kInf ? m : 0.0f) {}
+    __device__ __forceinline__ float operator()(float l) const { return __builtin_amdgcn_exp2f(fminf(l - top, 0.0f) * kLog2e); }
 };
+// (0 at -inf)
 __device__ __forceinline__ float sigmoid(float l) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-l * kLog2e)); }
 
 // A 16-bit float widened to 32 bits has its 13 lowest bits free: the order of the float as an unsigned
@@ -91,6 +88,13 @@ __global__ __launch_bounds__(kRouteThreads) void hccl_moe_route_kernel(RouteArgs
     const bool on = t < a.tokens;
     const char* row = (const char*)a.logits + t * a.ld * ES;
     const uint32_t e0 = sub * N;
+    float bias[PACK ? 1 : N] = {};
+    if constexpr (!PACK) {
+        if (a.bias) {  // (on their way together with the logits; no branch for each)
+#pragma unroll
+            for (int j = 0; j < N; ++j) bias[j] = a.bias[e0 + j < a.experts ? e0 + j : 0];
+        }
+    }
     float l[N];
     load_logits<DT, N>(row, e0, a.experts, on, l);
 
@@ -109,7 +113,7 @@ __global__ __launch_bounds__(kRouteThreads) void hccl_moe_route_kernel(RouteArgs
         total = sum_lanes<L>(total);
         inv = total > 0.0f ? 1.0f / total : 0.0f;
     }
-    auto score = [&](float x) { return x == -kInf ? 0.0f : a.sigmoid ? sigmoid(x) : exponential(x) * inv; };
+    auto score = [&](float x) { return a.sigmoid ? sigmoid(x) : exponential(x) * inv; };
 
     uint32_t mine = ~0u;   // lane k keeps choice k
     float logit = -kInf;
@@ -133,14 +137,33 @@ __global__ __launch_bounds__(kRouteThreads) void hccl_moe_route_kernel(RouteArgs
             mine = logit > -kInf ? HCCL_MAX_EXPERTS - 1 - (mine & kFree) : ~0u;
         }
     } else {
+        // the chosen logits are looked up here at the end
+        __shared__ float logits[kRouteThreads * N];
+        float* own = logits + slot * (L * N);
         float c[N];
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             c[j] = l[j];
-            if (a.bias && l[j] > -kInf) {
-                const float v = score(l[j]) + a.bias[e0 + j];
-                c[j] = v > -kInf ? v : -kInf;
+            own[e0 + j] = l[j];
+        }
+        // Choice values: logits, or with a bias scores and bias. Groups are judged by them, or by scores.
+        float v[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = l[j];
+        if (a.bias || (GROUPED && a.group_top == 2)) {
+            if (a.sigmoid) {
+#pragma unroll
+                for (int j = 0; j < N; ++j) v[j] = sigmoid(l[j]) + bias[j];
+            } else {
+#pragma unroll
+                for (int j = 0; j < N; ++j) v[j] = exponential(l[j]) * inv + bias[j];
             }
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[j] = l[j] > -kInf ? fmaxf(v[j], -kInf) : -kInf;
+        }
+        if (a.bias) {
+#pragma unroll
+            for (int j = 0; j < N; ++j) c[j] = v[j];
         }
         if constexpr (GROUPED) {
             // lane g: the greatest one or two values of group g, of those that may be chosen. Where groups
@@ -148,30 +171,27 @@ __global__ __launch_bounds__(kRouteThreads) void hccl_moe_route_kernel(RouteArgs
             __shared__ float seen[kRouteThreads * N];
             float* part = seen + slot * (L * N);
             float one = -kInf, two = -kInf;
-            auto take = [&](float v) {
-                two = fmaxf(two, fminf(one, v));
-                one = fmaxf(one, v);
+            auto take = [&](float x) {
+                two = fmaxf(two, fminf(one, x));
+                one = fmaxf(one, x);
             };
-            uint32_t each = a.group_size;
-            if (each % N == 0) {
-                each = each / N * 2;
+            uint32_t each = a.group_size;  // values of a group in LDS
+            if (a.group_lanes) {
+                each = a.group_lanes * 2;
 #pragma unroll
-                for (int j = 0; j < N; ++j) take(a.group_top == 2 && !a.bias && l[j] > -kInf ? score(l[j]) : c[j]);
+                for (int j = 0; j < N; ++j) take(v[j]);
                 part[sub * 2] = one;
                 part[sub * 2 + 1] = two;
                 one = two = -kInf;
             } else {
 #pragma unroll
-                for (int j = 0; j < N; ++j) part[e0 + j] = a.group_top == 2 && !a.bias && l[j] > -kInf ? score(l[j]) : c[j];
+                for (int j = 0; j < N; ++j) part[e0 + j] = v[j];
             }
             __syncthreads();
             if (sub < a.groups) {
-                uint32_t i = sub % each;  // (lanes begin apart from each other: different banks)
+                const float* group = part + sub * each;
 #pragma unroll 4
-                for (uint32_t n = 0; n < each; ++n) {
-                    take(part[sub * each + i]);
-                    if (++i == each) i = 0;
-                }
+                for (uint32_t n = 0; n < each; ++n) take(group[n]);
             }
             float left = a.group_top == 2 && two > -kInf ? one + two : one;
             uint32_t kept = 0;
@@ -201,7 +221,8 @@ __global__ __launch_bounds__(kRouteThreads) void hccl_moe_route_kernel(RouteArgs
 #pragma unroll
             for (int j = 0; j < N; ++j) c[j] = e0 + j == e ? -kInf : c[j];
         }
-        if (on && mine != ~0u) logit = widen1<DT>(load1<ES>(row + (uint64_t)mine * ES));
+        __syncthreads();
+        if (mine != ~0u) logit = own[mine];
     }
 
     if (on && a.mask && !a.mask[t]) {
@@ -329,13 +350,14 @@ hipError_t by_lanes(uint32_t experts, uint32_t across, F f) {
 bool too_many(uint64_t tokens, uint32_t lanes) { return (tokens + kRouteThreads) * lanes > 0xffffffffull; }
 
 template <int DT>
-hipError_t route_type(const RouteArgs& a, hipStream_t s) {
+hipError_t route_type(RouteArgs a, hipStream_t s) {
     const bool grouped = a.top_groups < a.groups;
     return by_lanes(a.experts, a.top_k > a.groups ? a.top_k : a.groups, [&](auto shape) {
         constexpr int L = decltype(shape)::lanes, N = decltype(shape)::each;
         if (too_many(a.tokens, L)) return hipErrorInvalidConfiguration;
         const dim3 grid((uint32_t)((a.tokens + kRouteThreads / L - 1) / (kRouteThreads / L))), block(kRouteThreads);
         if (grouped) {
+            a.group_lanes = a.group_size % N ? 0 : a.group_size / N;
             hipLaunchKernelGGL((hccl_moe_route_kernel<DT, L, N, false, true>), grid, block, 0, s, a);
         } else if (DT != hcclFp32 && !a.bias) {
             hipLaunchKernelGGL((hccl_moe_route_kernel<DT, L, N, DT != hcclFp32, false>), grid, block, 0, s, a);
