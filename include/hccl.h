@@ -593,8 +593,8 @@ hcclResult_t hccl_moe_combine_backward(hcclComm_t comm, const void* grad, size_t
                                        size_t ldgz, float* grad_weight, void* stream);
 
 /*
- * Rows to 8-bit codes: codes[i, c] = the whole number nearest to v * (127 / m), ties to even, scale[i] =
- * m / 127, with m = max_c |v| (quotients and product in fp32). v = x[i, c], or with `gated`, where x
+ * Rows to 8-bit codes: codes[i, c] = the whole number nearest to v * (1 / m * 127), ties to even, scale[i] =
+ * m / 127, with m = max_c |v| (quotients and products in fp32, each rounded to nearest). v = x[i, c], or with `gated`, where x
  * has 2 * cols columns, silu(x[i, c]) * x[i, cols + c] (in fp32, not rounded in between). A row whose
  * m is below 2^-119 has codes and scale 0; one with an infinity or NaN has codes 0 and that as its
  * scale, so that every product with it is NaN. limit (int64, device) may be NULL: only the first

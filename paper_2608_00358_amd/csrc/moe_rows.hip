@@ -176,7 +176,7 @@ __global__ __launch_bounds__(kThreads) void hccl_moe_dispatch_kernel(DispatchArg
 }
 
 // -------------------------------------------------------------------------------------- quantize
-// code = rint(x * (127 / max|x|)), scale = max|x| / 127: the quotient once for a row. The maximum is
+// code = rint(x * (1 / max|x| * 127)), scale = max|x| / 127: the reciprocal once for a row. The maximum is
 // taken of the values' bits without their sign, which orders infinities and NaN above the rest: such
 // a row gets codes of 0 and that scale, so that its products are NaN. Rows below 2^-119 count as 0
 // (127 over them would overflow).
@@ -184,7 +184,7 @@ __device__ __forceinline__ void row_scale(uint32_t top, float& inv, float& scale
     const float m = __uint_as_float(top);
     const bool none = top < 0x04000000u;  // 2^-119
     const bool finite = top < 0x7f800000u;
-    inv = none || !finite ? 0.0f : 127.0f / m;
+    inv = none || !finite ? 0.0f : 1.0f / m * 127.0f;
     scale = none ? 0.0f : finite ? m / 127.0f : m;
 }
 

@@ -139,7 +139,7 @@ def silu_gate(x):
 
 
 def quantize(x):
-    """Codes and scales of rows held in 32 bits; the quotients and the product are rounded to 32 bits."""
+    """Codes and scales of rows held in 32 bits; the reciprocal and the products are rounded to 32 bits."""
     x = x.astype(np.float32)
     codes, scale = np.zeros(x.shape, np.int8), np.zeros(x.shape[0], np.float32)
     for i in range(x.shape[0]):
@@ -147,7 +147,7 @@ def quantize(x):
         if not np.isfinite(m):
             scale[i] = m
         elif m >= np.float32(2.0 ** -119):
-            codes[i] = np.rint(x[i] * (np.float32(127) / m)).astype(np.int8)
+            codes[i] = np.rint(x[i] * (np.float32(1) / m * np.float32(127))).astype(np.int8)
             scale[i] = m / np.float32(127)
     return codes, scale
 
