@@ -4,6 +4,10 @@ Serving quantises rows and weights twice to 8 bits with a scale of max / 127: an
 a step, max / 254, of a row whose values are about max / 3.5 in size (normal, 512 of them): 0.8 % of a value in
 the mean square (step / sqrt(12)), for each of four operands, adding up in squares to 1.6 %; the gate passes
 errors on from both factors: 3 % bounds it. Training runs in 32 bits: sums of 64 to 200 terms, 1e-5.
+
+This file comes after those of the resident executor: matrix products of torch make streams that live on,
+and with some numbers of live streams the runtime gives the executor's stream the hardware queue of the
+default stream, whose work then waits until the executor has been idle for its limit.
 """
 import importlib.util
 import os
