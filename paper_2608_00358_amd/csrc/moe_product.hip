@@ -290,7 +290,7 @@ __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_many_kernel(Pro
         if (DIRECT && (inner.value || s < whole)) {
             __builtin_amdgcn_global_load_lds((const HCCL_AS1 void*)(src[i] + (uint64_t)s * kStep), (lds_ptr)slot(s, i), 16, 0, 0);
         } else if (inner.value || s < steps) {
-            const v4u v = inner.value ? load16<1>(src[i] + (uint64_t)s * kStep) : (v4u)load_k(src[i] - chunk, s * kStep + chunk, a.inner);
+            const v4u v = inner.value || s < whole ? load16<1>(src[i] + (uint64_t)s * kStep) : (v4u)load_k(src[i] - chunk, s * kStep + chunk, a.inner);
             if constexpr (DIRECT) *(v4u*)(slot(s, i) + lane * 16) = v;
             else held[parity][i] = v;
         }
@@ -454,10 +454,16 @@ __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_many_kernel(Pro
     }
 }
 
+// Tiles that rows in segments can make at most: a segment adds a part of one, and each has a row.
+uint64_t most_tiles(const ProductArgs& a, uint64_t bm) {
+    const uint64_t n = (a.rows + bm - 1) / bm + (a.offsets ? a.segments : 0);
+    return n < a.rows ? n : a.rows;
+}
+
 template <int DT, int BM, int BN, int WM, int WN>
 hipError_t launch_many(const ProductArgs& a, hipStream_t s) {
     const uint32_t nblocks = (a.cols + BN - 1) / BN, threads = WM * WN * 64;
-    const uint64_t blocks = ((a.rows + BM - 1) / BM + (a.offsets ? a.segments : 0)) * nblocks;
+    const uint64_t blocks = most_tiles(a, BM) * nblocks;
     if (blocks + 8 > 0xffffffffull / threads) return hipErrorInvalidConfiguration;
     const dim3 grid((uint32_t)((blocks + 7) / 8 * 8));
     const bool direct = ((uintptr_t)a.a | (uintptr_t)a.b | a.lda | a.ldb) % 16 == 0;
@@ -468,7 +474,7 @@ hipError_t launch_many(const ProductArgs& a, hipStream_t s) {
 
 template <int DT, int MB, int NB, int W, int U>
 hipError_t launch_few(const ProductArgs& a, hipStream_t s) {
-    const uint64_t nblocks = (a.cols + 16 * NB - 1) / (16 * NB), tiles = (a.rows + 16 * MB - 1) / (16 * MB) + (a.offsets ? a.segments : 0);
+    const uint64_t nblocks = (a.cols + 16 * NB - 1) / (16 * NB), tiles = most_tiles(a, 16 * MB);
     if (tiles * nblocks > 0xffffffffull / (W * 64)) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL((hccl_moe_product_few_kernel<DT, MB, NB, W, U>), dim3((uint32_t)(tiles * nblocks)), dim3(W * 64), 0, s, a, (uint32_t)nblocks);
     return hipGetLastError();
@@ -504,11 +510,13 @@ hipError_t product_type(const ProductArgs& a, int cus, hipStream_t s) {
         const uint64_t tiles = a.offsets ? a.rows / 16 + spread : 1, cols16 = (a.cols + 15) / 16;
         if (tiles * (cols16 / 4) >= (uint64_t)cus) return launch_few<DT, 1, 4, 4, 2>(a, s);
         if (tiles * (cols16 / 2) >= (uint64_t)cus) return launch_few<DT, 1, 2, 4, 4>(a, s);
+        if (a.inner <= 1024) return launch_few<DT, 1, 1, 4, 2>(a, s);
         return launch_few<DT, 1, 1, 16, 2>(a, s);
     }
     const uint64_t tiles = a.offsets ? a.rows / 32 + spread : (a.rows + 31) / 32, cols16 = (a.cols + 15) / 16;
     if (tiles * (cols16 / 4) >= (uint64_t)cus) return launch_few<DT, 2, 4, 4, 2>(a, s);
     if (tiles * (cols16 / 2) >= (uint64_t)cus) return launch_few<DT, 2, 2, 8, 2>(a, s);
+    if (a.inner <= 1024) return launch_few<DT, 2, 1, 4, 2>(a, s);
     return launch_few<DT, 2, 1, 16, 2>(a, s);
 }
 
