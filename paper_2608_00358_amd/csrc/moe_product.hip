@@ -28,57 +28,62 @@ __device__ __forceinline__ void segment(const ProductArgs& a, uint32_t s, uint64
     end = hi < (int64_t)first ? first : (uint64_t)hi < a.rows ? (uint64_t)hi : a.rows;
 }
 
-// Tiles of BM rows that the segments have.
+// 64 segments, one a lane: their rows, their tiles of BM rows and the running sum of those.
 template <uint32_t BM>
-__device__ __forceinline__ uint32_t count_tiles(const ProductArgs& a) {
-    if (!a.offsets) return (uint32_t)((a.rows + BM - 1) / BM);
-    const uint32_t lane = threadIdx.x & 63;
-    uint32_t n = 0;
-    for (uint32_t s = lane; s < a.segments; s += kWave) {
-        uint64_t first, end;
-        segment(a, s, first, end);
-        n += (uint32_t)((end - first + BM - 1) / BM);
-    }
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) n += (uint32_t)__shfl_xor((int)n, d);
-    return first_lane(n);
-}
-
-// Rows [first, end) of tile `tile`, and its expert; false where there are fewer tiles. One lane a segment:
-// the tiles in it, their running sum, and the segment that holds the tile.
-template <uint32_t BM>
-__device__ __forceinline__ bool find_rows(const ProductArgs& a, uint32_t tile, Rows& out) {
-    if (!a.offsets) {
-        out.first = (uint64_t)tile * BM;
-        out.end = a.rows;
-        out.expert = 0;
-        return out.first < a.rows;
-    }
-    const uint32_t lane = threadIdx.x & 63;
-    uint32_t left = tile;
-    for (uint32_t s0 = 0; s0 < a.segments; s0 += kWave) {
-        const uint32_t s = s0 + lane;
-        uint64_t first = 0, end = 0;
+struct Segments {
+    uint64_t first, end;
+    uint32_t n, incl, all;
+    __device__ __forceinline__ Segments(const ProductArgs& a, uint32_t s0) {
+        const uint32_t lane = threadIdx.x & 63, s = s0 + lane;
+        first = end = 0;
+        if (!a.offsets) {  // one segment, which find_rows does not look for
+            all = (uint32_t)((a.rows + BM - 1) / BM);
+            return;
+        }
         if (s < a.segments) segment(a, s, first, end);
-        const uint32_t n = (uint32_t)((end - first + BM - 1) / BM);
-        uint32_t incl = n;
+        n = (uint32_t)((end - first + BM - 1) / BM);
+        incl = n;
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
             const uint32_t v = (uint32_t)__shfl_up((int)incl, d);
             if (lane >= (uint32_t)d) incl += v;
         }
-        const uint32_t all = at_lane(incl, 63);
-        if (left < all) {
-            const uint32_t l = first_lane((uint32_t)__popcll(__ballot(incl <= left)));
-            const uint32_t skip = left - (at_lane(incl, l) - at_lane(n, l));
-            out.first = ((uint64_t)at_lane((uint32_t)(first >> 32), l) << 32 | at_lane((uint32_t)first, l)) + (uint64_t)skip * BM;
-            out.end = (uint64_t)at_lane((uint32_t)(end >> 32), l) << 32 | at_lane((uint32_t)end, l);
+        all = at_lane(incl, 63);
+    }
+};
+
+// Tiles that the segments have; `s` holds the first 64 of them.
+template <uint32_t BM>
+__device__ __forceinline__ uint32_t count_tiles(const ProductArgs& a, const Segments<BM>& s) {
+    uint32_t n = s.all;
+    for (uint32_t s0 = kWave; s0 < a.segments; s0 += kWave) n += Segments<BM>(a, s0).all;
+    return n;
+}
+
+// Rows [first, end) of tile `tile`, and its expert; false where there are fewer tiles.
+template <uint32_t BM>
+__device__ __forceinline__ bool find_rows(const ProductArgs& a, Segments<BM> s, uint32_t tile, Rows& out) {
+    if (!a.offsets) {
+        out.first = (uint64_t)tile * BM;
+        out.end = a.rows;
+        out.expert = 0;
+        return tile < s.all;
+    }
+    uint32_t left = tile;
+    for (uint32_t s0 = 0;;) {
+        if (left < s.all) {
+            const uint32_t l = first_lane((uint32_t)__popcll(__ballot(s.incl <= left)));
+            const uint32_t skip = left - (at_lane(s.incl, l) - at_lane(s.n, l));
+            out.first = ((uint64_t)at_lane((uint32_t)(s.first >> 32), l) << 32 | at_lane((uint32_t)s.first, l)) + (uint64_t)skip * BM;
+            out.end = (uint64_t)at_lane((uint32_t)(s.end >> 32), l) << 32 | at_lane((uint32_t)s.end, l);
             out.expert = (s0 + l) % a.experts;
             return true;
         }
-        left -= all;
+        left -= s.all;
+        s0 += kWave;
+        if (s0 >= a.segments) return false;
+        s = Segments<BM>(a, s0);
     }
-    return false;
 }
 
 // 16 bytes of a row at k; bytes from `inner` on are zero: the row's last 16 bytes, shifted down.
@@ -130,7 +135,7 @@ __global__ __launch_bounds__(W * 64) void hccl_moe_product_few_kernel(ProductArg
     const uint32_t lane = threadIdx.x & 63, w = first_lane(threadIdx.x >> 6);
     const uint32_t tile = blockIdx.x / nblocks, n0 = blockIdx.x % nblocks * BN;
     Rows rows;
-    if (!find_rows<BM>(a, tile, rows)) return;
+    if (!find_rows<BM>(a, Segments<BM>(a, 0), tile, rows)) return;
     const uint32_t i = lane & 15, q = lane >> 4;
     const int8_t* pa[MB];
     const int8_t* pb[NB];
@@ -241,9 +246,10 @@ __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_many_kernel(Pro
     // that the tiles it works on at a time share their rows and weights in its L2. (Ends of segments, which are
     // less work, in a turn of their own after the whole tiles read the weights twice: 346 us against 337 for
     // 16 384 rows through 16 experts.)
+    const Segments<BM> segments(a, 0);
     uint32_t tile, nb;
     {
-        const uint32_t tiles = count_tiles<BM>(a);
+        const uint32_t tiles = count_tiles<BM>(a, segments);
         const uint64_t all = (uint64_t)tiles * nblocks, share = (all + 7) / 8;
         const uint64_t id = (blockIdx.x & 7) * share + blockIdx.x / 8;
         if (blockIdx.x / 8 >= share || id >= all) return;
@@ -254,7 +260,7 @@ __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_many_kernel(Pro
         nb = (id < banded ? (uint32_t)(id / ((uint64_t)kBand * tiles)) * kBand : nblocks / kBand * kBand) + (uint32_t)(at % width);
     }
     Rows rows;
-    if (!find_rows<BM>(a, tile, rows)) return;
+    if (!find_rows<BM>(a, segments, tile, rows)) return;
     const uint32_t n0 = nb * BN;
 
     // where this lane's part of each load comes from, and where in a buffer each load goes
