@@ -205,7 +205,7 @@ __global__ __launch_bounds__(W * 64) void hccl_moe_product_few_kernel(ProductArg
 
 // Many rows a segment: BM rows by BN columns a block, in WM x WN waves, k in steps of 64 through four
 // LDS buffers: one is multiplied while the next three are filled, by loads that go to LDS directly
-// (DIRECT: both operands' rows are 16-byte aligned) or through registers (any alignment, and the
+// (DIRECT: 1 for rows, 2 for weights that are 16-byte aligned) or through registers (any alignment, and the
 // last step of an inner size that is no multiple of 64, where bytes past the end are zero).
 //
 // LDS holds a row's 64 bytes as 4 chunks of 16; chunk c of row r lies in slot c ^ (r / 4 & 3), so that the
@@ -233,7 +233,7 @@ __device__ __forceinline__ void meet() {
     asm volatile("" ::: "memory");
 }
 
-template <int DT, int BM, int BN, int WM, int WN, bool DIRECT>
+template <int DT, int BM, int BN, int WM, int WN, int DIRECT>
 __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_many_kernel(ProductArgs a, uint32_t nblocks) {
     constexpr int W = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
     constexpr int LA = BM / 16 / W, LB = BN / 16 / W, LN = LA + LB;  // loads a wave makes for a step: 16 rows each
@@ -290,14 +290,16 @@ __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_many_kernel(Pro
     // Waves of the same rows are neighbours, and so on different SIMDs: where an end of a segment leaves
     // waves without rows, those that have some share out the matrix units.
     const uint32_t wm = w / WN, wn = w % WN;
-    v4u held[2][DIRECT ? 1 : LN];  // on their way through registers: steps of either parity
+    constexpr bool kAll = DIRECT == 3;
+    auto direct = [](int i) { return (DIRECT & (i < LA ? 1 : 2)) != 0; };
+    v4u held[2][LN];  // on their way through registers: steps of either parity
     // Load i of those that bring in step s. INNER: it and the steps before it are whole.
     auto fetch = [&](uint32_t s, int parity, auto inner, int i) {
-        if (DIRECT && (inner.value || s < whole)) {
+        if (direct(i) && (inner.value || s < whole)) {
             __builtin_amdgcn_global_load_lds((const HCCL_AS1 void*)(src[i] + (uint64_t)s * kStep), (lds_ptr)slot(s, i), 16, 0, 0);
         } else if (inner.value || s < steps) {
             const v4u v = inner.value || s < whole ? load16<1>(src[i] + (uint64_t)s * kStep) : (v4u)load_k(src[i] - chunk, s * kStep + chunk, a.inner);
-            if constexpr (DIRECT) *(v4u*)(slot(s, i) + lane * 16) = v;
+            if (direct(i)) *(v4u*)(slot(s, i) + lane * 16) = v;
             else held[parity][i] = v;
         }
     };
@@ -306,10 +308,9 @@ __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_many_kernel(Pro
         for (int i = 0; i < LN; ++i) fetch(s, parity, inner, i);
     };
     auto put = [&](uint32_t s, int parity) {  // what registers hold of step s goes to its buffer
-        if constexpr (!DIRECT) {
 #pragma unroll
-            for (int i = 0; i < LN; ++i) *(v4u*)(slot(s, i) + lane * 16) = held[parity][i];
-        }
+        for (int i = 0; i < LN; ++i)
+            if (!direct(i)) *(v4u*)(slot(s, i) + lane * 16) = held[parity][i];
     };
     v4i va[2][TM], vb[2][TN];
     auto read = [&](uint32_t s, uint32_t part, int i) {  // fragment i of a part, in the order of their use
@@ -339,19 +340,23 @@ __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_many_kernel(Pro
     };
     // reads end two instructions before the part does, so that they are there when the next one begins
     constexpr int kReadSlots = kMfmas >= 8 ? kMfmas - kFirst - 2 : kMfmas >= 4 ? 2 : 1;
+    // Step s + 1 has landed for all waves, and all have read step s, whose buffer step s + 4 takes. Loads of
+    // the steps s + 2 and s + 3 stay on their way (where all are direct loads; where some pass through registers,
+    // step s + 2 is needed there, and only those of step s + 3 do).
+    auto land = [&](uint32_t s, int parity, auto inner) {
+        if (inner.value || s + 2 < steps) put(s + 2, parity);
+        if (DIRECT == 0) __builtin_amdgcn_s_waitcnt(0xc07f);  // LDS alone
+        else if (inner.value || s + 3 < whole) wait_loads<kAll ? 2 * LN : LN>();
+        else wait_loads<0>();
+        meet();
+    };
     auto step = [&](uint32_t s, int parity, auto inner) {
         multiply(0, 0, kMfmas, [&](int i) {
             spread(i, kFirst - 1, kReadSlots, kReads, [&](int r) { read(s, 1, r); });
             spread(i, kFirst - 1, kMfmas - kFirst + 1, LN, [&](int r) { fetch(s + 3, parity ^ 1, inner, r); });
         });
         multiply(1, 0, kFirst, [](int) {});
-        // Step s + 1 has landed for all waves, and all have read step s, whose buffer step s + 4 takes. Loads of
-        // the steps s + 2 and s + 3 stay on their way (where both are direct loads).
-        if (inner.value || s + 2 < steps) put(s + 2, parity);
-        if (!DIRECT) __builtin_amdgcn_s_waitcnt(0xc07f);  // LDS alone
-        else if (inner.value || s + 3 < whole) wait_loads<2 * LN>();
-        else wait_loads<0>();
-        meet();
+        land(s, parity, inner);
         const bool more = inner.value || s + 1 < steps;
         multiply(1, kFirst, kMfmas, [&](int i) {
             if (more) spread(i, kFirst, kReadSlots, kReads, [&](int r) { read(s + 1, 0, r); });
@@ -359,11 +364,7 @@ __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_many_kernel(Pro
     };
     auto idle = [&](uint32_t s, int parity, auto inner) {  // a step of a wave without rows: brings in its part for the others
         fetch_all(s + 3, parity ^ 1, inner);
-        if (inner.value || s + 2 < steps) put(s + 2, parity);
-        if (!DIRECT) __builtin_amdgcn_s_waitcnt(0xc07f);
-        else if (inner.value || s + 3 < whole) wait_loads<2 * LN>();
-        else wait_loads<0>();
-        meet();
+        land(s, parity, inner);
     };
     auto walk = [&](auto each) {
         uint32_t s = 0;
@@ -379,16 +380,11 @@ __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_many_kernel(Pro
     };
     if (steps) {
         const std::false_type any;
-        if constexpr (DIRECT) {
-#pragma unroll
-            for (uint32_t s = 0; s < kBuffers - 1; ++s) fetch_all(s, 0, any);
-        } else {
-            fetch_all(0, 0, any), fetch_all(1, 1, any);
-            put(0, 0);
-            if (steps > 1) put(1, 1);
-            fetch_all(2, 0, any);
-        }
-        if (DIRECT && whole >= kBuffers - 1) wait_loads<2 * LN>();
+        fetch_all(0, 0, any), fetch_all(1, 1, any);
+        put(0, 0);
+        if (steps > 1) put(1, 1);
+        fetch_all(2, 0, any);
+        if (kAll && whole >= kBuffers - 1) wait_loads<2 * LN>();
         else wait_loads<0>();
         meet();
         if (rows.first + wm * TM * 32 >= rows.end) {
@@ -472,9 +468,11 @@ hipError_t launch_many(const ProductArgs& a, hipStream_t s) {
     const uint64_t blocks = most_tiles(a, BM) * nblocks;
     if (blocks + 8 > 0xffffffffull / threads) return hipErrorInvalidConfiguration;
     const dim3 grid((uint32_t)((blocks + 7) / 8 * 8));
-    const bool direct = ((uintptr_t)a.a | (uintptr_t)a.b | a.lda | a.ldb) % 16 == 0;
-    if (direct) hipLaunchKernelGGL((hccl_moe_product_many_kernel<DT, BM, BN, WM, WN, true>), grid, dim3(threads), 0, s, a, nblocks);
-    else hipLaunchKernelGGL((hccl_moe_product_many_kernel<DT, BM, BN, WM, WN, false>), grid, dim3(threads), 0, s, a, nblocks);
+    const int direct = (((uintptr_t)a.a | a.lda) % 16 == 0 ? 1 : 0) | (((uintptr_t)a.b | a.ldb) % 16 == 0 ? 2 : 0);
+    if (direct == 3) hipLaunchKernelGGL((hccl_moe_product_many_kernel<DT, BM, BN, WM, WN, 3>), grid, dim3(threads), 0, s, a, nblocks);
+    else if (direct == 2) hipLaunchKernelGGL((hccl_moe_product_many_kernel<DT, BM, BN, WM, WN, 2>), grid, dim3(threads), 0, s, a, nblocks);
+    else if (direct == 1) hipLaunchKernelGGL((hccl_moe_product_many_kernel<DT, BM, BN, WM, WN, 1>), grid, dim3(threads), 0, s, a, nblocks);
+    else hipLaunchKernelGGL((hccl_moe_product_many_kernel<DT, BM, BN, WM, WN, 0>), grid, dim3(threads), 0, s, a, nblocks);
     return hipGetLastError();
 }
 
