@@ -373,7 +373,8 @@ def _list(t, n, dtype, what):
     """Address of a packed tensor of n elements of the named type (None stays None)."""
     if t is None:
         return None
-    if t.numel() != n or not t.is_contiguous() or str(t.dtype) != "torch." + dtype:
+    kind = str(t.dtype)[6:]  # "torch." before it; a mask may be bool
+    if t.numel() != n or not t.is_contiguous() or (kind != dtype and (dtype, kind) != ("uint8", "bool")):
         raise ValueError(f"{what} must be {n} packed {dtype} elements, not {tuple(t.shape)} {t.dtype}")
     return t.data_ptr()
 

@@ -53,6 +53,7 @@ def test_good_calls_pass_the_checks_on_a_communicator_without_a_device(comm):
     logits, index, weight, x = torch.zeros(T, E), _i32(T, K), torch.zeros(T, K), torch.zeros(T, C)
     row, offsets, out = _i32(T, K), torch.zeros(E + 1, dtype=torch.int64), torch.zeros(T * K, C)
     comm.moe_route(r, logits, index, weight, bias=torch.zeros(E), mask=torch.ones(T, dtype=torch.uint8))
+    comm.moe_route(r, logits, index, weight, mask=torch.ones(T, dtype=torch.bool))
     comm.moe_route_backward(r, logits, index, weight, torch.zeros_like(logits))
     comm.moe_plan(index, E, row, offsets, T * K, rank_counts=torch.zeros(4, dtype=torch.int64))
     comm.moe_dispatch(x, row, out)

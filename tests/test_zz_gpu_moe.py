@@ -165,6 +165,23 @@ def test_route_of_any_number_of_tokens(comm, tokens, experts):
     check_route(comm, dict(experts=experts, top_k=5, renormalize=True), rand(rng, tokens, experts, "bf16"))
 
 
+@pytest.mark.parametrize("dt,low", [("bf16", -1e9), ("fp32", -1e9), ("fp32", -1e30), ("fp16", -6e4)])
+@pytest.mark.parametrize("cfg", [dict(experts=128, top_k=8), dict(experts=128, top_k=8, renormalize=True), dict(experts=200, top_k=4, score="sigmoid"),
+                                 dict(experts=64, top_k=4, bias=True), dict(experts=64, top_k=4, groups=8, top_groups=2, renormalize=True)],
+                         ids=lambda c: "-".join(str(v) for v in c.values()))
+def test_route_of_finite_masks(comm, cfg, dt, low):
+    """Masks by a great negative number: rows with some experts left, with one, and with none but masked ones."""
+    rng = np.random.default_rng(3)
+    logits = rand(rng, 30, cfg["experts"], dt)
+    logits[:10, ::2] = low
+    logits[10:20, 1:] = low
+    logits[20:] = low
+    if cfg.get("bias"):
+        logits[10:] = logits[:1]  # (equal scores of 0 and a bias leave nothing to choose by but the bias)
+        logits[10:, 1:] = low
+    check_route(comm, cfg, logits, dt=dt)
+
+
 @pytest.mark.parametrize("dt", ["bf16", "fp16", "fp32"])
 def test_route_ties_go_to_the_lowest_expert(comm, dt):
     rng = np.random.default_rng(0)
@@ -455,6 +472,31 @@ def test_product_sums_are_whole(comm):
     out = torch.empty(3, 5, device=DEV)
     comm.moe_product(a, torch.ones(3, device=DEV), w, torch.ones(1, 5, device=DEV), out)
     assert out[0].tolist() == [float(np.float32(n * 16384))] * 5 and out[1].tolist() == [float(np.float32(-n * 127 * 128))] * 5
+
+
+def test_nothing_to_do(comm):
+    """No tokens, rows or columns: nothing is read, and what is left to write is."""
+    i32, f32, i8 = (dict(dtype=t, device=DEV) for t in (torch.int32, torch.float32, torch.int8))
+    r = H.hccl_router_init(experts=8, top_k=2)
+    none = torch.empty(0, 8, **f32)
+    comm.moe_route(r, none, torch.empty(0, 2, **i32), torch.empty(0, 2, **f32))
+    comm.moe_route_backward(r, none, torch.empty(0, 2, **i32), torch.empty(0, 2, **f32), none)
+    comm.moe_dispatch(none, torch.empty(0, 2, **i32), torch.empty(4, 8, **f32))
+    comm.moe_dispatch(torch.ones(3, 8, **f32), torch.zeros(3, 2, **i32), none)
+    out = torch.full((3, 8), 77.0, device=DEV)
+    comm.moe_combine(none, torch.zeros(3, 2, **i32), out)  # rows that there are none of
+    assert bool((out == 0).all())
+    gw = torch.full((3, 2), 77.0, device=DEV)
+    comm.moe_combine_backward(torch.empty(3, 0, **f32), torch.empty(6, 0, **f32), torch.arange(6, **i32).view(3, 2), torch.ones(3, 2, **f32),
+                              torch.empty(6, 0, **f32), gw)
+    assert bool((gw == 0).all())
+    comm.moe_quantize(none, torch.empty(0, 8, **i8), torch.empty(0, **f32))
+    scale = torch.full((3,), 77.0, device=DEV)
+    comm.moe_quantize(torch.empty(3, 0, **f32), torch.empty(3, 0, **i8), scale)
+    assert bool((scale == 0).all())
+    comm.moe_product(torch.empty(0, 8, **i8), torch.empty(0, **f32), torch.zeros(2, 4, 8, **i8), torch.ones(2, 4, **f32), torch.empty(0, 4, **f32),
+                     offsets=torch.zeros(3, dtype=torch.int64, device=DEV))
+    torch.cuda.synchronize()
 
 
 # ------------------------------------------------------------------- offsets, streams, graphs, order
