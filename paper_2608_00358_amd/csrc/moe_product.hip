@@ -6,6 +6,11 @@
 //
 // The weights are the instruction's first operand: a lane then holds neighbouring columns of one row.
 // The order of k within an instruction does not matter as long as both operands have the same.
+//
+// Bounds: with few rows a segment, the weights' bytes (256 rows over 64 experts of 2048 x 2048: 268 MB in 43 us,
+// 6.3 TB/s, the rate of a large copy); with many, power and the loads from L2 to LDS (8192 x 8192 x 8192 in
+// 475-490 us, 2.25-2.3 POPS, where a library product takes 518 us; in long products the matrix units alone, without
+// any load, bring the clock down to 1.9 GHz, and the whole kernel to 1.7).
 #include <type_traits>
 
 #include "moe_device.h"
@@ -485,20 +490,21 @@ hipError_t launch_few(const ProductArgs& a, hipStream_t s) {
 }
 
 // The largest tiles that leave at least 3/4 of the CUs a block and are not mostly empty: a tile is at most
-// twice as high as a segment has rows on average. us, in bf16 (rows x inner x columns x experts):
-//                            256 x 256   128 x 128   64 x 128   64 x 64    few rows
-//   16384 x 4096 x 4096 x 16    329          -          -         -           -
-//   12000 x 1024 x 1024 x 16     25         30         31        37           -
-//    2999 x 1408 x 2050 x 12     29         23         27        32           -
-//    2048 x 2048 x 2048 x 64     65         60         60        67          76
-//    1024 x 2048 x 2048 x 64     63         57         56         -          58
-//     512 x 2048 x 2048 x 64     62         55         52         -          49
-//    1024 x 4096 x 4096 x 1      50         24         33        43          87
-//     256 x 4096 x 4096 x 1      49         19         16        14          24
-//      64 x 4096 x 4096 x 1      32         17         15        13          10
+// twice as high as a segment has rows on average (4 times for 16 rows, where weights are all that counts). us, bf16:
+//   rows x inner x columns x experts   256 x 256   128 x 128   64 x 128   64 x 64   few rows
+//       16384 x 4096 x 4096 x 16           321         390        496        599      1379
+//       12000 x 1024 x 1024 x 16            23          29         31         36        84
+//        2999 x 1408 x 2050 x 12            25          22         25         29        65
+//        2048 x 2048 x 2048 x 64            65          61         61         68        76
+//        1024 x 2048 x 2048 x 64            61          55         55         60        58
+//         512 x 2048 x 2048 x 64            59          54         52         55        50
+//         256 x 2048 x 2048 x 64            57          52         49         52        46
+//        1024 x 4096 x 4096 x 1             42          24         31         41        87
+//         256 x 4096 x 4096 x 1             40          19         16         14        24
+//          64 x 4096 x 4096 x 1             30          17         15         13        10
 // Few rows: 32 a block from 9 rows a segment on (16 where one expert has no more), and of 64, 32 and 16 columns
 // the most that leave every CU a block, with k shared out over more waves the fewer columns there are
-// (1 x 4096 x 4096: 16 columns 5.4 us, 32 columns 6.7 us, 64 columns 10.5 us; 256 x 2048 x 2048 x 64: 74, 47, 47 us).
+// (1 x 4096 x 4096: 16 columns 5.4 us, 32 columns 7.0, 64 columns 10.5; 256 x 2048 x 2048 x 64: 80, 48 and 46 us).
 template <int DT>
 hipError_t product_type(const ProductArgs& a, int cus, hipStream_t s) {
     const uint64_t each = a.rows / a.segments, spread = a.offsets ? (a.rows < a.segments ? a.rows : a.segments) : 0;
@@ -514,13 +520,11 @@ hipError_t product_type(const ProductArgs& a, int cus, hipStream_t s) {
         const uint64_t tiles = a.offsets ? a.rows / 16 + spread : 1, cols16 = (a.cols + 15) / 16;
         if (tiles * (cols16 / 4) >= (uint64_t)cus) return launch_few<DT, 1, 4, 4, 2>(a, s);
         if (tiles * (cols16 / 2) >= (uint64_t)cus) return launch_few<DT, 1, 2, 4, 4>(a, s);
-        if (a.inner <= 1024) return launch_few<DT, 1, 1, 4, 2>(a, s);
         return launch_few<DT, 1, 1, 16, 2>(a, s);
     }
     const uint64_t tiles = a.offsets ? a.rows / 32 + spread : (a.rows + 31) / 32, cols16 = (a.cols + 15) / 16;
     if (tiles * (cols16 / 4) >= (uint64_t)cus) return launch_few<DT, 2, 4, 4, 2>(a, s);
     if (tiles * (cols16 / 2) >= (uint64_t)cus) return launch_few<DT, 2, 2, 8, 2>(a, s);
-    if (a.inner <= 1024) return launch_few<DT, 2, 1, 4, 2>(a, s);
     return launch_few<DT, 2, 1, 16, 2>(a, s);
 }
 

@@ -14,7 +14,8 @@ constexpr int kThreads = 256, kWaves = kThreads / 64;
 // the first kernel counts every block's routes per expert, and in the second a block adds up the
 // counts before its own and ranks its routes among themselves: wave by wave, a lane's peers (equal
 // expert) are found by one ballot for each bit of the expert's number. Only sums of whole numbers
-// are taken in no fixed order.
+// are taken in no fixed order. Bound by launches and latency: 148 routes over 64 experts 4.2 us in one
+// launch, 32 768 routes (0.26 MB) 3.7 + 4.7 us in two.
 
 __global__ __launch_bounds__(kPlanThreads) void hccl_moe_count_kernel(PlanArgs a) {
     __shared__ uint32_t n[HCCL_MAX_EXPERTS];
@@ -313,7 +314,8 @@ __global__ __launch_bounds__(kThreads) void hccl_moe_quantize_kernel(QuantizeArg
 
 // --------------------------------------------------------------------------------------- combine
 // y_t = sum_k w_k z_{row k}, added up in 32 bits in the order of the slots. A wave takes a piece of a
-// token; the loads of kBatch rows are in flight together.
+// token; the loads of kBatch rows are in flight together. Bound by memory: 8 192 tokens x 4 rows of 2 048
+// bf16 (168 MB) 31 us, 5.4 TB/s; 256 tokens x 4 rows of 4 096 3.3 us, little more than an empty launch.
 constexpr int kBatch = 4;
 constexpr int kCombineVecs = 2;
 
@@ -369,6 +371,7 @@ __global__ __launch_bounds__(kThreads) void hccl_moe_combine_kernel(CombineArgs 
 // dz_{row k} = w_k dy_t, dw_k = <dy_t, z_{row k}>. A block of W waves takes a token, as many as its row
 // has vectors for, up to 4 (3 001 tokens x 2 rows of 1 003 fp16: 2 waves 9 us, 4 waves 12 us). The
 // products are added up in a lane, over the lanes and then over the waves, always in the same order.
+// Bound by memory: 8 192 tokens x 4 rows of 2 048 bf16 (302 MB) 52 us, 5.8 TB/s.
 template <int DT, bool WHOLE, bool STREAM>
 __device__ __forceinline__ void backward_piece(const CombineBackwardArgs& a, const char* dy, const uint32_t (&r)[kBatch], const float (&wk)[kBatch],
                                                uint64_t e, float (&dot)[kBatch]) {
