@@ -2,7 +2,8 @@
 
 The P ranks of a collective are P buffers in one GPU's HBM. The C library (libhccl.so,
 declared in include/hccl.h) lowers each collective into a descriptor program on the host
-and runs it with one persistent HIP executor kernel; this package is its ctypes binding.
+and runs it with one persistent HIP executor kernel; the operators of a mixture-of-experts layer
+around the exchange are HIP kernels of their own. This package is the library's ctypes binding.
 """
 from .hccl import (  # noqa: F401
     ALGOS, DTYPES, EXPORTS, LIB_PATH, MAX_RANKS, NO_DEVICE, OPS, SCORES, Comm, HcclError,
