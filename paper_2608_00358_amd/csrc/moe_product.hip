@@ -502,7 +502,9 @@ hipError_t launch_few(const ProductArgs& a, hipStream_t s) {
 //        1024 x 4096 x 4096 x 1             42          24         31         41        87
 //         256 x 4096 x 4096 x 1             40          19         16         14        24
 //          64 x 4096 x 4096 x 1             30          17         15         13        10
-// Few rows: 32 a block from 9 rows a segment on (16 where one expert has no more), and of 64, 32 and 16 columns
+//         128 x 4096 x 1024 x 1              -          18         15         13         8
+//         505 x 4672 x  185 x 1              -          27         19         14         7
+// Few rows, and blocks too few for half the CUs: 32 a block from 9 rows a segment on (16 where one expert has no more), and of 64, 32 and 16 columns
 // the most that leave every CU a block, with k shared out over more waves the fewer columns there are
 // (1 x 4096 x 4096: 16 columns 5.4 us, 32 columns 7.0, 64 columns 10.5; 256 x 2048 x 2048 x 64: 80, 48 and 46 us).
 template <int DT>
@@ -515,7 +517,7 @@ hipError_t product_type(const ProductArgs& a, int cus, hipStream_t s) {
     if (each >= 128 && blocks(256, 256) >= most) return launch_many<DT, 256, 256, 2, 4>(a, s);
     if (each >= 32 && blocks(128, 128) >= most) return launch_many<DT, 128, 128, 2, 2>(a, s);
     if (each >= 16 && blocks(64, 128) >= most) return launch_many<DT, 64, 128, 1, 4>(a, s);
-    if (each > 64) return launch_many<DT, 64, 64, 1, 2>(a, s);
+    if (each > 64 && blocks(64, 64) >= (uint64_t)cus / 2) return launch_many<DT, 64, 64, 1, 2>(a, s);
     if (a.offsets ? each <= 8 : a.rows <= 16) {
         const uint64_t tiles = a.offsets ? a.rows / 16 + spread : 1, cols16 = (a.cols + 15) / 16;
         if (tiles * (cols16 / 4) >= (uint64_t)cus) return launch_few<DT, 1, 4, 4, 2>(a, s);

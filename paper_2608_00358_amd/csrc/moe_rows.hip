@@ -176,6 +176,20 @@ __global__ __launch_bounds__(kThreads) void hccl_moe_dispatch_kernel(DispatchArg
     else dispatch_piece<ES, false, STREAM>(a, t, c0 + lane * V, mine);
 }
 
+// Rows of up to G vectors: a wave takes 64 / G tokens, G lanes each.
+template <int ES, int G>
+__global__ __launch_bounds__(kThreads) void hccl_moe_dispatch_narrow_kernel(DispatchArgs a) {
+    const uint64_t t = (uint64_t)blockIdx.x * (kThreads / G) + threadIdx.x / G, e = threadIdx.x % G * (16 / ES);
+    if (t >= a.tokens || e >= a.cols) return;
+    const v4u v = load_row<ES>((const char*)a.x + t * a.ldx * ES, e, a.cols);
+    const int32_t* row = a.row + t * a.top_k;
+#pragma unroll 4
+    for (uint32_t k = 0; k < a.top_k; ++k) {
+        const uint32_t r = (uint32_t)row[k];
+        if (r < a.capacity) store_row<ES>((char*)a.out + (uint64_t)r * a.ldo * ES, e, a.cols, v);
+    }
+}
+
 // -------------------------------------------------------------------------------------- quantize
 // code = rint(x * (1 / max|x| * 127)), scale = max|x| / 127: the reciprocal once for a row. The maximum is
 // taken of the values' bits without their sign, which orders infinities and NaN above the rest: such
@@ -368,6 +382,40 @@ __global__ __launch_bounds__(kThreads) void hccl_moe_combine_kernel(CombineArgs 
     else combine_piece<DT, false>(a, t, c0, lane);
 }
 
+// Rows of up to G vectors: a wave takes 64 / G tokens, G lanes each.
+template <int DT, int G>
+__global__ __launch_bounds__(kThreads) void hccl_moe_combine_narrow_kernel(CombineArgs a) {
+    constexpr int V = kVecOf<DT>, ES = kSize<DT>;
+    const uint64_t t = (uint64_t)blockIdx.x * (kThreads / G) + threadIdx.x / G, e = threadIdx.x % G * V;
+    if (t >= a.tokens || e >= a.cols) return;
+    const int32_t* row = a.row + t * a.top_k;
+    float acc[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) acc[i] = 0.0f;
+    for (uint32_t k = 0; k < a.top_k; k += kBatch) {
+        uint32_t r[kBatch];
+        float w[kBatch];
+        v4u z[kBatch];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            r[j] = k + j < a.top_k ? (uint32_t)row[k + j] : ~0u;
+            w[j] = a.weight && k + j < a.top_k ? a.weight[t * a.top_k + k + j] : 1.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+            if (r[j] < a.capacity) z[j] = load_row<ES>((const char*)a.z + (uint64_t)r[j] * a.ldz * ES, e, a.cols);
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            if (r[j] >= a.capacity) continue;
+            float x[V];
+            widen<DT>(z[j], x);
+#pragma unroll
+            for (int i = 0; i < V; ++i) acc[i] += w[j] * x[i];
+        }
+    }
+    store_row<ES>((char*)a.out + t * a.ldo * ES, e, a.cols, narrow<DT>(acc));
+}
+
 // dz_{row k} = w_k dy_t, dw_k = <dy_t, z_{row k}>. A block of W waves takes a token, as many as its row
 // has vectors for, up to 4 (3 001 tokens x 2 rows of 1 003 fp16: 2 waves 9 us, 4 waves 12 us). The
 // products are added up in a lane, over the lanes and then over the waves, always in the same order.
@@ -454,6 +502,64 @@ __global__ __launch_bounds__(W * 64) void hccl_moe_combine_backward_kernel(Combi
     }
 }
 
+// Rows of up to G vectors: a wave takes 64 / G tokens, G lanes each (all of them until the sums are made).
+template <int DT, int G>
+__global__ __launch_bounds__(kThreads) void hccl_moe_combine_backward_narrow_kernel(CombineBackwardArgs a) {
+    constexpr int V = kVecOf<DT>, ES = kSize<DT>;
+    const uint64_t t = (uint64_t)blockIdx.x * (kThreads / G) + threadIdx.x / G, e = threadIdx.x % G * V;
+    const bool on = t < a.tokens && e < a.cols;
+    const uint64_t route = t < a.tokens ? t * a.top_k : 0;
+    float x[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = 0.0f;
+    if (on) widen<DT>(load_row<ES>((const char*)a.grad + t * a.ldg * ES, e, a.cols), x);
+    for (uint32_t k = 0; k < a.top_k; k += kBatch) {
+        uint32_t r[kBatch];
+        float w[kBatch];
+        v4u z[kBatch];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            r[j] = k + j < a.top_k ? (uint32_t)a.row[route + k + j] : ~0u;
+            w[j] = k + j < a.top_k ? a.weight[route + k + j] : 0.0f;
+        }
+        if (a.grad_weight) {
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {
+                z[j] = v4u{0, 0, 0, 0};
+                if (on && r[j] < a.capacity) z[j] = load_row<ES>((const char*)a.z + (uint64_t)r[j] * a.ldz * ES, e, a.cols);
+            }
+        }
+        if (a.grad_z) {
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {
+                if (!on || r[j] >= a.capacity) continue;
+                float d[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) d[i] = w[j] * x[i];
+                store_row<ES>((char*)a.grad_z + (uint64_t)r[j] * a.ldo * ES, e, a.cols, narrow<DT>(d));
+            }
+        }
+        if (!a.grad_weight) continue;
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            float y[V], dot = 0.0f;
+            widen<DT>(z[j], y);
+#pragma unroll
+            for (int i = 0; i < V; ++i) dot += x[i] * y[i];
+            dot = sum_lanes<G>(dot);
+            if (t < a.tokens && threadIdx.x % G == 0 && k + j < a.top_k) a.grad_weight[route + k + j] = r[j] < a.capacity ? dot : 0.0f;
+        }
+    }
+}
+
+// Lanes for a token whose row has few vectors, 0 where a wave or more takes it: with one wave a token most of its
+// lanes would idle. us in bf16 (tokens x columns x rows a token), lanes / a wave: dispatch 12 691 x 64 x 6 4.4 / 6.6;
+// combine 15 168 x 128 x 8 7.8 / 24; gradients 12 213 x 256 x 6 15 / 21.
+int narrow_lanes(uint64_t cols, uint64_t es) {
+    const uint64_t vecs = (cols * es + 15) / 16;
+    return vecs <= 16 ? 16 : vecs <= 32 ? 32 : 0;
+}
+
 // A launch's threads are counted in 32 bits.
 bool too_many(uint64_t blocks, uint32_t threads) { return blocks * threads > 0xffffffffull; }
 
@@ -488,6 +594,15 @@ hipError_t launch_plan(const PlanArgs& a, hipStream_t s) {
 
 hipError_t launch_dispatch(const DispatchArgs& a, hcclDataType_t dt, hipStream_t s) {
     const uint32_t es = dt == hcclFp32 ? 4 : 2, per = kWave * 16 / es;
+    if (const int lanes = narrow_lanes(a.cols, es)) {
+        if (too_many(a.tokens / kThreads + 1, kThreads * lanes)) return hipErrorInvalidConfiguration;
+        const dim3 grid((uint32_t)((a.tokens * lanes + kThreads - 1) / kThreads)), block(kThreads);
+        if (es == 2 && lanes == 16) hipLaunchKernelGGL((hccl_moe_dispatch_narrow_kernel<2, 16>), grid, block, 0, s, a);
+        else if (es == 2) hipLaunchKernelGGL((hccl_moe_dispatch_narrow_kernel<2, 32>), grid, block, 0, s, a);
+        else if (lanes == 16) hipLaunchKernelGGL((hccl_moe_dispatch_narrow_kernel<4, 16>), grid, block, 0, s, a);
+        else hipLaunchKernelGGL((hccl_moe_dispatch_narrow_kernel<4, 32>), grid, block, 0, s, a);
+        return hipGetLastError();
+    }
     const uint32_t pieces = (uint32_t)((a.cols + per - 1) / per);
     const uint64_t blocks = (a.tokens * pieces + kWaves - 1) / kWaves;
     if (too_many(blocks, kThreads)) return hipErrorInvalidConfiguration;
@@ -526,6 +641,15 @@ hipError_t launch_quantize(const QuantizeArgs& a, hcclDataType_t dt, bool gated,
 }
 
 hipError_t launch_combine(const CombineArgs& a, hcclDataType_t dt, hipStream_t s) {
+    if (const int lanes = narrow_lanes(a.cols, dt == hcclFp32 ? 4 : 2)) {
+        if (too_many(a.tokens / kThreads + 1, kThreads * lanes)) return hipErrorInvalidConfiguration;
+        return by_type(dt, [&](auto type) {
+            constexpr int DT = decltype(type)::value;
+            const dim3 grid((uint32_t)((a.tokens * lanes + kThreads - 1) / kThreads)), block(kThreads);
+            if (lanes == 16) hipLaunchKernelGGL((hccl_moe_combine_narrow_kernel<DT, 16>), grid, block, 0, s, a);
+            else hipLaunchKernelGGL((hccl_moe_combine_narrow_kernel<DT, 32>), grid, block, 0, s, a);
+        });
+    }
     const uint32_t per = kCombineVecs * kWave * (dt == hcclFp32 ? 4 : 8), pieces = (uint32_t)((a.cols + per - 1) / per);
     const uint64_t blocks = (a.tokens * pieces + kWaves - 1) / kWaves;
     if (too_many(blocks, kThreads)) return hipErrorInvalidConfiguration;
@@ -537,15 +661,20 @@ hipError_t launch_combine(const CombineArgs& a, hcclDataType_t dt, hipStream_t s
 }
 
 hipError_t launch_combine_backward(const CombineBackwardArgs& a, hcclDataType_t dt, hipStream_t s) {
-    if (too_many(a.tokens, 256)) return hipErrorInvalidConfiguration;
+    if (too_many(a.tokens, 1024)) return hipErrorInvalidConfiguration;
     const uint64_t es = dt == hcclFp32 ? 4 : 2, vecs = a.cols * es / (kWave * 16);
     const uint64_t arrays = (a.grad_z ? 1 : 0) + (a.grad_weight ? 1 : 0);
     const bool stream = a.tokens * (a.top_k * arrays + 1) * a.cols * es > kLastLevelCache;
+    const int lanes = narrow_lanes(a.cols, es);
     return by_type(dt, [&](auto type) {
         constexpr int DT = decltype(type)::value;
-        const dim3 grid((uint32_t)a.tokens);
-        if (vecs < 1) hipLaunchKernelGGL((hccl_moe_combine_backward_kernel<DT, 1, false>), grid, dim3(64), 0, s, a);
+        const dim3 grid((uint32_t)a.tokens), narrow_grid((uint32_t)((a.tokens * lanes + kThreads - 1) / kThreads));
+        if (lanes == 16) hipLaunchKernelGGL((hccl_moe_combine_backward_narrow_kernel<DT, 16>), narrow_grid, dim3(kThreads), 0, s, a);
+        else if (lanes == 32) hipLaunchKernelGGL((hccl_moe_combine_backward_narrow_kernel<DT, 32>), narrow_grid, dim3(kThreads), 0, s, a);
+        else if (vecs < 1) hipLaunchKernelGGL((hccl_moe_combine_backward_kernel<DT, 1, false>), grid, dim3(64), 0, s, a);
         else if (vecs < 2) hipLaunchKernelGGL((hccl_moe_combine_backward_kernel<DT, 2, false>), grid, dim3(128), 0, s, a);
+        // (tokens for no more than one block a CU: 64 tokens x 8 rows of 7 040 fp32 30 -> 15 us)
+        else if (vecs >= 16 && a.tokens <= 256) hipLaunchKernelGGL((hccl_moe_combine_backward_kernel<DT, 16, false>), grid, dim3(1024), 0, s, a);
         else if (stream) hipLaunchKernelGGL((hccl_moe_combine_backward_kernel<DT, 4, true>), grid, dim3(256), 0, s, a);
         else hipLaunchKernelGGL((hccl_moe_combine_backward_kernel<DT, 4, false>), grid, dim3(256), 0, s, a);
     });
