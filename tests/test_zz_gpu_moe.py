@@ -270,7 +270,7 @@ def routes(rng, tokens, top_k, rows, holes=0.1):
     return row
 
 
-SHAPES = [(1, 1, 1), (1, 4, 4096), (3, 2, 7), (5, 32, 64), (37, 4, 1001), (16, 5, 511), (9, 3, 513), (20, 8, 2048), (6, 6, 5003), (130, 1, 100)]
+SHAPES = [(1, 1, 1), (70, 3, 128), (33, 6, 129), (21, 7, 250), (1, 4, 4096), (3, 2, 7), (5, 32, 64), (37, 4, 1001), (16, 5, 511), (9, 3, 513), (20, 8, 2048), (6, 6, 5003), (130, 1, 100)]
 
 
 @pytest.mark.parametrize("dt", ["bf16", "fp16", "fp32"])
@@ -320,6 +320,34 @@ def test_combine_and_its_gradients(comm, tokens, top_k, cols, dt):
         comm.moe_combine_backward(grad, z, d_row, d_w, grad_z=one)
         comm.moe_combine_backward(grad, z, d_row, d_w, grad_weight=two)
         assert torch.equal(one, gz.view) and torch.equal(two, gw.view)
+
+
+@pytest.mark.parametrize("dt,tokens,top_k,cols", [("bf16", 9000, 4, 4096), ("fp32", 5000, 3, 5001), ("fp16", 130, 2, 9000), ("bf16", 70000, 8, 300)])
+def test_large_calls(comm, dt, tokens, top_k, cols):
+    """Calls that move more than the last-level cache, and rows of many vectors, against 64 bits on the GPU."""
+    g = torch.Generator(device=DEV).manual_seed(tokens)
+    row = torch.randperm(tokens * top_k, generator=g, device=DEV).to(torch.int32).view(tokens, top_k)
+    x = torch.randn(tokens, cols, generator=g, device=DEV).to(TYPES[dt])
+    rows = torch.empty(tokens * top_k, cols, device=DEV, dtype=TYPES[dt])
+    comm.moe_dispatch(x, row, rows)
+    for k in range(top_k):
+        assert torch.equal(rows[row[:, k].long()], x)
+    del rows
+    z = torch.randn(tokens * top_k, cols, generator=g, device=DEV).to(TYPES[dt])
+    w = torch.rand(tokens, top_k, generator=g, device=DEV)
+    y, gz, gw = torch.empty_like(x), torch.empty_like(z), torch.empty_like(w)
+    comm.moe_combine(z, row, y, weight=w)
+    comm.moe_combine_backward(x, z, row, w, gz, gw)
+    torch.cuda.synchronize()
+    for at in range(0, tokens, 1000):
+        part = slice(at, at + 1000)
+        zs = z[row[part].long()].double()
+        terms = w[part, :, None].double() * zs
+        rounded(y[part], host(terms.sum(1)), (top_k + 1) * F32 * host(terms.abs().sum(1)), "combine")
+        products = x[part, None].double() * zs
+        close(gw[part], host(products.sum(2)), (cols / 64 + 24) * F32 * host(products.abs().sum(2)), "grad_weight")
+        for k in range(top_k):
+            rounded(gz[row[part, k].long()], host(w[part, k:k + 1].double() * x[part].double()), 0.0, "grad_z")
 
 
 def test_gradient_of_dispatch_is_combine_without_weights(comm):
@@ -387,6 +415,29 @@ def test_quantize_of_a_gate(comm, rows, cols, dt):
     close(scale.view[0], m[:, 0] / 127, 16 * F32 * m[:, 0])
 
 
+@pytest.mark.parametrize("cols", [13, 61, 131, 509, 1003, 2501, 7003])
+@pytest.mark.parametrize("dt", TYPES)
+def test_quantize_many_odd_rows(comm, cols, dt):
+    """Rows of odd sizes that fill the chip, as themselves and to the rows of a dispatch."""
+    g = torch.Generator(device=DEV).manual_seed(cols)
+    rows = 5000
+    x = torch.randn(rows, cols + 3, generator=g, device=DEV).to(TYPES[dt])[:, 1:cols + 1]
+    m = x.float().abs().amax(1, keepdim=True).cpu()
+    want = torch.round(x.float().cpu() * (1 / m * 127)).to(torch.int8)
+    codes, scale = Room(rows, cols, torch.int8, 2, 1), Room(1, rows, torch.float32)
+    comm.moe_quantize(x, codes.view, scale.view)
+    row = torch.randperm(2 * rows, generator=g, device=DEV).to(torch.int32).view(rows, 2)
+    many, scales = Room(2 * rows, cols, torch.int8, 2, 1), Room(1, 2 * rows, torch.float32)
+    comm.moe_dispatch(x, row, many.view, scale=scales.view[0])
+    torch.cuda.synchronize()
+    for room in (codes, scale, many, scales):
+        room.check()
+    assert torch.equal(codes.view.cpu(), want) and torch.equal(scale.view[0].cpu(), (m / 127)[:, 0])
+    for k in range(2):
+        at = row[:, k].long().cpu()
+        assert torch.equal(many.view.cpu()[at], want) and torch.equal(scales.view[0].cpu()[at], (m / 127)[:, 0])
+
+
 def test_quantize_up_to_a_limit_on_the_device(comm):
     rng = np.random.default_rng(0)
     x = rand(rng, 30, 100, "bf16")
@@ -447,6 +498,65 @@ def test_product_of_segments(comm, rows, inner, cols, experts, sources, dt):
     check_product(comm, rng, rows, inner, cols, experts, [first] + [rows] * n, dt, pad=16)
     # offsets beyond the rows, or that go back, move nothing beyond them
     check_product(comm, rng, rows, inner, cols, experts, [0] + [rows + 1000] * n, dt)
+
+
+def on_gpu(codes, scale, weights, weight_scale, ends):
+    """The product in 64 bits on the GPU, segment by segment (whole sums below 2^53)."""
+    out = torch.zeros(codes.shape[0], weights.shape[1], device=DEV, dtype=torch.float64)
+    for s, (a, b) in enumerate(zip(ends[:-1], ends[1:])):
+        e = s % weights.shape[0]
+        if b > a:
+            out[a:b] = torch.mm(codes[a:b].double(), weights[e].double().t().contiguous()) * scale[a:b, None].double() * weight_scale[e].double()
+    return out
+
+
+# (rows, columns, experts): sizes for each of the tiles that a product chooses among on 256 CUs
+TILES = {"256x256": (6000, 2100, 8), "256x256 dense": (3000, 4100, 1), "128x128": (3000, 1500, 12), "64x128": (1000, 2000, 40), "64x64": (300, 3000, 1),
+         "few 16x64": (100, 4096, 30), "few 16x32": (3, 8200, 1), "few 16x16": (9, 300, 1), "few 32x64": (512, 2050, 40), "few 32x32": (48, 4100, 1),
+         "few 32x16": (505, 185, 1)}
+
+
+@pytest.mark.parametrize("inner", [16, 64, 65, 128, 191, 192, 256, 320, 321, 384, 447, 640, 1000])
+@pytest.mark.parametrize("tile", TILES)
+def test_product_of_every_tile_and_length(comm, tile, inner):
+    rows, cols, experts = TILES[tile]
+    g = torch.Generator(device=DEV).manual_seed(inner)
+    rng = np.random.default_rng(rows + inner)
+    sizes = rng.multinomial(rows, rng.dirichlet(np.full(experts, 8.0)))
+    ends = np.concatenate([[0], np.cumsum(sizes)]).tolist()
+    offsets = torch.tensor(ends, device=DEV) if experts > 1 else None
+    dt = ("bf16", "fp16", "fp32")[inner % 3]
+    sa, sb = torch.rand(rows, generator=g, device=DEV) / 64, torch.rand(experts, cols, generator=g, device=DEV) / 64
+    whole = (inner + 15) // 16 * 16
+    for pa, pb in ((whole - inner, whole - inner), (1 + whole - inner, whole - inner), (whole - inner, 1 + whole - inner), (3, 3)):
+        a = torch.randint(-128, 128, (rows, inner + pa), generator=g, device=DEV, dtype=torch.int8)[:, :inner]
+        w = torch.randint(-128, 128, (experts, cols, inner + pb), generator=g, device=DEV, dtype=torch.int8)[:, :, :inner]
+        out = Room(rows, cols, TYPES[dt], pa)
+        comm.moe_product(a, sa, w, sb, out.view, offsets=offsets)
+        torch.cuda.synchronize()
+        out.check()
+        want = on_gpu(a, sa, w, sb, ends)
+        bound = 4 * F32 * want.abs() + 1e-37
+        lo, hi = ((want + s * bound).float().to(TYPES[dt]).double() for s in (-1, 1))
+        got = out.view.double()
+        bad = ~((lo <= got) & (got <= hi))
+        assert not bool(bad.any()), f"{int(bad.sum())} of {bad.numel()} off, first at {bad.nonzero()[0].tolist()}"
+
+
+def test_product_of_many_segments(comm):
+    """More segments than a wave has lanes, in one-row tiles and in large ones, some of them empty."""
+    g = torch.Generator(device=DEV).manual_seed(0)
+    for rows, cols, experts, sources in ((700, 512, 100, 3), (9000, 1024, 70, 2), (20000, 300, 33, 8)):
+        n = experts * sources
+        rng = np.random.default_rng(n)
+        ends = np.concatenate([[0], np.cumsum(rng.multinomial(rows, rng.dirichlet(np.full(n, 0.7))))]).tolist()
+        a = torch.randint(-128, 128, (rows, 96), generator=g, device=DEV, dtype=torch.int8)
+        w = torch.randint(-128, 128, (experts, cols, 96), generator=g, device=DEV, dtype=torch.int8)
+        sa, sb = torch.rand(rows, generator=g, device=DEV), torch.rand(experts, cols, generator=g, device=DEV)
+        out = torch.empty(rows, cols, device=DEV)
+        comm.moe_product(a, sa, w, sb, out, offsets=torch.tensor(ends, device=DEV))
+        want = on_gpu(a, sa, w, sb, ends)
+        assert bool(((out.double() - want).abs() <= 4 * F32 * want.abs()).all())
 
 
 def test_product_of_rows_that_are_no_numbers(comm):
