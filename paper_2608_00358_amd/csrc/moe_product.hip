@@ -504,9 +504,10 @@ hipError_t launch_few(const ProductArgs& a, hipStream_t s) {
 //          64 x 4096 x 4096 x 1             30          17         15         13        10
 //         128 x 4096 x 1024 x 1              -          18         15         13         8
 //         505 x 4672 x  185 x 1              -          27         19         14         7
-// Few rows, and blocks too few for half the CUs: 32 a block from 9 rows a segment on (16 where one expert has no more), and of 64, 32 and 16 columns
-// the most that leave every CU a block, with k shared out over more waves the fewer columns there are
-// (1 x 4096 x 4096: 16 columns 5.4 us, 32 columns 7.0, 64 columns 10.5; 256 x 2048 x 2048 x 64: 80, 48 and 46 us).
+// Few rows, or too few blocks for half the CUs: 32 rows a block from 9 rows a segment on (16 where one expert has
+// no more), and of 64, 32 and 16 columns the most that leave every CU a block, with k shared out over more waves
+// the fewer columns there are (1 x 4096 x 4096: 16 columns 5.4 us, 32 columns 7.0, 64 columns 10.5;
+// 256 x 2048 x 2048 x 64: 80, 48 and 46 us).
 template <int DT>
 hipError_t product_type(const ProductArgs& a, int cus, hipStream_t s) {
     const uint64_t each = a.rows / a.segments, spread = a.offsets ? (a.rows < a.segments ? a.rows : a.segments) : 0;
