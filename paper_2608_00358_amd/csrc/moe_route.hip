@@ -234,6 +234,9 @@ __global__ __launch_bounds__(kRouteThreads) void hccl_moe_route_kernel(RouteArgs
     }
     float w = score(logit);
     if (a.renormalize) {
+        // Where the greatest logit of all need not be among the chosen (a bias, groups by two values) their
+        // scores may all be too small for 32 bits; their shares are not, by the greatest logit among them.
+        if (!a.sigmoid && a.whole_sum) w = Exponential(max_lanes<L>(logit))(logit);
         const float sum = sum_lanes<L>(w);
         w = sum > 0.0f ? w / sum : 0.0f;
     }
@@ -294,7 +297,7 @@ __global__ __launch_bounds__(kRouteThreads) void hccl_moe_route_backward_kernel(
         for (int j = 0; j < N; ++j) l[j] *= inv;
         common = sum_lanes<L>(g * (exponential(logit) * inv));
     } else {
-        float u = sigmoid(logit), d = u * (1.0f - u);  // (0 at -inf)
+        float u = sigmoid(logit), d = u * sigmoid(-logit);  // (1 - s = sigmoid(-l) without its cancellation; 0 at -inf)
         if (!a.sigmoid) u = d = Exponential(max_lanes<L>(logit))(logit);
         if (a.renormalize) {
             const float r = sum_lanes<L>(u), mean = sum_lanes<L>(g * u);

@@ -158,6 +158,57 @@ def test_route_and_its_gradient(comm, cfg, dt):
     rounded(out.view, want, 4e-5 * size)
 
 
+@pytest.mark.parametrize("dt", ["bf16", "fp16", "fp32"])
+def test_slope_of_a_sigmoid_far_from_zero(comm, dt):
+    """s (1 - s), where 1 - s is far below the spacing of numbers near 1."""
+    rng = np.random.default_rng(4)
+    T, E, K = 40, 64, 4
+    logits = rand(rng, T, E, dt, std=10.0)
+    index = np.stack([rng.permutation(E)[:K] for _ in range(T)]).astype(np.int32)
+    grad = rng.normal(size=(T, K)).astype(np.float32)
+    l, want = host(logits), np.zeros((T, E))
+    e = np.exp(-np.abs(l))
+    np.put_along_axis(want, index, grad.astype(np.float64), 1)
+    want *= e / (1.0 + e) ** 2
+    out = Room(T, E, TYPES[dt])
+    comm.moe_route_backward(H.hccl_router_init(experts=E, top_k=K, score="sigmoid"), logits, torch.from_numpy(index).to(DEV),
+                            torch.from_numpy(grad).to(DEV), out.view)
+    torch.cuda.synchronize()
+    out.check()
+    # two exponentials (their arguments: a constant and a product, rounded: 1.5 |l| units; themselves 2), sums (1),
+    # reciprocals (2) and two products
+    rounded(out.view, want, F32 * (3.0 * np.abs(l) + 12.0) * np.abs(want))
+
+
+@pytest.mark.parametrize("dt", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("experts", [32, 200, 600])
+def test_shares_of_chosen_experts_far_below_the_greatest(comm, experts, dt):
+    """A bias chooses experts whose softmax scores are too small for 32 bits; among themselves they have shares."""
+    rng = np.random.default_rng(experts)
+    T, K = 21, 4
+    logits = rand(rng, T, experts, dt)
+    logits[:, 8:] -= 120.0
+    bias = np.linspace(9.0, 5.0, experts).astype(np.float32)
+    bias[:8] = 0.0
+    cfg = dict(experts=experts, top_k=K, renormalize=True, scale=2.5)
+    index = check_route(comm, dict(cfg, bias=True), logits, dt=dt, bias_host=bias)
+    assert (index == np.arange(8, 8 + K)).all()
+    grad = torch.from_numpy(rng.normal(size=(T, K)).astype(np.float32)).to(DEV)
+    out = Room(T, experts, TYPES[dt])
+    comm.moe_route_backward(H.hccl_router_init(**cfg), logits, torch.from_numpy(index.astype(np.int32)).to(DEV), grad, out.view)
+    torch.cuda.synchronize()
+    out.check()
+    l = host(logits)
+    size = np.zeros((T, experts))
+    size[:, 8:8 + K] = 2.5 * np.abs(host(grad)).max(1, keepdims=True)
+    want = ref.route_backward(l, index, host(grad), **cfg)
+    # sum_k du_k u_k = 0 where weights are renormalised, so experts not chosen have no gradient; in 64 bits that sum
+    # is its terms' rounding, which the quotient by r (1e-52) does not make small
+    assert np.abs(np.delete(want, range(8, 8 + K), 1)).max() < 1e-14
+    want[:, :8], want[:, 8 + K:] = 0.0, 0.0
+    rounded(out.view, want, 4e-5 * size)
+
+
 @pytest.mark.parametrize("tokens", [1, 2, 3, 15, 16, 17, 255, 1025])
 @pytest.mark.parametrize("experts", [16, 96, 200, 320, 768])
 def test_route_of_any_number_of_tokens(comm, tokens, experts):
