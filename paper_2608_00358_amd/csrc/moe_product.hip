@@ -1,7 +1,8 @@
 // moe_product.hip -- the experts' product in 8-bit integers:
 //   out[m, n] = a_scale[m] * b_scale[e, n] * sum_k a[m, k] b[e, n, k],   e the expert of row m's segment
 // on the matrix instructions for 8-bit integers, with whole sums in 32 bits (exact: at most
-// 131 071 products of at most 2^14). The rows of a segment follow each other; where segments begin is
+// 131 071 products of at most 2^14), which become 32-bit floats only for the scales (a sum above 2^24 is rounded
+// there, by 2^-24 of itself at most, as each of the two products with the scales is). The rows of a segment follow each other; where segments begin is
 // read on the device, so the grid is sized for the worst case and surplus blocks end at once.
 //
 // The weights are the instruction's first operand: a lane then holds neighbouring columns of one row.
