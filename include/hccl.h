@@ -509,8 +509,9 @@ typedef enum { hcclScoreSoftmax = 0, hcclScoreSigmoid = 1 } hcclScore_t;
  * The top_k greatest choice values left are chosen, in descending order. Ties go to the lowest
  * index, of groups and of experts. Where fewer are left, the last choices are -1 with weight 0.
  * weight_k = scale * s_{e_k}, or with renormalize scale * s_{e_k} / sum_j s_{e_j} (0 if that sum is).
- * Scores below 2^-126 count as 0, but renormalised softmax weights, and their gradient, are shares by
- * the greatest logit among the chosen, however small the scores are.
+ * Scores below 2^-126 count as 0, but renormalised weights, and their gradient, are taken relative to
+ * the greatest logit among the chosen, however small the scores are; only where that logit is below
+ * -708 are all of a sigmoid's 0, as under a mask by a great negative number.
  */
 typedef struct {
     uint32_t experts;      /* 1 .. HCCL_MAX_EXPERTS */

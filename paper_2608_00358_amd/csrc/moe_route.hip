@@ -68,6 +68,19 @@ struct Exponential {
 // (0 at -inf)
 __device__ __forceinline__ float sigmoid(float l) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-l * kLog2e)); }
 
+// What the weights of a token's choices are shares by, once they are renormalised: the scores, without a factor
+// that they have in common. The greatest logit m among the chosen has none too small for 32 bits: a softmax's
+// are e^(l - m), and a sigmoid's, e^l / (1 + e^l), are e^(l - m) s(-l) where m is below 0. Sigmoids below e^-708, the
+// least normal number of 64 bits, are 0 all the same: a mask by a great negative number leaves nothing to share.
+// A lane has one choice's logit, -inf without one.
+constexpr float kNoScore = -708.0f;
+template <int L>
+__device__ __forceinline__ float share(float logit, bool of_sigmoid) {
+    const float m = max_lanes<L>(logit), u = Exponential(m)(logit);
+    if (!of_sigmoid) return u;
+    return m < kNoScore ? 0.0f : m < 0.0f ? u * sigmoid(-logit) : sigmoid(logit);
+}
+
 // A 16-bit float widened to 32 bits has its 13 lowest bits free: the order of the float as an unsigned
 // number there, and 1023 less the expert below it. -0 counts as 0. And back.
 constexpr uint32_t kFree = 0x1fffu;
@@ -234,9 +247,9 @@ __global__ __launch_bounds__(kRouteThreads) void hccl_moe_route_kernel(RouteArgs
     }
     float w = score(logit);
     if (a.renormalize) {
-        // Where the greatest logit of all need not be among the chosen (a bias, groups by two values) their
-        // scores may all be too small for 32 bits; their shares are not, by the greatest logit among them.
-        if (!a.sigmoid && a.whole_sum) w = Exponential(max_lanes<L>(logit))(logit);
+        // Where the greatest logit of all need not be among the chosen (a bias, groups by two values), and with
+        // sigmoids anyway, the chosen scores may all be too small for 32 bits; their shares are not.
+        if (a.sigmoid || a.whole_sum) w = share<L>(logit, a.sigmoid);
         const float sum = sum_lanes<L>(w);
         w = sum > 0.0f ? w / sum : 0.0f;
     }
@@ -251,8 +264,9 @@ __global__ __launch_bounds__(kRouteThreads) void hccl_moe_route_kernel(RouteArgs
 //   softmax: dl_e = s_e (du_e - sum_k du_k u_k)     sigmoid: dl_e = du_e s_e (1 - s_e)
 // Scores are computed again from the logits: reading them costs less than storing them would.
 // DENSE: a softmax without renormalisation, where every expert's logit moves the weights. Otherwise only
-// the chosen ones' do: with the sum, sum_k du_k u_k is nothing, and s_k / r is the weight itself, so a
-// lane needs its choice's logit and no other. The gradients of the chosen go to the lanes that hold
+// the chosen ones' do: with the sum, sum_k du_k u_k is nothing, and with the shares p_k = u_k / r
+//   dl_e = scale (g_e - sum_j g_j p_j) p_e   (times 1 - s_e: sigmoid)
+// so a lane needs its choice's logit and no other. The gradients of the chosen go to the lanes that hold
 // those experts through LDS.
 template <int DT, int L, int N, bool DENSE>
 __global__ __launch_bounds__(kRouteThreads) void hccl_moe_route_backward_kernel(RouteBackwardArgs a) {
@@ -297,12 +311,17 @@ __global__ __launch_bounds__(kRouteThreads) void hccl_moe_route_backward_kernel(
         for (int j = 0; j < N; ++j) l[j] *= inv;
         common = sum_lanes<L>(g * (exponential(logit) * inv));
     } else {
-        float u = sigmoid(logit), d = u * sigmoid(-logit);  // (1 - s = sigmoid(-l) without its cancellation; 0 at -inf)
-        if (!a.sigmoid) u = d = Exponential(max_lanes<L>(logit))(logit);
+        // The quotients by r are taken of the scores, not of the gradients: a share p_k = u_k / r is at most 1 where
+        // 1 / r may be beyond 32 bits. 1 - s = s(-l), without its cancellation.
+        float d = 1.0f;
         if (a.renormalize) {
-            const float r = sum_lanes<L>(u), mean = sum_lanes<L>(g * u);
-            g = r > 0.0f ? (g - mean / r) / r : 0.0f;
+            const float u = share<L>(logit, a.sigmoid), r = sum_lanes<L>(u);
+            const float p = r > 0.0f ? u / r : 0.0f;
+            g = (g - sum_lanes<L>(g * p)) * p;
+        } else {
+            d = sigmoid(logit);  // (0 at -inf)
         }
+        if (a.sigmoid) d *= sigmoid(-logit);
         g *= d;
     }
     if (some) atomicAdd(&part[mine], g);  // (a router names an expert once)
