@@ -232,14 +232,23 @@ def hccl_config_init(**kw) -> hcclConfig_t:
     return cfg
 
 
+_comm_ranks = {}  # ranks of the communicators made here, by address
+
+
+def _comm_key(comm) -> Optional[int]:
+    return comm.value if isinstance(comm, ctypes.c_void_p) else comm
+
+
 def hccl_comm_create(nranks: int, device: int = 0, cfg: Optional[hcclConfig_t] = None) -> ctypes.c_void_p:
     comm = ctypes.c_void_p()
     _check(load().hccl_comm_create(nranks, device, ctypes.byref(cfg) if cfg is not None else None,
                                    ctypes.byref(comm)))
+    _comm_ranks[comm.value] = nranks
     return comm
 
 
 def hccl_comm_destroy(comm) -> None:
+    _comm_ranks.pop(_comm_key(comm), None)
     _check(load().hccl_comm_destroy(comm))
 
 
@@ -411,7 +420,10 @@ def _call_moe_plan(comm, index, experts, row, offsets, capacity, rank_counts=Non
     T, K = index.shape
     counts = None
     if rank_counts is not None:
-        counts = _list(rank_counts, rank_counts.numel(), "int64", "rank_counts")
+        ranks = _comm_ranks.get(_comm_key(comm))
+        if ranks is None:
+            raise ValueError("rank_counts need a communicator made by hccl_comm_create")
+        counts = _list(rank_counts, ranks, "int64", "rank_counts")
     size = 0 if workspace is None else workspace.numel() * workspace.element_size()
     return load().hccl_moe_plan, (comm, _list(index, T * K, "int32", "index"), T, K, experts, capacity,
                                   _list(row, T * K, "int32", "row"), _list(offsets, experts + 1, "int64", "offsets"), counts,
@@ -679,17 +691,12 @@ class Comm:
                                router, logits, index, grad_weight, grad_logits)
 
     def moe_plan(self, index, experts, row, offsets, capacity, rank_counts=None, workspace=None, stream=None):
-        hccl_moe_plan(self.handle, index, experts, row, offsets, capacity, self._rank_counts(rank_counts), workspace, stream)
+        hccl_moe_plan(self.handle, index, experts, row, offsets, capacity, rank_counts, workspace, stream)
 
     def bind_moe_plan(self, index, experts, row, offsets, capacity, rank_counts=None, workspace=None, stream=None):
-        return _bound_operator(self, _call_moe_plan(self.handle, index, experts, row, offsets, capacity, self._rank_counts(rank_counts),
+        return _bound_operator(self, _call_moe_plan(self.handle, index, experts, row, offsets, capacity, rank_counts,
                                                  workspace, stream),
                                index, row, offsets, rank_counts, workspace)
-
-    def _rank_counts(self, rank_counts):
-        if rank_counts is not None and rank_counts.numel() != self.nranks:
-            raise ValueError(f"rank_counts must be {self.nranks} packed int64 elements")
-        return rank_counts
 
     def moe_dispatch(self, x, row, out, scale=None, stream=None):
         hccl_moe_dispatch(self.handle, x, row, out, scale, stream)

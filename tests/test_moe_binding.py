@@ -1,0 +1,47 @@
+"""What the Python binding of the mixture-of-experts operators passes on: nothing that its C call could write beyond."""
+import pytest
+import torch
+
+import paper_2608_00358_amd as H
+
+
+@pytest.fixture()
+def comm():
+    with H.Comm(4, device=H.NO_DEVICE) as c:
+        yield c
+
+
+def _plan_arrays(T=5, K=2, E=8):
+    i32 = torch.int32
+    return (torch.zeros(T, K, dtype=i32), E, torch.zeros(T, K, dtype=i32), torch.zeros(E + 1, dtype=torch.int64), T * K)
+
+
+@pytest.mark.parametrize("n", [0, 1, 3, 5])
+def test_rank_counts_hold_a_number_for_every_rank(comm, n):
+    counts = torch.zeros(n, dtype=torch.int64)
+    for handle in (comm.handle, comm.handle.value):
+        with pytest.raises(ValueError):
+            H.hccl_moe_plan(handle, *_plan_arrays(), rank_counts=counts)
+        H.hccl_moe_plan(handle, *_plan_arrays(), rank_counts=torch.zeros(4, dtype=torch.int64))
+        H.hccl_moe_plan(handle, *_plan_arrays())
+    for method in (comm.moe_plan, comm.bind_moe_plan):
+        with pytest.raises(ValueError):
+            method(*_plan_arrays(), rank_counts=counts)
+
+
+def test_rank_counts_of_a_communicator_that_the_binding_does_not_know(comm, monkeypatch):
+    """Nobody can say how many counts such a communicator writes."""
+    counts = torch.zeros(4, dtype=torch.int64)
+    H.hccl_moe_plan(comm.handle, *_plan_arrays(), rank_counts=counts)
+    monkeypatch.setattr(H.hccl, "_comm_ranks", {})
+    with pytest.raises(ValueError):
+        H.hccl_moe_plan(comm.handle, *_plan_arrays(), rank_counts=counts)
+    H.hccl_moe_plan(comm.handle, *_plan_arrays())
+
+
+def test_a_destroyed_communicator_is_forgotten():
+    handle = H.hccl_comm_create(3, H.NO_DEVICE)
+    at = handle.value
+    assert H.hccl._comm_ranks[at] == 3
+    H.hccl_comm_destroy(handle)
+    assert at not in H.hccl._comm_ranks
