@@ -424,6 +424,8 @@ def _call_moe_plan(comm, index, experts, row, offsets, capacity, rank_counts=Non
         if ranks is None:
             raise ValueError("rank_counts need a communicator made by hccl_comm_create")
         counts = _list(rank_counts, ranks, "int64", "rank_counts")
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("workspace must be packed")
     size = 0 if workspace is None else workspace.numel() * workspace.element_size()
     return load().hccl_moe_plan, (comm, _list(index, T * K, "int32", "index"), T, K, experts, capacity,
                                   _list(row, T * K, "int32", "row"), _list(offsets, experts + 1, "int64", "offsets"), counts,

@@ -45,3 +45,17 @@ def test_a_destroyed_communicator_is_forgotten():
     assert H.hccl._comm_ranks[at] == 3
     H.hccl_comm_destroy(handle)
     assert at not in H.hccl._comm_ranks
+
+
+def test_a_workspace_is_packed(comm):
+    """Its bytes are those from its address on, which a strided or expanded tensor does not have."""
+    T, K, E = 4096, 2, 8
+    need = H.hccl_moe_plan_bytes(T, K, E)
+    arrays = _plan_arrays(T, K, E)
+    comm.moe_plan(*arrays, workspace=torch.zeros(need, dtype=torch.uint8))
+    comm.moe_plan(*arrays, workspace=torch.zeros(8, need // 8, dtype=torch.uint8))
+    for bad in (torch.zeros(2 * need, dtype=torch.uint8)[::2], torch.zeros(1, dtype=torch.int32).expand(need),
+                torch.zeros(need // 8, 16, dtype=torch.uint8)[:, :8]):
+        for call in (comm.moe_plan, comm.bind_moe_plan):
+            with pytest.raises(ValueError):
+                call(*arrays, workspace=bad)
