@@ -398,10 +398,15 @@ def _codes(t, what):
         raise ValueError(f"{what} must be int8, not {t.dtype}")
 
 
+def _router(router):
+    """The router as it is now, for a call that may be made when it is another one: its arrays are checked against this."""
+    return ctypes.byref(hcclRouter_t.from_buffer_copy(router))
+
+
 def _call_moe_route(comm, router, logits, index, weight, bias=None, mask=None, stream=None):
     T, E, K = logits.shape[0], router.experts, router.top_k
     at, ld = _rows(logits, T, E, "logits")
-    return load().hccl_moe_route, (comm, ctypes.byref(router), at, ld, _dtype_code(logits.dtype), T, _list(bias, E, "float32", "bias"),
+    return load().hccl_moe_route, (comm, _router(router), at, ld, _dtype_code(logits.dtype), T, _list(bias, E, "float32", "bias"),
                                    _list(mask, T, "uint8", "mask"), _list(index, T * K, "int32", "index"),
                                    _list(weight, T * K, "float32", "weight"), _stream_handle(stream))
 
@@ -411,7 +416,7 @@ def _call_moe_route_backward(comm, router, logits, index, grad_weight, grad_logi
     at, ld = _rows(logits, T, E, "logits")
     out, ldg = _rows(grad_logits, T, E, "grad_logits")
     _same_type(grad_logits, logits, "grad_logits")
-    return load().hccl_moe_route_backward, (comm, ctypes.byref(router), at, ld, _dtype_code(logits.dtype), T,
+    return load().hccl_moe_route_backward, (comm, _router(router), at, ld, _dtype_code(logits.dtype), T,
                                             _list(index, T * K, "int32", "index"),
                                             _list(grad_weight, T * K, "float32", "grad_weight"), out, ldg, _stream_handle(stream))
 
@@ -677,20 +682,20 @@ class Comm:
                       _dtype_code(send[0].dtype), _stream_handle(stream))
 
     # Mixture-of-experts operators: one rank's tensors, no list of them (see include/hccl.h). The bind_*
-    # forms keep their tensors alive and the stream that is current when they are made.
+    # forms keep their tensors alive, the stream that is current when they are made, and the router as it is then.
     def moe_route(self, router, logits, index, weight, bias=None, mask=None, stream=None):
         hccl_moe_route(self.handle, router, logits, index, weight, bias, mask, stream)
 
     def bind_moe_route(self, router, logits, index, weight, bias=None, mask=None, stream=None):
         return _bound_operator(self, _call_moe_route(self.handle, router, logits, index, weight, bias, mask, stream),
-                               router, logits, index, weight, bias, mask)
+                               logits, index, weight, bias, mask)
 
     def moe_route_backward(self, router, logits, index, grad_weight, grad_logits, stream=None):
         hccl_moe_route_backward(self.handle, router, logits, index, grad_weight, grad_logits, stream)
 
     def bind_moe_route_backward(self, router, logits, index, grad_weight, grad_logits, stream=None):
         return _bound_operator(self, _call_moe_route_backward(self.handle, router, logits, index, grad_weight, grad_logits, stream),
-                               router, logits, index, grad_weight, grad_logits)
+                               logits, index, grad_weight, grad_logits)
 
     def moe_plan(self, index, experts, row, offsets, capacity, rank_counts=None, workspace=None, stream=None):
         hccl_moe_plan(self.handle, index, experts, row, offsets, capacity, rank_counts, workspace, stream)

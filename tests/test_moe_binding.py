@@ -59,3 +59,15 @@ def test_a_workspace_is_packed(comm):
         for call in (comm.moe_plan, comm.bind_moe_plan):
             with pytest.raises(ValueError):
                 call(*arrays, workspace=bad)
+
+
+def test_a_bound_call_keeps_its_router(comm):
+    """The arrays were checked against the router as it was: a larger one would write beyond them."""
+    T, E = 5, 8
+    logits, index, weight = torch.zeros(T, E), torch.zeros(T, 2, dtype=torch.int32), torch.zeros(T, 2)
+    router = H.hccl_router_init(experts=E, top_k=2)
+    calls = [comm.bind_moe_route(router, logits, index, weight),
+             comm.bind_moe_route_backward(router, logits, index, weight, torch.zeros_like(logits))]
+    router.top_k = E + 1  # (refused where it is read)
+    for call in calls:
+        call()
