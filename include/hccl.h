@@ -488,7 +488,10 @@ hcclResult_t hccl_comm_trace(hcclComm_t comm, hcclTileTrace_t* out, size_t capac
  * accesses. An array that is written may not overlap another, except for rows of two arrays of the
  * same stride that lie side by side. `dtype` is hcclBf16, hcclFp16 or hcclFp32. Sums, softmax
  * statistics, scores and weights are held in 32 bits, and a result is rounded to its type once. All
- * results are the same in every call. Zero tokens, rows or columns are allowed.
+ * results are the same in every call. Zero tokens, rows or columns are allowed. A launch's threads are
+ * counted in 32 bits: a call that would take more fails with hcclUnsupported and enqueues nothing.
+ * Routing takes at least 2^26 - 512 tokens, quantisation (and dispatch in 8 bits) and combine's gradient
+ * 2^24 - 1 rows or tokens, dispatch and combine 2^26 - 4 tokens of up to 1 KiB or as many KiB of longer ones.
  */
 #define HCCL_MAX_EXPERTS 1024
 #define HCCL_MAX_TOP_K 32

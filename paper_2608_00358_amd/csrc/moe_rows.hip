@@ -620,23 +620,28 @@ void launch_quantize_rows(const QuantizeArgs& a, hipStream_t s) {
     hipLaunchKernelGGL((hccl_moe_quantize_kernel<DT, GATED, W>), dim3((uint32_t)((a.rows * W + kWaves - 1) / kWaves)), dim3(kThreads), 0, s, a);
 }
 
+// As many waves a row as leave its lanes at most kKeep vectors, up to 4; one for up to 2 vectors a lane
+// (16 384 rows of bf16: 512 columns 1 / 2 / 4 waves 7.3 / 9.9 / 14 us, 4 096 columns 50 / 37 / 38 us, 8 192
+// columns 106 / 87 / 71 us).
+uint32_t quantize_waves(uint64_t cols, hcclDataType_t dt) {
+    const uint64_t per = kWave * (dt == hcclFp32 ? 4 : 8), vecs = (cols + per - 1) / per;
+    return vecs <= 2 ? 1 : vecs <= 2 * kKeep ? 2 : 4;
+}
+
 template <int DT, bool GATED>
-void quantize_type(const QuantizeArgs& a, hipStream_t s) {
-    // As many waves a row as leave its lanes at most kKeep vectors, up to 4; one for up to 2 vectors a lane
-    // (16 384 rows of bf16: 512 columns 1 / 2 / 4 waves 7.3 / 9.9 / 14 us, 4 096 columns 50 / 37 / 38 us, 8 192
-    // columns 106 / 87 / 71 us).
-    const uint64_t vecs = (a.cols + kWave * kVecOf<DT> - 1) / (kWave * kVecOf<DT>);
-    if (vecs <= 2) launch_quantize_rows<DT, GATED, 1>(a, s);
-    else if (vecs <= 2 * kKeep) launch_quantize_rows<DT, GATED, 2>(a, s);
+void quantize_type(const QuantizeArgs& a, uint32_t waves, hipStream_t s) {
+    if (waves == 1) launch_quantize_rows<DT, GATED, 1>(a, s);
+    else if (waves == 2) launch_quantize_rows<DT, GATED, 2>(a, s);
     else launch_quantize_rows<DT, GATED, 4>(a, s);
 }
 
 hipError_t launch_quantize(const QuantizeArgs& a, hcclDataType_t dt, bool gated, hipStream_t s) {
-    if (too_many(a.rows, kThreads)) return hipErrorInvalidConfiguration;
+    const uint32_t waves = quantize_waves(a.cols, dt);
+    if (too_many((a.rows * waves + kWaves - 1) / kWaves, kThreads)) return hipErrorInvalidConfiguration;
     return by_type(dt, [&](auto type) {
         constexpr int DT = decltype(type)::value;
-        if (gated) quantize_type<DT, true>(a, s);
-        else quantize_type<DT, false>(a, s);
+        if (gated) quantize_type<DT, true>(a, waves, s);
+        else quantize_type<DT, false>(a, waves, s);
     });
 }
 
@@ -661,22 +666,23 @@ hipError_t launch_combine(const CombineArgs& a, hcclDataType_t dt, hipStream_t s
 }
 
 hipError_t launch_combine_backward(const CombineBackwardArgs& a, hcclDataType_t dt, hipStream_t s) {
-    if (too_many(a.tokens, 1024)) return hipErrorInvalidConfiguration;
     const uint64_t es = dt == hcclFp32 ? 4 : 2, vecs = a.cols * es / (kWave * 16);
     const uint64_t arrays = (a.grad_z ? 1 : 0) + (a.grad_weight ? 1 : 0);
     const bool stream = a.tokens * (a.top_k * arrays + 1) * a.cols * es > kLastLevelCache;
     const int lanes = narrow_lanes(a.cols, es);
+    // (16 waves for tokens for no more than one block a CU: 64 tokens x 8 rows of 7 040 fp32 30 -> 15 us)
+    const uint32_t waves = vecs < 1 ? 1 : vecs < 2 ? 2 : vecs >= 16 && a.tokens <= 256 ? 16 : 4;
+    if (lanes ? too_many(a.tokens / kThreads + 1, kThreads * lanes) : too_many(a.tokens, waves * kWave)) return hipErrorInvalidConfiguration;
     return by_type(dt, [&](auto type) {
         constexpr int DT = decltype(type)::value;
-        const dim3 grid((uint32_t)a.tokens), narrow_grid((uint32_t)((a.tokens * lanes + kThreads - 1) / kThreads));
+        const dim3 grid((uint32_t)a.tokens), narrow_grid((uint32_t)((a.tokens * lanes + kThreads - 1) / kThreads)), block(waves * kWave);
         if (lanes == 16) hipLaunchKernelGGL((hccl_moe_combine_backward_narrow_kernel<DT, 16>), narrow_grid, dim3(kThreads), 0, s, a);
         else if (lanes == 32) hipLaunchKernelGGL((hccl_moe_combine_backward_narrow_kernel<DT, 32>), narrow_grid, dim3(kThreads), 0, s, a);
-        else if (vecs < 1) hipLaunchKernelGGL((hccl_moe_combine_backward_kernel<DT, 1, false>), grid, dim3(64), 0, s, a);
-        else if (vecs < 2) hipLaunchKernelGGL((hccl_moe_combine_backward_kernel<DT, 2, false>), grid, dim3(128), 0, s, a);
-        // (tokens for no more than one block a CU: 64 tokens x 8 rows of 7 040 fp32 30 -> 15 us)
-        else if (vecs >= 16 && a.tokens <= 256) hipLaunchKernelGGL((hccl_moe_combine_backward_kernel<DT, 16, false>), grid, dim3(1024), 0, s, a);
-        else if (stream) hipLaunchKernelGGL((hccl_moe_combine_backward_kernel<DT, 4, true>), grid, dim3(256), 0, s, a);
-        else hipLaunchKernelGGL((hccl_moe_combine_backward_kernel<DT, 4, false>), grid, dim3(256), 0, s, a);
+        else if (waves == 1) hipLaunchKernelGGL((hccl_moe_combine_backward_kernel<DT, 1, false>), grid, block, 0, s, a);
+        else if (waves == 2) hipLaunchKernelGGL((hccl_moe_combine_backward_kernel<DT, 2, false>), grid, block, 0, s, a);
+        else if (waves == 16) hipLaunchKernelGGL((hccl_moe_combine_backward_kernel<DT, 16, false>), grid, block, 0, s, a);
+        else if (stream) hipLaunchKernelGGL((hccl_moe_combine_backward_kernel<DT, 4, true>), grid, block, 0, s, a);
+        else hipLaunchKernelGGL((hccl_moe_combine_backward_kernel<DT, 4, false>), grid, block, 0, s, a);
     });
 }
 
