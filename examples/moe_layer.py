@@ -32,6 +32,7 @@ class ServingLayer:
 
     def __init__(self, comm, router, w_router, w_in, w_out, tokens):
         """w_router (E, C); w_in (E, 2 F, C): the gates' rows, then the ups'; w_out (E, C, F)."""
+        self.stream = torch.cuda.current_stream()  # which the bound calls keep
         P, E, K = comm.nranks, router.experts, router.top_k
         C, F, dev = w_router.shape[1], w_out.shape[2], w_router.device
         T, each, room = tokens, E // P, P * tokens * K  # (every route of every rank could go to one rank)
@@ -77,7 +78,17 @@ class ServingLayer:
         self.combine = [comm.bind_moe_combine(home[r], row[r], self.out[r], weight=weight[r]) for r in ranks]
 
     def __call__(self):
-        """self.x (P tensors) -> self.out"""
+        """self.x (P tensors) -> self.out, in the order of the current stream"""
+        here = torch.cuda.current_stream()
+        if here == self.stream:
+            return self._layer()
+        self.stream.wait_stream(here)
+        with torch.cuda.stream(self.stream):
+            out = self._layer()
+        here.wait_stream(self.stream)
+        return out
+
+    def _layer(self):
         P = self.comm.nranks
         for r in range(P):
             torch.mm(self.x[r].float(), self.w_router.t(), out=self.logits[r])
