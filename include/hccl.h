@@ -381,6 +381,10 @@ hcclResult_t hccl_get_async_error(hcclComm_t comm);
  * until hccl_comm_destroy. hccl_get_async_error is not available while the executor runs.
  * hipDeviceSynchronize (and anything that waits for every stream of the device) waits for the
  * executor too, which ends only at hccl_resident_stop or its idle limit: synchronise streams.
+ * The HIP runtime shares a few hardware queues (GPU_MAX_HW_QUEUES) among a process's streams. If the
+ * executor's stream shares the queue of another one, which may be the default stream, work enqueued there
+ * waits until the executor has ended. Which streams do follows from all those that the process has
+ * made (torch's matrix products make some): write inputs on a stream that was seen to progress beside it.
  */
 hcclResult_t hccl_resident_start(hcclComm_t comm, uint32_t blocks, uint32_t idle_ms);
 
@@ -478,7 +482,8 @@ hcclResult_t hccl_comm_trace(hcclComm_t comm, hcclTileTrace_t* out, size_t capac
  * They work on one rank's arrays in device memory and name no rank. Unlike a collective they are no
  * work packets: nothing is compiled or kept between calls, they take no trigger and write no
  * program record, a device error of a collective does not stop them, and while a resident executor
- * runs they are launched on `stream` as ever (which does not order them with its packets). So they
+ * runs they are launched on `stream` all the same: not ordered with its packets, and, like other
+ * work, held up until it ends where `stream` shares its hardware queue (hccl_resident_start). So they
  * may be captured into a HIP graph at their first call, and calls on one communicator on several
  * streams need no order among themselves. Inside a group they fail with hcclUnsupported. On a
  * communicator without a device their arguments are checked and nothing is enqueued.
