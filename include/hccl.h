@@ -622,8 +622,9 @@ hcclResult_t hccl_moe_quantize(hcclComm_t comm, const void* x, size_t ldx, hcclD
  * offsets (int64[segments + 1], device, ascending): rows [offsets[s], offsets[s + 1]) are segment
  * s's and use expert s % experts, so that the rows that an exchange brought in, ordered by source and
  * then by expert, are segments as they lie. segments is a multiple of experts; segments may be empty.
- * Offsets outside 0 .. rows are clipped, and rows in no segment are left as they are. offsets may be
- * NULL with one expert: every row uses it.
+ * Offsets outside 0 .. rows are clipped, a segment that then ends before it begins is empty, and rows in
+ * no segment are left as they are. Of rows in two segments it is unspecified which are written, and
+ * by which of the two; nothing else is touched. offsets may be NULL with one expert: every row uses it.
  */
 hcclResult_t hccl_moe_product(hcclComm_t comm, const int8_t* codes, size_t lda, const float* scale, size_t rows,
                               size_t inner, const int8_t* weights, size_t ldb, const float* weight_scale, size_t cols,

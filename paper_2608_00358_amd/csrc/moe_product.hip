@@ -34,7 +34,8 @@ __device__ __forceinline__ void segment(const ProductArgs& a, uint32_t s, uint64
     end = hi < (int64_t)first ? first : (uint64_t)hi < a.rows ? (uint64_t)hi : a.rows;
 }
 
-// 64 segments, one a lane: their rows, their tiles of BM rows and the running sum of those.
+// 64 segments, one a lane: their rows, their tiles of BM rows and the running sum of those (which 32 bits hold even
+// where all 64 have every row: that is at most 2^25 tiles of 64 rows each, or, by the limit of a launch, 2^24 of fewer).
 template <uint32_t BM>
 struct Segments {
     uint64_t first, end;
