@@ -494,52 +494,45 @@ def _call_moe_product(comm, codes, scale, weights, weight_scale, out, offsets=No
                                      _dtype_code(out.dtype), _stream_handle(stream))
 
 
-def hccl_moe_route(*args, **kw) -> None:
-    """(comm, router, logits, index, weight, bias=None, mask=None, stream=None)"""
-    fn, a = _call_moe_route(*args, **kw)
+def hccl_moe_route(comm, router, logits, index, weight, bias=None, mask=None, stream=None) -> None:
+    fn, a = _call_moe_route(comm, router, logits, index, weight, bias, mask, stream)
     _check(fn(*a))
 
 
-def hccl_moe_route_backward(*args, **kw) -> None:
-    """(comm, router, logits, index, grad_weight, grad_logits, stream=None)"""
-    fn, a = _call_moe_route_backward(*args, **kw)
+def hccl_moe_route_backward(comm, router, logits, index, grad_weight, grad_logits, stream=None) -> None:
+    fn, a = _call_moe_route_backward(comm, router, logits, index, grad_weight, grad_logits, stream)
     _check(fn(*a))
 
 
-def hccl_moe_plan(*args, **kw) -> None:
-    """(comm, index, experts, row, offsets, capacity, rank_counts=None, workspace=None, stream=None)"""
-    fn, a = _call_moe_plan(*args, **kw)
+def hccl_moe_plan(comm, index, experts, row, offsets, capacity, rank_counts=None, workspace=None, stream=None) -> None:
+    fn, a = _call_moe_plan(comm, index, experts, row, offsets, capacity, rank_counts, workspace, stream)
     _check(fn(*a))
 
 
-def hccl_moe_dispatch(*args, **kw) -> None:
-    """(comm, x, row, out, scale=None, stream=None): int8 rows with a scale"""
-    fn, a = _call_moe_dispatch(*args, **kw)
+def hccl_moe_dispatch(comm, x, row, out, scale=None, stream=None) -> None:
+    """With a scale, out is int8 and holds the rows as hccl_moe_quantize gives them."""
+    fn, a = _call_moe_dispatch(comm, x, row, out, scale, stream)
     _check(fn(*a))
 
 
-def hccl_moe_combine(*args, **kw) -> None:
-    """(comm, z, row, out, weight=None, stream=None)"""
-    fn, a = _call_moe_combine(*args, **kw)
+def hccl_moe_combine(comm, z, row, out, weight=None, stream=None) -> None:
+    fn, a = _call_moe_combine(comm, z, row, out, weight, stream)
     _check(fn(*a))
 
 
-def hccl_moe_combine_backward(*args, **kw) -> None:
-    """(comm, grad, z, row, weight, grad_z=None, grad_weight=None, stream=None)"""
-    fn, a = _call_moe_combine_backward(*args, **kw)
+def hccl_moe_combine_backward(comm, grad, z, row, weight, grad_z=None, grad_weight=None, stream=None) -> None:
+    fn, a = _call_moe_combine_backward(comm, grad, z, row, weight, grad_z, grad_weight, stream)
     _check(fn(*a))
 
 
-def hccl_moe_quantize(*args, **kw) -> None:
-    """(comm, x, codes, scale, gated=False, limit=None, stream=None)"""
-    fn, a = _call_moe_quantize(*args, **kw)
+def hccl_moe_quantize(comm, x, codes, scale, gated=False, limit=None, stream=None) -> None:
+    fn, a = _call_moe_quantize(comm, x, codes, scale, gated, limit, stream)
     _check(fn(*a))
 
 
-def hccl_moe_product(*args, **kw) -> None:
-    """(comm, codes, scale, weights, weight_scale, out, offsets=None, stream=None): codes (rows, inner),
-    weights (experts, columns, inner)"""
-    fn, a = _call_moe_product(*args, **kw)
+def hccl_moe_product(comm, codes, scale, weights, weight_scale, out, offsets=None, stream=None) -> None:
+    """codes (rows, inner), weights (experts, columns, inner)."""
+    fn, a = _call_moe_product(comm, codes, scale, weights, weight_scale, out, offsets, stream)
     _check(fn(*a))
 
 

@@ -1,4 +1,6 @@
 """What the Python binding of the mixture-of-experts operators passes on: nothing that its C call could write beyond."""
+import inspect
+
 import pytest
 import torch
 
@@ -71,3 +73,12 @@ def test_a_bound_call_keeps_its_router(comm):
     router.top_k = E + 1  # (refused where it is read)
     for call in calls:
         call()
+
+
+@pytest.mark.parametrize("name", ["route", "route_backward", "plan", "dispatch", "combine", "combine_backward", "quantize", "product"])
+def test_functions_and_methods_have_one_signature(name):
+    """The function takes a communicator's handle first, the methods are those of the communicator."""
+    function, method, bind = (list(inspect.signature(f).parameters.values())[1:] for f in (
+        getattr(H, f"hccl_moe_{name}"), getattr(H.Comm, f"moe_{name}"), getattr(H.Comm, f"bind_moe_{name}")))
+    assert function and all(p.kind is p.POSITIONAL_OR_KEYWORD for p in function)
+    assert [(p.name, p.default) for p in function] == [(p.name, p.default) for p in method] == [(p.name, p.default) for p in bind]
