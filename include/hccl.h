@@ -520,6 +520,8 @@ typedef enum { hcclScoreSoftmax = 0, hcclScoreSigmoid = 1 } hcclScore_t;
  * Scores below 2^-126 count as 0, but renormalised weights, and their gradient, are taken relative to
  * the greatest logit among the chosen, however small the scores are; only where that logit is below
  * -708 are all of a sigmoid's 0, as under a mask by a great negative number.
+ * With d a logit's distance from the greatest (softmax) or from 0 (sigmoid), its score is off by at most
+ * (2.5 |d| + 48) 2^-24 of itself: an exponential is one of base 2, of a product that is rounded once.
  */
 typedef struct {
     uint32_t experts;      /* 1 .. HCCL_MAX_EXPERTS */
@@ -574,7 +576,8 @@ hcclResult_t hccl_moe_plan(hcclComm_t comm, const int32_t* index, size_t tokens,
 
 /*
  * Dispatch: out[row[t * top_k + k]] = x[t] for every k; rows outside 0 .. capacity - 1 are skipped,
- * and rows that none names keep what they held. x: tokens rows of cols; out: capacity rows.
+ * and rows that none names keep what they held. No two routes may have the same row. x: tokens rows of cols;
+ * out: capacity rows.
  * With scale NULL, out has dtype. Else out is int8 and scale fp32[capacity] (written), and the rows
  * are quantised as by hccl_moe_quantize.
  * Its gradient is hccl_moe_combine without weights.
@@ -605,11 +608,11 @@ hcclResult_t hccl_moe_combine_backward(hcclComm_t comm, const void* grad, size_t
 
 /*
  * Rows to 8-bit codes: codes[i, c] = the whole number nearest to v * (1 / m * 127), ties to even, scale[i] =
- * m / 127, with m = max_c |v| (quotients and products in fp32, each rounded to nearest). v = x[i, c], or with `gated`, where x
- * has 2 * cols columns, silu(x[i, c]) * x[i, cols + c] (in fp32, not rounded in between). A row whose
- * m is below 2^-119 has codes and scale 0; one with an infinity or NaN has codes 0 and that as its
- * scale, so that every product with it is NaN. limit (int64, device) may be NULL: only the first
- * *limit rows are read and written.
+ * m / 127, with m = max_c |v| (quotients and products in fp32, each rounded to nearest). v = x[i, c], or with
+ * `gated`, where x has 2 * cols columns, silu(x[i, c]) * x[i, cols + c] in fp32: off by at most
+ * (1.5 |x[i, c]| + 8) 2^-24 of itself, and 0 where x[i, c] is below -87. A row whose m is below 2^-119 has codes
+ * and scale 0; one with an infinity or NaN has codes 0 and that as its scale, so that every product with it is
+ * NaN. limit (int64, device) may be NULL: only the first *limit rows are read and written.
  */
 hcclResult_t hccl_moe_quantize(hcclComm_t comm, const void* x, size_t ldx, hcclDataType_t dtype, size_t rows,
                                size_t cols, int gated, const int64_t* limit, int8_t* codes, size_t ldq, float* scale,
@@ -617,7 +620,8 @@ hcclResult_t hccl_moe_quantize(hcclComm_t comm, const void* x, size_t ldx, hcclD
 
 /*
  * The experts' product: out[m, n] = scale[m] * weight_scale[e, n] * sum_k codes[m, k] * weights[e, n, k],
- * the sum exact in 32 bits (inner is at most 131 071), then one rounding to dtype.
+ * the sum exact in 32 bits (inner is at most 131 071), to fp32 and times each scale with a rounding there
+ * (3 of 2^-24), then one rounding to dtype.
  * codes: rows rows of inner; weights: experts * cols rows of inner (ldb apart).
  * offsets (int64[segments + 1], device, ascending): rows [offsets[s], offsets[s + 1]) are segment
  * s's and use expert s % experts, so that the rows that an exchange brought in, ordered by source and
