@@ -518,8 +518,8 @@ typedef enum { hcclScoreSoftmax = 0, hcclScoreSigmoid = 1 } hcclScore_t;
  * index, of groups and of experts. Where fewer are left, the last choices are -1 with weight 0.
  * weight_k = scale * s_{e_k}, or with renormalize scale * s_{e_k} / sum_j s_{e_j} (0 if that sum is).
  * Scores below 2^-126 count as 0, but renormalised weights, and their gradient, are taken relative to
- * the greatest logit among the chosen, however small the scores are; only where that logit is below
- * -708 are all of a sigmoid's 0, as under a mask by a great negative number.
+ * the greatest logit among the chosen, however small the scores are (shares below 2^-102 may be 0); only
+ * where that logit is below -708 are all of a sigmoid's 0, as under a mask by a great negative number.
  * With d a logit's distance from the greatest (softmax) or from 0 (sigmoid), its score is off by at most
  * (2.5 |d| + 48) 2^-24 of itself: an exponential is one of base 2, of a product that is rounded once.
  */

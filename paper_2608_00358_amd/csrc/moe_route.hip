@@ -68,17 +68,18 @@ struct Exponential {
 // (0 at -inf)
 __device__ __forceinline__ float sigmoid(float l) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-l * kLog2e)); }
 
-// What the weights of a token's choices are shares by, once they are renormalised: the scores, without a factor
-// that they have in common. The greatest logit m among the chosen has none too small for 32 bits: a softmax's
-// are e^(l - m), and a sigmoid's, e^l / (1 + e^l), are e^(l - m) s(-l) where m is below 0. Sigmoids below e^-708, the
-// least normal number of 64 bits, are 0 all the same: a mask by a great negative number leaves nothing to share.
-// A lane has one choice's logit, -inf without one.
-constexpr float kNoScore = -708.0f;
+// Sigmoids of a token's choices (a lane has one choice's logit, -inf without one), for shares of their sum. Where the
+// sum r is small, some or all of them may be too small for 32 bits, and 1 / r too great; so there they are taken without a
+// factor that they have in common: e^l / (1 + e^l) = e^m e^(l - m) s(-l), m the greatest logit. (Above 2^-24 a share that
+// is lost is below 2^-102.) Below e^-708, the least normal number of 64 bits, they are 0 all the same: a mask by a
+// great negative number leaves nothing to share. The branch is a wave's, the choice between the two each token's.
+constexpr float kSmallSum = 0x1p-24f, kNoScore = -708.0f;
 template <int L>
-__device__ __forceinline__ float share(float logit, bool of_sigmoid) {
-    const float m = max_lanes<L>(logit), u = Exponential(m)(logit);
-    if (!of_sigmoid) return u;
-    return m < kNoScore ? 0.0f : m < 0.0f ? u * sigmoid(-logit) : sigmoid(logit);
+__device__ __forceinline__ void small_sigmoids(float logit, float& u, float& r) {
+    if (!__ballot(r < kSmallSum)) return;
+    const float m = max_lanes<L>(logit), v = m < kNoScore ? 0.0f : Exponential(m)(logit) * sigmoid(-logit), sum = sum_lanes<L>(v);
+    u = r < kSmallSum ? v : u;
+    r = r < kSmallSum ? sum : r;
 }
 
 // A 16-bit float widened to 32 bits has its 13 lowest bits free: the order of the float as an unsigned
@@ -247,10 +248,11 @@ __global__ __launch_bounds__(kRouteThreads) void hccl_moe_route_kernel(RouteArgs
     }
     float w = score(logit);
     if (a.renormalize) {
-        // Where the greatest logit of all need not be among the chosen (a bias, groups by two values), and with
-        // sigmoids anyway, the chosen scores may all be too small for 32 bits; their shares are not.
-        if (a.sigmoid || a.whole_sum) w = share<L>(logit, a.sigmoid);
-        const float sum = sum_lanes<L>(w);
+        // Where the greatest logit of all need not be among the chosen (a bias, groups by two values) their
+        // scores may all be too small for 32 bits; their shares are not, by the greatest logit among them.
+        if (!a.sigmoid && a.whole_sum) w = Exponential(max_lanes<L>(logit))(logit);
+        float sum = sum_lanes<L>(w);
+        if (a.sigmoid) small_sigmoids<L>(logit, w, sum);
         w = sum > 0.0f ? w / sum : 0.0f;
     }
     if (on && sub < a.top_k) {
@@ -311,18 +313,19 @@ __global__ __launch_bounds__(kRouteThreads) void hccl_moe_route_backward_kernel(
         for (int j = 0; j < N; ++j) l[j] *= inv;
         common = sum_lanes<L>(g * (exponential(logit) * inv));
     } else {
-        // The quotients by r are taken of the scores, not of the gradients: a share p_k = u_k / r is at most 1 where
-        // 1 / r may be beyond 32 bits. 1 - s = s(-l), without its cancellation.
-        float d = 1.0f;
+        // 1 - s = s(-l), without its cancellation. (0 at -inf)
+        float u = sigmoid(logit), d = u, slope = a.sigmoid ? sigmoid(-logit) : 1.0f;
+        if (!a.sigmoid) u = Exponential(max_lanes<L>(logit))(logit);
         if (a.renormalize) {
-            const float u = share<L>(logit, a.sigmoid), r = sum_lanes<L>(u);
-            const float p = r > 0.0f ? u / r : 0.0f;
-            g = (g - sum_lanes<L>(g * p)) * p;
-        } else {
-            d = sigmoid(logit);  // (0 at -inf)
+            float r = sum_lanes<L>(u), mean = sum_lanes<L>(g * u);
+            if (a.sigmoid && __ballot(r < kSmallSum)) {
+                small_sigmoids<L>(logit, u, r);
+                mean = sum_lanes<L>(g * u);
+            }
+            d = r > 0.0f ? u / r : 0.0f;
+            g = r > 0.0f ? g - mean / r : 0.0f;
         }
-        if (a.sigmoid) d *= sigmoid(-logit);
-        g *= d;
+        g *= d * slope;
     }
     if (some) atomicAdd(&part[mine], g);  // (a router names an expert once)
     __syncthreads();
