@@ -1,17 +1,18 @@
 // moe_product.hip -- the experts' product in 8-bit integers:
 //   out[m, n] = a_scale[m] * b_scale[e, n] * sum_k a[m, k] b[e, n, k],   e the expert of row m's segment
-// on the matrix instructions for 8-bit integers, with whole sums in 32 bits (exact: at most
-// 131 071 products of at most 2^14), which become 32-bit floats only for the scales (a sum above 2^24 is rounded
-// there, by 2^-24 of itself at most, as each of the two products with the scales is). The rows of a segment follow each other; where segments begin is
-// read on the device, so the grid is sized for the worst case and surplus blocks end at once.
+// on the matrix instructions for 8-bit integers, with whole sums in 32 bits (exact: at most 131 071 products of at
+// most 2^14), which become 32-bit floats only for the scales (a sum above 2^24 is rounded there, by 2^-24 of itself at
+// most, as each of the two products with the scales is). The rows of a segment follow each other; where segments begin
+// is read on the device, so the grid is sized for the worst case and surplus blocks end at once. A tile holds rows of one
+// segment: where several segments use one expert (rows of several sources), its weights are read for each of them.
 //
 // The weights are the instruction's first operand: a lane then holds neighbouring columns of one row.
 // The order of k within an instruction does not matter as long as both operands have the same.
 //
-// Bounds: with few rows a segment, the weights' bytes (256 rows over 64 experts of 2048 x 2048: 268 MB in 43 us,
-// 6.3 TB/s, the rate of a large copy); with many, power and the loads from L2 to LDS (8192 x 8192 x 8192 in
-// 475-490 us, 2.25-2.3 POPS, where a library product takes 518 us; in long products the matrix units alone, without
-// any load, bring the clock down to 1.9 GHz, and the whole kernel to 1.7).
+// Bounds: with few rows a segment, the weights' bytes (256 rows over 64 experts of 2048 x 2048, of which about 53 have
+// a row: 235 MB in 42 us, 5.6 TB/s, where a large copy reaches 6.2); with many, power and the loads from L2 to LDS
+// (8192 x 8192 x 8192 in 475-490 us, 2.25-2.3 POPS, where a library product takes 518 us; in long products the matrix
+// units alone, without any load, bring the clock down to 1.9 GHz, and the whole kernel to 1.7).
 #include <type_traits>
 
 #include "moe_device.h"
@@ -510,6 +511,10 @@ hipError_t launch_few(const ProductArgs& a, hipStream_t s) {
 // no more), and of 64, 32 and 16 columns the most that leave every CU a block, with k shared out over more waves
 // the fewer columns there are (1 x 4096 x 4096: 16 columns 5.4 us, 32 columns 7.0, 64 columns 10.5;
 // 256 x 2048 x 2048 x 64: 80, 48 and 46 us).
+// All of this goes by the rows of the array, which are known on the host; where it has room for more rows than its
+// segments hold, the tiles are those of the room.
+// Short inner sizes leave most of 16 waves without k, at no cost (inner 64-1024, 16 against 4 waves, both within 0.1 us:
+// 9 x 300 columns 3.6-3.9 us, 505 x 185 3.9 us, 100 x 512 over 16 experts 3.9-4.1 us).
 template <int DT>
 hipError_t product_type(const ProductArgs& a, int cus, hipStream_t s) {
     const uint64_t each = a.rows / a.segments, spread = a.offsets ? (a.rows < a.segments ? a.rows : a.segments) : 0;
