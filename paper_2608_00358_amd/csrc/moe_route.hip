@@ -4,9 +4,9 @@
 // routes 64 / L tokens and nothing is exchanged beyond those lanes. One round of the top k is a
 // maximum over N registers and L lanes; the maximum of the exponentials' argument, their sum and the
 // chosen weights' sum are reductions over the same lanes. All of it is held in 32 bits.
-// Bound by launch and latency up to thousands of tokens (one token of 64 experts 2.2-2.5 us, 4 099 of 192 fp32 with
-// bias and groups 5.7-7.0 us), then by the arithmetic of the rounds: 32 768 tokens x 128 bf16 experts, top 8, 6.5 us
-// for 10.5 MB, their gradient 4.7-5.6 us for 18.9 MB, also without renormalisation (512 experts 14 us for 69 MB);
+// Bound by launch and latency up to thousands of tokens (one token of 64 experts 2.1-2.5 us, 4 099 of 192 fp32 with
+// bias and groups 5.7-7.2 us), then by the arithmetic of the rounds: 32 768 tokens x 128 bf16 experts, top 8, 5.6-7.2 us
+// for 10.5 MB, their gradient 4.7-5.7 us for 18.9 MB, also without renormalisation (512 experts 14 us for 69 MB);
 // 32 768 x 256 fp32 sigmoids with a bias 21 us for 36 MB: two reductions a round where 16-bit logits have one.
 //
 //   s_e = exp(l_e - max l) / sum, or 1 / (1 + exp(-l_e))
