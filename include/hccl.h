@@ -635,6 +635,55 @@ hcclResult_t hccl_moe_product(hcclComm_t comm, const int8_t* codes, size_t lda, 
                               size_t experts, const int64_t* offsets, size_t segments, void* out, size_t ldo,
                               hcclDataType_t dtype, void* stream);
 
+/*
+ * Microscaled 4-bit floats. A row's elements lie two a byte, the first of a pair in the lower half: codes 0 to 7 are
+ * 0, 0.5, 1, 1.5, 2, 3, 4 and 6, codes 8 to 15 their negatives. Every 32 neighbours of a row, the last block maybe fewer,
+ * have a scale byte b in the row's scales: element = code * 2^(b - 127); b = 255 is no number, and such elements are NaN.
+ * A row of n elements has (n + 1) / 2 bytes of codes and (n + 31) / 32 scales; the upper half of an odd row's last byte
+ * is written as 0 and never counts. Strides of codes and scales are in bytes, and any alignment is taken.
+ */
+
+/*
+ * Rows to microscaled 4-bit floats. v = x[i, c], or with `gated`, where x has 2 * cols columns,
+ * silu(x[i, c]) * x[i, cols + c] in fp32, with the error that hccl_moe_quantize states. A block whose greatest magnitude
+ * is m has the least scale 2^s, s >= -127, with m < 7 * 2^s, and codes are the values nearest to v / 2^s, ties to the even
+ * code; a zero keeps its sign. A block with an infinity or NaN has scale 255 and codes 0. limit (int64, device) may be
+ * NULL: only the first *limit rows are read and written.
+ */
+hcclResult_t hccl_moe_quantize_mx(hcclComm_t comm, const void* x, size_t ldx, hcclDataType_t dtype, size_t rows,
+                                  size_t cols, int gated, const int64_t* limit, uint8_t* codes, size_t ldq,
+                                  uint8_t* scale, size_t lds, void* stream);
+
+/*
+ * Dispatch into 4 bits: rows row[t * top_k + k] of codes and scale are token t's, quantised as by hccl_moe_quantize_mx;
+ * rows outside 0 .. capacity - 1 are skipped, and rows that none names keep what they held. No two routes may have the
+ * same row. x: tokens rows of cols; codes and scale: capacity rows.
+ */
+hcclResult_t hccl_moe_dispatch_mx(hcclComm_t comm, const void* x, size_t ldx, hcclDataType_t dtype, size_t tokens,
+                                  size_t cols, const int32_t* row, uint32_t top_k, uint8_t* codes, size_t ldq,
+                                  uint8_t* scale, size_t lds, size_t capacity, void* stream);
+
+/*
+ * Rows of microscaled 4-bit floats to dtype: out[i, c] = code * 2^(b - 127) in fp32, exact where fp32 holds it, then one
+ * rounding to dtype. limit as above: rows from *limit on are left as they are.
+ */
+hcclResult_t hccl_moe_dequantize_mx(hcclComm_t comm, const uint8_t* codes, size_t ldq, const uint8_t* scale, size_t lds,
+                                    size_t rows, size_t cols, const int64_t* limit, void* out, size_t ldo,
+                                    hcclDataType_t dtype, void* stream);
+
+/*
+ * The experts' product in microscaled 4-bit floats: out[m, n] = sum_k a[m, k] * b[e, n, k], a the values of codes and
+ * scale, b those of weights and weight_scale (experts * cols rows of inner, ldb and ldsb bytes apart). Segments, experts
+ * and offsets are hccl_moe_product's. The sum over a block of 32 is exact; blocks are added up in fp32, in an order
+ * that depends on sizes and alignment alone, with at most one rounding each, of 2^-23 of the magnitudes added so far,
+ * then one rounding to dtype. A product of a row and a column with a scale of 255 in either is NaN.
+ */
+hcclResult_t hccl_moe_product_mx(hcclComm_t comm, const uint8_t* codes, size_t lda, const uint8_t* scale, size_t ldsa,
+                                 size_t rows, size_t inner, const uint8_t* weights, size_t ldb,
+                                 const uint8_t* weight_scale, size_t ldsb, size_t cols, size_t experts,
+                                 const int64_t* offsets, size_t segments, void* out, size_t ldo, hcclDataType_t dtype,
+                                 void* stream);
+
 #ifdef __cplusplus
 }
 #endif

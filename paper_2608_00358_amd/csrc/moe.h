@@ -75,6 +75,26 @@ struct QuantizeArgs {
     uint32_t top_k;
 };
 
+// Rows to microscaled 4-bit floats, `blocks` blocks of 32 a row: row t goes to the rows that `row` names, or to row t.
+struct QuantizeMxArgs {
+    const void* x;
+    const int32_t* row;
+    const int64_t* limit;  // NULL, or the number of rows that hold anything
+    uint8_t* codes;
+    uint8_t* scale;
+    uint64_t rows, cols, ldx, ldq, lds, capacity;
+    uint32_t top_k, blocks;
+};
+
+struct DequantizeMxArgs {
+    const uint8_t* codes;
+    const uint8_t* scale;
+    const int64_t* limit;
+    void* out;
+    uint64_t rows, cols, ldq, lds, ldo;
+    uint32_t blocks;
+};
+
 struct CombineArgs {
     const void* z;
     const int32_t* row;
@@ -95,6 +115,34 @@ struct CombineBackwardArgs {
     uint32_t top_k;
 };
 
+struct ProductMxArgs {
+    const uint8_t* a;
+    const uint8_t* a_scale;
+    const uint8_t* b;
+    const uint8_t* b_scale;
+    const int64_t* offsets;  // NULL: one segment with every row
+    void* out;
+    uint64_t rows, lda, ldas, ldb, ldbs, ldo;
+    uint32_t inner, cols, segments, experts;
+    uint32_t type;  // hcclDataType_t of the results
+};
+
+// A whole layer for few tokens. Row f of an expert's w_in is a gate's, row inner + f the up's.
+struct LayerMxArgs {
+    const void* x;
+    const uint8_t* w_in;
+    const uint8_t* w_in_scale;
+    const uint8_t* w_out;
+    const uint8_t* w_out_scale;
+    const int32_t* index;  // as routing wrote them
+    const float* weight;
+    void* out;
+    uint16_t* hidden;  // [route][plane][inner padded to 32], bf16 planes whose sum is the hidden value
+    uint64_t ldx, ld_in, ld_in_scale, ld_out, ld_out_scale, ldo;
+    uint32_t tokens, top_k, cols, inner;
+    uint32_t first, held;  // experts whose weights are there
+};
+
 struct ProductArgs {
     const int8_t* a;
     const float* a_scale;
@@ -113,6 +161,10 @@ hipError_t launch_dispatch(const DispatchArgs& a, hcclDataType_t dt, hipStream_t
 hipError_t launch_quantize(const QuantizeArgs& a, hcclDataType_t dt, bool gated, hipStream_t s);
 hipError_t launch_combine(const CombineArgs& a, hcclDataType_t dt, hipStream_t s);
 hipError_t launch_combine_backward(const CombineBackwardArgs& a, hcclDataType_t dt, hipStream_t s);
+hipError_t launch_quantize_mx(const QuantizeMxArgs& a, hcclDataType_t dt, bool gated, hipStream_t s);
+hipError_t launch_dequantize_mx(const DequantizeMxArgs& a, hcclDataType_t dt, hipStream_t s);
+hipError_t launch_product_mx(const ProductMxArgs& a, int cus, hipStream_t s);
+hipError_t launch_layer_mx(const LayerMxArgs& a, hcclDataType_t dt, hipStream_t s);
 hipError_t launch_product(const ProductArgs& a, hcclDataType_t dt, int cus, hipStream_t s);
 
 }  // namespace hccl

@@ -18,6 +18,7 @@ namespace {
 constexpr uint64_t kMaxCount = 0x7fffffffull;  // rows and routes are numbered in 32 bits, -1 is none
 constexpr uint64_t kMaxBytes = 1ull << 62;
 constexpr uint32_t kMaxInner = 131071;         // * 2^14 < 2^31: sums of products never wrap
+constexpr uint64_t kMxBlock = 32;               // elements of a row that share a scale
 
 // Rows of an array: `rows` of `width` bytes, `pitch` bytes apart.
 struct Rows2D {
@@ -81,6 +82,10 @@ private:
 
 uint64_t float_size(hcclDataType_t dt) { return dt == hcclFp32 ? 4 : 2; }
 bool is_float(hcclDataType_t dt) { return dt == hcclBf16 || dt == hcclFp16 || dt == hcclFp32; }
+
+// A row of `cols` 4-bit floats: its bytes, two elements each, and its scales'.
+uint64_t mx_bytes(uint64_t cols) { return (cols + 1) / 2; }
+uint64_t mx_blocks(uint64_t cols) { return (cols + kMxBlock - 1) / kMxBlock; }
 
 template <typename F>
 hcclResult_t enqueue(const Check& c, F launch) {
@@ -392,6 +397,141 @@ hcclResult_t hccl_moe_quantize(hcclComm_t comm, const void* x, size_t ldx, hcclD
         a.capacity = rows;
         a.top_k = 1;
         return enqueue(c, [&] { return launch_quantize(a, dtype, gated != 0, (hipStream_t)stream); });
+    });
+}
+
+hcclResult_t hccl_moe_quantize_mx(hcclComm_t comm, const void* x, size_t ldx, hcclDataType_t dtype, size_t rows,
+                                  size_t cols, int gated, const int64_t* limit, uint8_t* codes, size_t ldq,
+                                  uint8_t* scale, size_t lds, void* stream) {
+    return guarded([&] {
+        Check c(comm);
+        c.that(is_float(dtype), "rows must be bf16, fp16 or fp32")
+            .that(rows <= kMaxCount, "more than 2^31 - 1 rows")
+            .that(cols <= kMaxCount, "more than 2^31 - 1 columns")
+            .rows(x, rows, gated ? 2 * cols : cols, ldx, float_size(dtype), false, "x")
+            .rows(codes, rows, mx_bytes(cols), ldq, 1, true, "codes")
+            .rows(scale, rows, mx_blocks(cols), lds, 1, true, "scale");
+        if (limit) c.list(limit, 1, 8, false, "limit");
+        if (!c.ok() || rows == 0 || cols == 0) return c.result();
+        QuantizeMxArgs a{};
+        a.x = x;
+        a.limit = limit;
+        a.codes = codes;
+        a.scale = scale;
+        a.rows = rows;
+        a.cols = cols;
+        a.ldx = ldx;
+        a.ldq = ldq;
+        a.lds = lds;
+        a.capacity = rows;
+        a.top_k = 1;
+        a.blocks = (uint32_t)mx_blocks(cols);
+        return enqueue(c, [&] { return launch_quantize_mx(a, dtype, gated != 0, (hipStream_t)stream); });
+    });
+}
+
+hcclResult_t hccl_moe_dispatch_mx(hcclComm_t comm, const void* x, size_t ldx, hcclDataType_t dtype, size_t tokens,
+                                  size_t cols, const int32_t* row, uint32_t top_k, uint8_t* codes, size_t ldq,
+                                  uint8_t* scale, size_t lds, size_t capacity, void* stream) {
+    return guarded([&] {
+        Check c(comm);
+        c.that(is_float(dtype), "rows must be bf16, fp16 or fp32");
+        check_routes(c, tokens, top_k)
+            .that(capacity <= kMaxCount, "capacity is more than 2^31 - 1 rows")
+            .that(cols <= kMaxCount, "more than 2^31 - 1 columns")
+            .rows(x, tokens, cols, ldx, float_size(dtype), false, "x")
+            .list(row, tokens * top_k, 4, false, "row")
+            .rows(codes, capacity, mx_bytes(cols), ldq, 1, true, "codes")
+            .rows(scale, capacity, mx_blocks(cols), lds, 1, true, "scale");
+        if (!c.ok() || tokens == 0 || capacity == 0 || cols == 0) return c.result();
+        QuantizeMxArgs a{};
+        a.x = x;
+        a.row = row;
+        a.codes = codes;
+        a.scale = scale;
+        a.rows = tokens;
+        a.cols = cols;
+        a.ldx = ldx;
+        a.ldq = ldq;
+        a.lds = lds;
+        a.capacity = capacity;
+        a.top_k = top_k;
+        a.blocks = (uint32_t)mx_blocks(cols);
+        return enqueue(c, [&] { return launch_quantize_mx(a, dtype, false, (hipStream_t)stream); });
+    });
+}
+
+hcclResult_t hccl_moe_dequantize_mx(hcclComm_t comm, const uint8_t* codes, size_t ldq, const uint8_t* scale, size_t lds,
+                                    size_t rows, size_t cols, const int64_t* limit, void* out, size_t ldo,
+                                    hcclDataType_t dtype, void* stream) {
+    return guarded([&] {
+        Check c(comm);
+        c.that(is_float(dtype), "rows must be bf16, fp16 or fp32")
+            .that(rows <= kMaxCount, "more than 2^31 - 1 rows")
+            .that(cols <= kMaxCount, "more than 2^31 - 1 columns")
+            .rows(codes, rows, mx_bytes(cols), ldq, 1, false, "codes")
+            .rows(scale, rows, mx_blocks(cols), lds, 1, false, "scale")
+            .rows(out, rows, cols, ldo, float_size(dtype), true, "out");
+        if (limit) c.list(limit, 1, 8, false, "limit");
+        if (!c.ok() || rows == 0 || cols == 0) return c.result();
+        DequantizeMxArgs a{};
+        a.codes = codes;
+        a.scale = scale;
+        a.limit = limit;
+        a.out = out;
+        a.rows = rows;
+        a.cols = cols;
+        a.ldq = ldq;
+        a.lds = lds;
+        a.ldo = ldo;
+        a.blocks = (uint32_t)mx_blocks(cols);
+        return enqueue(c, [&] { return launch_dequantize_mx(a, dtype, (hipStream_t)stream); });
+    });
+}
+
+hcclResult_t hccl_moe_product_mx(hcclComm_t comm, const uint8_t* codes, size_t lda, const uint8_t* scale, size_t ldsa,
+                                 size_t rows, size_t inner, const uint8_t* weights, size_t ldb,
+                                 const uint8_t* weight_scale, size_t ldsb, size_t cols, size_t experts,
+                                 const int64_t* offsets, size_t segments, void* out, size_t ldo, hcclDataType_t dtype,
+                                 void* stream) {
+    return guarded([&] {
+        Check c(comm);
+        c.that(is_float(dtype), "the result must be bf16, fp16 or fp32")
+            .that(rows <= kMaxCount, "more than 2^31 - 1 rows")
+            .that(cols <= kMaxCount, "more than 2^31 - 1 columns")
+            .that(inner <= kMaxCount, "inner size above 2^31 - 1")
+            .that(experts >= 1 && experts <= kMaxCount, "experts must be 1 or more")
+            .that(offsets ? segments >= 1 && segments <= kMaxCount : true, "segments must be 1 or more")
+            .that(offsets ? segments % (experts ? experts : 1) == 0 : experts == 1, offsets ? "segments must be a multiple of the experts" : "several experts need offsets");
+        if (!c.ok()) return c.result();
+        c.that(experts <= kMaxBytes / (cols ? cols : 1), "array too large: weights");
+        if (!c.ok()) return c.result();
+        c.rows(codes, rows, mx_bytes(inner), lda, 1, false, "codes")
+            .rows(scale, rows, mx_blocks(inner), ldsa, 1, false, "scale")
+            .rows(weights, experts * cols, mx_bytes(inner), ldb, 1, false, "weights")
+            .rows(weight_scale, experts * cols, mx_blocks(inner), ldsb, 1, false, "weight_scale")
+            .rows(out, rows, cols, ldo, float_size(dtype), true, "out");
+        if (offsets) c.list(offsets, segments + 1, 8, false, "offsets");
+        if (!c.ok() || rows == 0 || cols == 0) return c.result();
+        ProductMxArgs a{};
+        a.a = codes;
+        a.a_scale = scale;
+        a.b = weights;
+        a.b_scale = weight_scale;
+        a.offsets = offsets;
+        a.out = out;
+        a.rows = rows;
+        a.lda = lda;
+        a.ldas = ldsa;
+        a.ldb = ldb;
+        a.ldbs = ldsb;
+        a.ldo = ldo;
+        a.inner = (uint32_t)inner;
+        a.cols = (uint32_t)cols;
+        a.segments = offsets ? (uint32_t)segments : 1u;
+        a.experts = (uint32_t)experts;
+        a.type = dtype;
+        return enqueue(c, [&] { return launch_product_mx(a, api_cus(comm), (hipStream_t)stream); });
     });
 }
 

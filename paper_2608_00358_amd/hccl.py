@@ -34,6 +34,7 @@ EXPORTS = [
     "hccl_allreduce_noalloc", "hccl_comm_trace", "hccl_comm_program_image",
     "hccl_router_init", "hccl_moe_route", "hccl_moe_route_backward", "hccl_moe_plan_bytes", "hccl_moe_plan",
     "hccl_moe_dispatch", "hccl_moe_combine", "hccl_moe_combine_backward", "hccl_moe_quantize", "hccl_moe_product",
+    "hccl_moe_quantize_mx", "hccl_moe_dispatch_mx", "hccl_moe_dequantize_mx", "hccl_moe_product_mx",
 ]
 CMPS = {"eq": 0, "ne": 1, "ge": 2, "gt": 3, "le": 4, "lt": 5}
 
@@ -142,6 +143,10 @@ def load(path: str = LIB_PATH):
     lib.hccl_moe_combine_backward.argtypes = [vp, vp, sz, i32, sz, sz, vp, sz, sz, vp, u32, vp, vp, sz, vp, vp]
     lib.hccl_moe_quantize.argtypes = [vp, vp, sz, i32, sz, sz, i32, vp, vp, sz, vp, vp]
     lib.hccl_moe_product.argtypes = [vp, vp, sz, vp, sz, sz, vp, sz, vp, sz, sz, vp, sz, vp, sz, i32, vp]
+    lib.hccl_moe_quantize_mx.argtypes = [vp, vp, sz, i32, sz, sz, i32, vp, vp, sz, vp, sz, vp]
+    lib.hccl_moe_dispatch_mx.argtypes = [vp, vp, sz, i32, sz, sz, vp, u32, vp, sz, vp, sz, sz, vp]
+    lib.hccl_moe_dequantize_mx.argtypes = [vp, vp, sz, vp, sz, sz, sz, vp, vp, sz, i32, vp]
+    lib.hccl_moe_product_mx.argtypes = [vp, vp, sz, vp, sz, sz, sz, vp, sz, vp, sz, sz, sz, vp, sz, vp, sz, i32, vp]
     for name in EXPORTS:
         if name not in ("hccl_get_last_error", "hccl_result_string"):
             getattr(lib, name).restype = res
@@ -494,6 +499,66 @@ def _call_moe_product(comm, codes, scale, weights, weight_scale, out, offsets=No
                                      _dtype_code(out.dtype), _stream_handle(stream))
 
 
+def _rows_mx(codes, scale, rows, cols, what):
+    """Addresses and row strides of `rows` rows of `cols` microscaled 4-bit floats: packed codes and scale bytes."""
+    for t, name in ((codes, what), (scale, what + "'s scales")):
+        if str(t.dtype) != "torch.uint8":
+            raise ValueError(f"{name} must be uint8, not {t.dtype}")
+    return (*_rows(codes, rows, (cols + 1) // 2, what), *_rows(scale, rows, (cols + 31) // 32, what + "'s scales"))
+
+
+def _weights_mx(codes, scale, cols, what):
+    """The same for weights (experts, rows, bytes), whose experts follow each other at one stride; and experts and rows."""
+    out = []
+    for t, n, name in ((codes, (cols + 1) // 2, what), (scale, (cols + 31) // 32, what + "'s scales")):
+        if str(t.dtype) != "torch.uint8":
+            raise ValueError(f"{name} must be uint8, not {t.dtype}")
+        if t.dim() != 3 or t.shape[:2] != codes.shape[:2] or t.shape[2] != n:
+            raise ValueError(f"{name} must have shape (experts, rows, {n}), not {tuple(t.shape)}")
+        E, N = t.shape[:2]
+        ld = t.stride(1) if N > 1 else t.stride(0) if E > 1 else n
+        if (n > 1 and t.stride(2) != 1) or (E > 1 and t.stride(0) != N * ld):
+            raise ValueError(f"the rows of {name} must be one distance apart")
+        out += [t.data_ptr(), ld]
+    return (*out, *codes.shape[:2])
+
+
+def _call_moe_quantize_mx(comm, x, codes, scale, gated=False, limit=None, stream=None):
+    R, C = x.shape
+    if gated and C % 2:
+        raise ValueError("gated rows must have an even number of columns")
+    C = C // 2 if gated else C
+    at, ldx = _rows(x, R, x.shape[1], "x")
+    to, ldq, scales, lds = _rows_mx(codes, scale, R, C, "codes")
+    return load().hccl_moe_quantize_mx, (comm, at, ldx, _dtype_code(x.dtype), R, C, int(bool(gated)), _list(limit, 1, "int64", "limit"),
+                                         to, ldq, scales, lds, _stream_handle(stream))
+
+
+def _call_moe_dispatch_mx(comm, x, row, codes, scale, stream=None):
+    (T, C), R, K = x.shape, codes.shape[0], row.shape[1]
+    at, ldx = _rows(x, T, C, "x")
+    to, ldq, scales, lds = _rows_mx(codes, scale, R, C, "codes")
+    return load().hccl_moe_dispatch_mx, (comm, at, ldx, _dtype_code(x.dtype), T, C, _list(row, T * K, "int32", "row"), K,
+                                         to, ldq, scales, lds, R, _stream_handle(stream))
+
+
+def _call_moe_dequantize_mx(comm, codes, scale, out, limit=None, stream=None):
+    R, C = out.shape
+    to, ldo = _rows(out, R, C, "out")
+    return load().hccl_moe_dequantize_mx, (comm, *_rows_mx(codes, scale, R, C, "codes"), R, C, _list(limit, 1, "int64", "limit"),
+                                           to, ldo, _dtype_code(out.dtype), _stream_handle(stream))
+
+
+def _call_moe_product_mx(comm, codes, scale, weights, weight_scale, out, inner, offsets=None, stream=None):
+    R = codes.shape[0]
+    b, ldb, scales, ldsb, E, N = _weights_mx(weights, weight_scale, inner, "weights")
+    to, ldo = _rows(out, R, N, "out")
+    S = 0 if offsets is None else offsets.numel() - 1
+    return load().hccl_moe_product_mx, (comm, *_rows_mx(codes, scale, R, inner, "codes"), R, inner, b, ldb, scales, ldsb, N, E,
+                                        None if offsets is None else _list(offsets, S + 1, "int64", "offsets"), S, to, ldo,
+                                        _dtype_code(out.dtype), _stream_handle(stream))
+
+
 def hccl_moe_route(comm, router, logits, index, weight, bias=None, mask=None, stream=None) -> None:
     fn, a = _call_moe_route(comm, router, logits, index, weight, bias, mask, stream)
     _check(fn(*a))
@@ -533,6 +598,28 @@ def hccl_moe_quantize(comm, x, codes, scale, gated=False, limit=None, stream=Non
 def hccl_moe_product(comm, codes, scale, weights, weight_scale, out, offsets=None, stream=None) -> None:
     """codes (rows, inner), weights (experts, columns, inner)."""
     fn, a = _call_moe_product(comm, codes, scale, weights, weight_scale, out, offsets, stream)
+    _check(fn(*a))
+
+
+def hccl_moe_quantize_mx(comm, x, codes, scale, gated=False, limit=None, stream=None) -> None:
+    """codes (rows, ceil(columns / 2)) and scale (rows, ceil(columns / 32)) are uint8."""
+    fn, a = _call_moe_quantize_mx(comm, x, codes, scale, gated, limit, stream)
+    _check(fn(*a))
+
+
+def hccl_moe_dispatch_mx(comm, x, row, codes, scale, stream=None) -> None:
+    fn, a = _call_moe_dispatch_mx(comm, x, row, codes, scale, stream)
+    _check(fn(*a))
+
+
+def hccl_moe_dequantize_mx(comm, codes, scale, out, limit=None, stream=None) -> None:
+    fn, a = _call_moe_dequantize_mx(comm, codes, scale, out, limit, stream)
+    _check(fn(*a))
+
+
+def hccl_moe_product_mx(comm, codes, scale, weights, weight_scale, out, inner, offsets=None, stream=None) -> None:
+    """codes (rows, bytes) of `inner` elements a row, weights (experts, columns, bytes), each with its scales."""
+    fn, a = _call_moe_product_mx(comm, codes, scale, weights, weight_scale, out, inner, offsets, stream)
     _check(fn(*a))
 
 
@@ -731,6 +818,34 @@ class Comm:
 
     def bind_moe_product(self, codes, scale, weights, weight_scale, out, offsets=None, stream=None):
         return _bound_operator(self, _call_moe_product(self.handle, codes, scale, weights, weight_scale, out, offsets, stream),
+                               codes, scale, weights, weight_scale, out, offsets)
+
+    def moe_quantize_mx(self, x, codes, scale, gated=False, limit=None, stream=None):
+        hccl_moe_quantize_mx(self.handle, x, codes, scale, gated, limit, stream)
+
+    def bind_moe_quantize_mx(self, x, codes, scale, gated=False, limit=None, stream=None):
+        return _bound_operator(self, _call_moe_quantize_mx(self.handle, x, codes, scale, gated, limit, stream),
+                               x, codes, scale, limit)
+
+    def moe_dispatch_mx(self, x, row, codes, scale, stream=None):
+        hccl_moe_dispatch_mx(self.handle, x, row, codes, scale, stream)
+
+    def bind_moe_dispatch_mx(self, x, row, codes, scale, stream=None):
+        return _bound_operator(self, _call_moe_dispatch_mx(self.handle, x, row, codes, scale, stream),
+                               x, row, codes, scale)
+
+    def moe_dequantize_mx(self, codes, scale, out, limit=None, stream=None):
+        hccl_moe_dequantize_mx(self.handle, codes, scale, out, limit, stream)
+
+    def bind_moe_dequantize_mx(self, codes, scale, out, limit=None, stream=None):
+        return _bound_operator(self, _call_moe_dequantize_mx(self.handle, codes, scale, out, limit, stream),
+                               codes, scale, out, limit)
+
+    def moe_product_mx(self, codes, scale, weights, weight_scale, out, inner, offsets=None, stream=None):
+        hccl_moe_product_mx(self.handle, codes, scale, weights, weight_scale, out, inner, offsets, stream)
+
+    def bind_moe_product_mx(self, codes, scale, weights, weight_scale, out, inner, offsets=None, stream=None):
+        return _bound_operator(self, _call_moe_product_mx(self.handle, codes, scale, weights, weight_scale, out, inner, offsets, stream),
                                codes, scale, weights, weight_scale, out, offsets)
 
     def triggered(self, wait=None, done=None):

@@ -1,0 +1,135 @@
+"""Microscaled 4-bit operators without a GPU: what they refuse, and the 64-bit reference's own rules."""
+import inspect
+
+import numpy as np
+import pytest
+import torch
+
+import mx_reference as mx
+import paper_2608_00358_amd as H
+
+U8 = torch.uint8
+
+
+@pytest.fixture()
+def comm():
+    with H.Comm(4, device=H.NO_DEVICE) as c:
+        yield c
+
+
+def _u8(*shape):
+    return torch.zeros(shape, dtype=U8)
+
+
+def _refused(code, fn, *a, **kw):
+    with pytest.raises(H.HcclError) as e:
+        fn(*a, **kw)
+    assert e.value.code == code, str(e.value)
+
+
+def test_good_calls_pass_the_checks(comm):
+    for dt in (torch.bfloat16, torch.float16, torch.float32):
+        x = torch.zeros(6, 41, dtype=dt)
+        comm.moe_quantize_mx(x, _u8(6, 21), _u8(6, 2))
+        comm.moe_quantize_mx(torch.zeros(6, 82, dtype=dt), _u8(6, 21), _u8(6, 2), gated=True, limit=torch.zeros(1, dtype=torch.int64))
+        comm.moe_dispatch_mx(x, torch.zeros(6, 3, dtype=torch.int32), _u8(18, 30)[:, :21], _u8(18, 2))
+        comm.moe_dequantize_mx(_u8(6, 21), _u8(6, 2), x)
+        comm.moe_product_mx(_u8(6, 21), _u8(6, 2), _u8(3, 7, 21), _u8(3, 7, 2), torch.zeros(6, 7, dtype=dt), 41, offsets=torch.zeros(4, dtype=torch.int64))
+        comm.moe_product_mx(_u8(6, 21), _u8(6, 2), _u8(1, 7, 21), _u8(1, 7, 2), torch.zeros(6, 7, dtype=dt), 42)
+
+
+def test_refusals(comm):
+    lib, h = H.load(), comm.handle
+    A, B, C, D = 1 << 20, 1 << 24, 1 << 28, 1 << 30
+    ok = [h, A, 64, 0, 4, 64, 0, None, B, 32, C, 2, None]
+    assert lib.hccl_moe_quantize_mx(*ok) == 0
+
+    def bad(fn, args, **change):
+        args = list(args)
+        for k, v in change.items():
+            args[int(k[1:])] = v
+        assert fn(*args) == 1, change
+
+    q = lib.hccl_moe_quantize_mx
+    for change in (dict(_0=None), dict(_1=None), dict(_1=A + 1), dict(_2=63), dict(_3=3), dict(_4=1 << 31), dict(_5=1 << 31), dict(_6=1), dict(_7=4),
+                   dict(_8=None), dict(_9=31), dict(_10=None), dict(_11=1), dict(_8=A), dict(_10=A + 10), dict(_10=B + 5), dict(_7=B)):
+        bad(q, ok, **change)
+    ok = [h, A, 64, 0, 4, 64, D, 2, B, 32, C, 2, 8, None]
+    d = lib.hccl_moe_dispatch_mx
+    assert d(*ok) == 0
+    for change in (dict(_1=None), dict(_2=63), dict(_3=3), dict(_4=1 << 31), dict(_6=None), dict(_6=D + 2), dict(_7=0), dict(_7=33), dict(_8=None), dict(_9=31),
+                   dict(_10=None), dict(_11=1), dict(_12=1 << 31), dict(_8=A), dict(_8=D), dict(_10=B)):
+        bad(d, ok, **change)
+    ok = [h, B, 32, C, 2, 4, 64, None, A, 64, 0, None]
+    u = lib.hccl_moe_dequantize_mx
+    assert u(*ok) == 0
+    for change in (dict(_1=None), dict(_2=31), dict(_3=None), dict(_4=1), dict(_5=1 << 31), dict(_6=1 << 31), dict(_8=None), dict(_8=A + 1), dict(_9=63), dict(_10=3),
+                   dict(_8=B), dict(_8=C - 128), dict(_7=A)):
+        bad(u, ok, **change)
+    E = 1 << 32
+    ok = [h, A, 32, B, 2, 4, 64, C, 32, D, 2, 16, 2, E, 4, E + 4096, 16, 0, None]
+    p = lib.hccl_moe_product_mx
+    assert p(*ok) == 0
+    for change in (dict(_1=None), dict(_2=31), dict(_3=None), dict(_4=1), dict(_5=1 << 31), dict(_6=1 << 31), dict(_7=None), dict(_8=31), dict(_9=None), dict(_10=1),
+                   dict(_11=1 << 31), dict(_12=0), dict(_12=3), dict(_13=None), dict(_14=0), dict(_14=3), dict(_15=None), dict(_15=E + 4097), dict(_16=15), dict(_17=3),
+                   dict(_15=A), dict(_15=B), dict(_15=C), dict(_15=D), dict(_15=E)):
+        bad(p, ok, **change)
+
+
+def test_nothing_to_do_needs_no_arrays(comm):
+    lib, h = H.load(), comm.handle
+    assert lib.hccl_moe_quantize_mx(h, None, 0, 0, 0, 64, 0, None, None, 0, None, 0, None) == 0
+    assert lib.hccl_moe_quantize_mx(h, None, 0, 0, 4, 0, 0, None, None, 0, None, 0, None) == 0
+    assert lib.hccl_moe_dequantize_mx(h, None, 0, None, 0, 0, 64, None, None, 0, 0, None) == 0
+    assert lib.hccl_moe_product_mx(h, None, 0, None, 0, 0, 64, 1 << 20, 32, 1 << 24, 2, 16, 1, None, 0, None, 16, 0, None) == 0
+
+
+def test_the_binding_passes_on_nothing_that_a_call_could_write_beyond(comm):
+    x = torch.zeros(6, 41)
+    row, offsets = torch.zeros(6, 3, dtype=torch.int32), torch.zeros(4, dtype=torch.int64)
+    y = torch.zeros(6, 7)
+    w, ws = _u8(3, 7, 21), _u8(3, 7, 2)
+    for call in (lambda: comm.moe_quantize_mx(x, _u8(6, 20), _u8(6, 2)), lambda: comm.moe_quantize_mx(x, _u8(6, 21), _u8(6, 1)),
+                 lambda: comm.moe_quantize_mx(x, _u8(5, 21), _u8(6, 2)), lambda: comm.moe_quantize_mx(x, _u8(6, 21).char(), _u8(6, 2)),
+                 lambda: comm.moe_quantize_mx(x, _u8(6, 21), _u8(6, 2), gated=True), lambda: comm.moe_quantize_mx(x, _u8(6, 42)[:, ::2], _u8(6, 2)),
+                 lambda: comm.moe_quantize_mx(x, _u8(6, 21), _u8(6, 2), limit=torch.zeros(1, dtype=torch.int32)),
+                 lambda: comm.moe_dispatch_mx(x, row, _u8(18, 21), _u8(17, 2)), lambda: comm.moe_dispatch_mx(x, row.long(), _u8(18, 21), _u8(18, 2)),
+                 lambda: comm.moe_dispatch_mx(x, row[:5], _u8(18, 21), _u8(18, 2)),
+                 lambda: comm.moe_dequantize_mx(_u8(6, 21), _u8(6, 2), torch.zeros(6, 43)), lambda: comm.moe_dequantize_mx(_u8(6, 21), _u8(6, 2), torch.zeros(7, 41)),
+                 lambda: comm.moe_product_mx(_u8(6, 21), _u8(6, 2), w, ws, y, 43, offsets=offsets), lambda: comm.moe_product_mx(_u8(6, 21), _u8(6, 2), w, ws, y, 40, offsets=offsets),
+                 lambda: comm.moe_product_mx(_u8(6, 21), _u8(6, 2), w, ws[:, :6], y, 41, offsets=offsets),
+                 lambda: comm.moe_product_mx(_u8(6, 21), _u8(6, 2), _u8(6, 7, 21)[::2], ws, y, 41, offsets=offsets),
+                 lambda: comm.moe_product_mx(_u8(6, 21), _u8(6, 2), w, ws, torch.zeros(6, 8), 41, offsets=offsets),
+                 lambda: comm.moe_product_mx(_u8(6, 21), _u8(6, 2), w, ws, y, 41, offsets=offsets.int())):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(TypeError):
+        comm.moe_dequantize_mx(_u8(6, 21), _u8(6, 2), torch.zeros(6, 41, dtype=torch.float64))
+
+
+def test_refused_inside_a_group(comm):
+    H.hccl_group_start(comm.handle)
+    _refused(2, comm.moe_quantize_mx, torch.zeros(6, 41), _u8(6, 21), _u8(6, 2))
+    H.hccl_group_end(comm.handle)
+
+
+@pytest.mark.parametrize("name", ["quantize_mx", "dispatch_mx", "dequantize_mx", "product_mx"])
+def test_functions_and_methods_have_one_signature(name):
+    function, method, bind = (list(inspect.signature(f).parameters.values())[1:] for f in (
+        getattr(H, f"hccl_moe_{name}"), getattr(H.Comm, f"moe_{name}"), getattr(H.Comm, f"bind_moe_{name}")))
+    assert function and [(p.name, p.default) for p in function] == [(p.name, p.default) for p in method] == [(p.name, p.default) for p in bind]
+
+
+def test_reference_codes_are_the_nearest(comm):
+    rng = np.random.default_rng(0)
+    v = rng.normal(size=(50, 70)) * 2.0 ** rng.integers(-20, 20, (50, 1))
+    packed, scale = mx.quantize(v)
+    back, m = mx.values(packed, scale, 70), np.abs(v)
+    unit = 2.0 ** (np.repeat(scale, 32, 1)[:, :70].astype(float) - 127)
+    step = np.where(m < 2 * unit, 0.5, np.where(m < 4 * unit, 1, 2)) * unit
+    assert (np.abs(back - v) <= step / 2).all()
+    top = np.abs(np.pad(v, ((0, 0), (0, 26)))).reshape(50, 3, 32).max(2)
+    assert (top < 7 * 2.0 ** (scale - 127.0)).all() and (top >= 3.5 * 2.0 ** (scale - 127.0)).all()
+    ties = np.array([[4, 0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, -0.75, -5.0, 6.9, 0, -0.0]])
+    assert mx.values(*mx.quantize(ties), 13).tolist() == [[4, 0, 1, 1, 2, 2, 4, 4, -1, -4, 6, 0, 0]]
+    assert mx.quantize(np.array([[7.0]]))[1][0, 0] == 128 and mx.quantize(np.array([[np.nextafter(7, 0)]]))[1][0, 0] == 127
