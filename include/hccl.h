@@ -684,6 +684,34 @@ hcclResult_t hccl_moe_product_mx(hcclComm_t comm, const uint8_t* codes, size_t l
                                  const int64_t* offsets, size_t segments, void* out, size_t ldo, hcclDataType_t dtype,
                                  void* stream);
 
+/* The most tokens that hccl_moe_layer_mx takes. */
+#define HCCL_MAX_LAYER_TOKENS 64
+
+/* *bytes = the workspace that hccl_moe_layer_mx needs for these sizes. */
+hcclResult_t hccl_moe_layer_mx_bytes(size_t tokens, uint32_t top_k, size_t cols, size_t inner, size_t held, size_t* bytes);
+
+/*
+ * A whole layer for up to HCCL_MAX_LAYER_TOKENS tokens, as a decoding step has them: choices and their weights as by
+ * hccl_moe_route (written to index and weight: tokens * top_k each), and
+ *   out[t] = sum_k weight[t, k] * D_e h,   h = silu(G_e x[t]) * (U_e x[t]),   e = index[t, k]
+ * over the experts that are held here, first to first + held - 1; choices of others, and a token without any, add
+ * nothing. So ranks that hold an expert each and have all the tokens add up their results by hccl_allreduce.
+ * x: tokens rows of cols in dtype; out: the same. w_in: held * 2 * inner rows of cols in microscaled 4-bit floats, an expert's
+ * inner rows of G and then those of U; w_out: held * cols rows of inner, D. x enters as it is; products are added
+ * up in fp32, h is kept to 2^-16 of itself (exactly with fp32), and the sum over experts is taken in fp32 in an order
+ * that depends on sizes and choices alone, then rounded to dtype once. silu has the error that hccl_moe_quantize states.
+ * Results of a token with an infinity or NaN are infinite or NaN, and no other's are.
+ * workspace: hccl_moe_layer_mx_bytes bytes, 4-byte aligned, free again once the call's work is done; calls that may run at
+ * a time, and graphs that may, need one each.
+ */
+hcclResult_t hccl_moe_layer_mx(hcclComm_t comm, const hcclRouter_t* router, const void* logits, size_t ldl,
+                               hcclDataType_t logits_dtype, const float* bias, const uint8_t* mask, const void* x,
+                               size_t ldx, hcclDataType_t dtype, size_t tokens, size_t cols, size_t inner,
+                               const uint8_t* w_in, size_t ld_in, const uint8_t* w_in_scale, size_t ld_in_scale,
+                               const uint8_t* w_out, size_t ld_out, const uint8_t* w_out_scale, size_t ld_out_scale,
+                               size_t first, size_t held, int32_t* index, float* weight, void* out, size_t ldo,
+                               void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -13,5 +13,5 @@ from .hccl import (  # noqa: F401
     hccl_resident_last_seq, hccl_resident_start, hccl_resident_stop, hccl_resident_wait, hccl_set_trigger, load,
     hccl_moe_combine, hccl_moe_combine_backward, hccl_moe_dispatch, hccl_moe_plan, hccl_moe_plan_bytes, hccl_moe_product,
     hccl_moe_dequantize_mx, hccl_moe_dispatch_mx, hccl_moe_product_mx, hccl_moe_quantize_mx,
-    hccl_moe_quantize, hccl_moe_route, hccl_moe_route_backward, hccl_router_init,
+    hccl_moe_layer_mx, hccl_moe_layer_mx_bytes, hccl_moe_quantize, hccl_moe_route, hccl_moe_route_backward, hccl_router_init,
 )

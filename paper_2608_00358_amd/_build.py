@@ -28,7 +28,7 @@ ARCH = "gfx950"
 HOST_SOURCES = ["compiler.cpp", "validate.cpp"]
 # every source with kernels: the executor's and the mixture-of-experts operators'
 EXECUTOR_SOURCES = ["executor_generic.hip", "executor_resident.hip", "executor.hip", "executor_uniform.hip", "executor_dynamic.hip",
-                    "moe_route.hip", "moe_rows.hip", "moe_product.hip", "moe_mx_rows.hip", "moe_mx_product.hip"]
+                    "moe_route.hip", "moe_rows.hip", "moe_product.hip", "moe_mx_rows.hip", "moe_mx_product.hip", "moe_mx_layer.hip"]
 HIP_SOURCES = EXECUTOR_SOURCES + ["api.cpp", "moe_api.cpp"]
 
 HIPCC_FLAGS = [

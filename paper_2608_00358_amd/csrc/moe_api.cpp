@@ -76,7 +76,7 @@ private:
     }
     hcclResult_t result_;
     int device_ = HCCL_NO_DEVICE;
-    Rows2D seen_[10];
+    Rows2D seen_[16];
     int n_ = 0;
 };
 
@@ -86,6 +86,9 @@ bool is_float(hcclDataType_t dt) { return dt == hcclBf16 || dt == hcclFp16 || dt
 // A row of `cols` 4-bit floats: its bytes, two elements each, and its scales'.
 uint64_t mx_bytes(uint64_t cols) { return (cols + 1) / 2; }
 uint64_t mx_blocks(uint64_t cols) { return (cols + kMxBlock - 1) / kMxBlock; }
+
+// The hidden values of every route, in up to three parts of 16 bits; a row's end is whole blocks.
+uint64_t layer_mx_bytes(uint64_t tokens, uint64_t top_k, uint64_t inner) { return tokens * top_k * mx_blocks(inner) * kMxBlock * 3 * 2; }
 
 template <typename F>
 hcclResult_t enqueue(const Check& c, F launch) {
@@ -121,6 +124,30 @@ void check_router(Check& c, const hcclRouter_t* r) {
         .that(r->group_top == 1 || r->group_top == 2, "group_top must be 1 or 2")
         .that(r->groups == 0 || r->top_k <= r->top_groups * (r->experts / r->groups), "top_k is more than the kept groups hold")
         .that(std::isfinite(r->scale), "scale must be finite");
+}
+
+RouteArgs route_args(const hcclRouter_t& router, const void* logits, size_t ld, size_t tokens, const float* bias, const uint8_t* mask,
+                     int32_t* index, float* weight) {
+    RouteArgs a{};
+    a.logits = logits;
+    a.bias = bias;
+    a.mask = mask;
+    a.index = index;
+    a.weight = weight;
+    a.tokens = tokens;
+    a.ld = ld;
+    a.scale = router.scale;
+    a.experts = router.experts;
+    a.top_k = router.top_k;
+    a.groups = router.groups;
+    a.top_groups = router.top_groups;
+    a.group_top = router.group_top;
+    a.group_size = router.experts / router.groups;
+    a.group_magic = ((1u << 20) + a.group_size - 1) / a.group_size;
+    a.sigmoid = router.score == hcclScoreSigmoid;
+    a.renormalize = router.renormalize != 0;
+    a.whole_sum = bias || !a.renormalize || (a.top_groups < a.groups && a.group_top == 2);
+    return a;
 }
 
 Check& check_routes(Check& c, size_t tokens, uint32_t top_k) {
@@ -159,25 +186,7 @@ hcclResult_t hccl_moe_route(hcclComm_t comm, const hcclRouter_t* router, const v
         if (bias) c.list(bias, router->experts, 4, false, "bias");
         if (mask) c.list(mask, tokens, 1, false, "mask");
         if (!c.ok() || tokens == 0) return c.result();
-        RouteArgs a{};
-        a.logits = logits;
-        a.bias = bias;
-        a.mask = mask;
-        a.index = index;
-        a.weight = weight;
-        a.tokens = tokens;
-        a.ld = ld;
-        a.scale = router->scale;
-        a.experts = router->experts;
-        a.top_k = router->top_k;
-        a.groups = router->groups;
-        a.top_groups = router->top_groups;
-        a.group_top = router->group_top;
-        a.group_size = router->experts / router->groups;
-        a.group_magic = ((1u << 20) + a.group_size - 1) / a.group_size;
-        a.sigmoid = router->score == hcclScoreSigmoid;
-        a.renormalize = router->renormalize != 0;
-        a.whole_sum = bias || !a.renormalize || (a.top_groups < a.groups && a.group_top == 2);
+        const RouteArgs a = route_args(*router, logits, ld, tokens, bias, mask, index, weight);
         return enqueue(c, [&] { return launch_route(a, dtype, (hipStream_t)stream); });
     });
 }
@@ -532,6 +541,78 @@ hcclResult_t hccl_moe_product_mx(hcclComm_t comm, const uint8_t* codes, size_t l
         a.experts = (uint32_t)experts;
         a.type = dtype;
         return enqueue(c, [&] { return launch_product_mx(a, api_cus(comm), (hipStream_t)stream); });
+    });
+}
+
+hcclResult_t hccl_moe_layer_mx_bytes(size_t tokens, uint32_t top_k, size_t cols, size_t inner, size_t held, size_t* bytes) {
+    return guarded([&] {
+        if (!bytes) return api_fail(hcclInvalidArgument, "null argument");
+        if (tokens > HCCL_MAX_LAYER_TOKENS) return api_fail(hcclInvalidArgument, "more than 64 tokens");
+        if (top_k < 1 || top_k > HCCL_MAX_TOP_K) return api_fail(hcclInvalidArgument, "top_k must be 1 to 32");
+        if (held < 1 || held > HCCL_MAX_EXPERTS) return api_fail(hcclInvalidArgument, "held must be 1 to 1024");
+        if (cols > kMaxCount || inner > kMaxCount / 2) return api_fail(hcclInvalidArgument, "more than 2^31 - 1 columns");
+        *bytes = layer_mx_bytes(tokens, top_k, inner);
+        return hcclSuccess;
+    });
+}
+
+hcclResult_t hccl_moe_layer_mx(hcclComm_t comm, const hcclRouter_t* router, const void* logits, size_t ldl,
+                               hcclDataType_t logits_dtype, const float* bias, const uint8_t* mask, const void* x,
+                               size_t ldx, hcclDataType_t dtype, size_t tokens, size_t cols, size_t inner,
+                               const uint8_t* w_in, size_t ld_in, const uint8_t* w_in_scale, size_t ld_in_scale,
+                               const uint8_t* w_out, size_t ld_out, const uint8_t* w_out_scale, size_t ld_out_scale,
+                               size_t first, size_t held, int32_t* index, float* weight, void* out, size_t ldo,
+                               void* workspace, size_t workspace_bytes, void* stream) {
+    return guarded([&] {
+        Check c(comm);
+        check_router(c, router);
+        if (!c.ok()) return c.result();
+        c.that(is_float(dtype) && is_float(logits_dtype), "rows and logits must be bf16, fp16 or fp32")
+            .that(tokens <= HCCL_MAX_LAYER_TOKENS, "more than 64 tokens")
+            .that(cols <= kMaxCount && inner <= kMaxCount / 2, "more than 2^31 - 1 columns")
+            .that(held >= 1 && held <= router->experts && first <= router->experts - held, "held experts must be some of the router's");
+        if (!c.ok()) return c.result();
+        const uint64_t es = float_size(dtype), routes = tokens * router->top_k, need = layer_mx_bytes(tokens, router->top_k, inner);
+        c.rows(logits, tokens, router->experts, ldl, float_size(logits_dtype), false, "logits");
+        if (bias) c.list(bias, tokens ? router->experts : 0, 4, false, "bias");
+        if (mask) c.list(mask, tokens, 1, false, "mask");
+        c.rows(x, tokens, cols, ldx, es, false, "x");
+        if (tokens) {
+            c.rows(w_in, held * 2 * inner, mx_bytes(cols), ld_in, 1, false, "w_in")
+                .rows(w_in_scale, held * 2 * inner, mx_blocks(cols), ld_in_scale, 1, false, "w_in_scale")
+                .rows(w_out, held * cols, mx_bytes(inner), ld_out, 1, false, "w_out")
+                .rows(w_out_scale, held * cols, mx_blocks(inner), ld_out_scale, 1, false, "w_out_scale");
+        }
+        c.list(index, routes, 4, true, "index").list(weight, routes, 4, true, "weight").rows(out, tokens, cols, ldo, es, true, "out");
+        if (need) c.that(workspace != nullptr && workspace_bytes >= need, "workspace too small (hccl_moe_layer_mx_bytes)").list(workspace, need / 4, 4, true, "workspace");
+        if (!c.ok() || tokens == 0) return c.result();
+        const RouteArgs r = route_args(*router, logits, ldl, tokens, bias, mask, index, weight);
+        LayerMxArgs a{};
+        a.x = x;
+        a.w_in = w_in;
+        a.w_in_scale = w_in_scale;
+        a.w_out = w_out;
+        a.w_out_scale = w_out_scale;
+        a.index = index;
+        a.weight = weight;
+        a.out = out;
+        a.hidden = (uint16_t*)workspace;
+        a.ldx = ldx;
+        a.ld_in = ld_in;
+        a.ld_in_scale = ld_in_scale;
+        a.ld_out = ld_out;
+        a.ld_out_scale = ld_out_scale;
+        a.ldo = ldo;
+        a.tokens = (uint32_t)tokens;
+        a.top_k = router->top_k;
+        a.cols = (uint32_t)cols;
+        a.inner = (uint32_t)inner;
+        a.first = (uint32_t)first;
+        a.held = (uint32_t)held;
+        return enqueue(c, [&] {
+            const hipError_t e = launch_route(r, logits_dtype, (hipStream_t)stream);
+            return e != hipSuccess || a.cols == 0 ? e : launch_layer_mx(a, dtype, (hipStream_t)stream);
+        });
     });
 }
 

@@ -35,6 +35,7 @@ EXPORTS = [
     "hccl_router_init", "hccl_moe_route", "hccl_moe_route_backward", "hccl_moe_plan_bytes", "hccl_moe_plan",
     "hccl_moe_dispatch", "hccl_moe_combine", "hccl_moe_combine_backward", "hccl_moe_quantize", "hccl_moe_product",
     "hccl_moe_quantize_mx", "hccl_moe_dispatch_mx", "hccl_moe_dequantize_mx", "hccl_moe_product_mx",
+    "hccl_moe_layer_mx_bytes", "hccl_moe_layer_mx",
 ]
 CMPS = {"eq": 0, "ne": 1, "ge": 2, "gt": 3, "le": 4, "lt": 5}
 
@@ -147,6 +148,9 @@ def load(path: str = LIB_PATH):
     lib.hccl_moe_dispatch_mx.argtypes = [vp, vp, sz, i32, sz, sz, vp, u32, vp, sz, vp, sz, sz, vp]
     lib.hccl_moe_dequantize_mx.argtypes = [vp, vp, sz, vp, sz, sz, sz, vp, vp, sz, i32, vp]
     lib.hccl_moe_product_mx.argtypes = [vp, vp, sz, vp, sz, sz, sz, vp, sz, vp, sz, sz, sz, vp, sz, vp, sz, i32, vp]
+    lib.hccl_moe_layer_mx_bytes.argtypes = [sz, u32, sz, sz, sz, szp]
+    lib.hccl_moe_layer_mx.argtypes = [vp, rp, vp, sz, i32, vp, vp, vp, sz, i32, sz, sz, sz, vp, sz, vp, sz, vp, sz, vp, sz, sz, sz,
+                                      vp, vp, vp, sz, vp, sz, vp]
     for name in EXPORTS:
         if name not in ("hccl_get_last_error", "hccl_result_string"):
             getattr(lib, name).restype = res
@@ -369,6 +373,13 @@ def hccl_moe_plan_bytes(tokens: int, top_k: int, experts: int) -> int:
     return int(out.value)
 
 
+def hccl_moe_layer_mx_bytes(tokens: int, top_k: int, cols: int, inner: int, held: int) -> int:
+    """Bytes of the workspace that moe_layer_mx needs for these sizes."""
+    out = ctypes.c_size_t(0)
+    _check(load().hccl_moe_layer_mx_bytes(tokens, top_k, cols, inner, held, ctypes.byref(out)))
+    return int(out.value)
+
+
 # The operators' C calls, as (function, arguments): the hccl_moe_* functions below make them at once, the
 # bind_moe_* methods of Comm as often as they are called. Arrays of rows are 2-D tensors whose rows may be
 # any distance apart; the others are packed. Sizes come from the tensors, which must agree.
@@ -517,7 +528,7 @@ def _weights_mx(codes, scale, cols, what):
             raise ValueError(f"{name} must have shape (experts, rows, {n}), not {tuple(t.shape)}")
         E, N = t.shape[:2]
         ld = t.stride(1) if N > 1 else t.stride(0) if E > 1 else n
-        if (n > 1 and t.stride(2) != 1) or (E > 1 and t.stride(0) != N * ld):
+        if t.numel() and ((n > 1 and t.stride(2) != 1) or (E > 1 and t.stride(0) != N * ld)):
             raise ValueError(f"the rows of {name} must be one distance apart")
         out += [t.data_ptr(), ld]
     return (*out, *codes.shape[:2])
@@ -557,6 +568,27 @@ def _call_moe_product_mx(comm, codes, scale, weights, weight_scale, out, inner, 
     return load().hccl_moe_product_mx, (comm, *_rows_mx(codes, scale, R, inner, "codes"), R, inner, b, ldb, scales, ldsb, N, E,
                                         None if offsets is None else _list(offsets, S + 1, "int64", "offsets"), S, to, ldo,
                                         _dtype_code(out.dtype), _stream_handle(stream))
+
+
+def _call_moe_layer_mx(comm, router, logits, x, w_in, w_in_scale, w_out, w_out_scale, index, weight, out, bias=None, mask=None, first=0,
+                       workspace=None, stream=None):
+    (T, C), E, K = x.shape, router.experts, router.top_k
+    at, ldl = _rows(logits, T, E, "logits")
+    rows, ldx = _rows(x, T, C, "x")
+    to, ldo = _rows(out, T, C, "out")
+    _same_type(out, x, "out")
+    held, F = w_in.shape[0], w_in.shape[1] // 2 if w_in.dim() > 1 else 0
+    a, lda, a_scale, ldas, _, both = _weights_mx(w_in, w_in_scale, C, "w_in")
+    b, ldb, b_scale, ldbs, experts, columns = _weights_mx(w_out, w_out_scale, F, "w_out")
+    if both % 2 or (experts, columns) != (held, C):
+        raise ValueError(f"w_in and w_out must be (experts, 2 * inner, ...) and (experts, {C}, ...), not {tuple(w_in.shape)} and {tuple(w_out.shape)}")
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("workspace must be packed")
+    size = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    return load().hccl_moe_layer_mx, (comm, _router(router), at, ldl, _dtype_code(logits.dtype), _list(bias, E, "float32", "bias"),
+                                      _list(mask, T, "uint8", "mask"), rows, ldx, _dtype_code(x.dtype), T, C, F, a, lda, a_scale, ldas, b, ldb, b_scale, ldbs,
+                                      first, held, _list(index, T * K, "int32", "index"), _list(weight, T * K, "float32", "weight"), to, ldo,
+                                      _addr_or_null(workspace), size, _stream_handle(stream))
 
 
 def hccl_moe_route(comm, router, logits, index, weight, bias=None, mask=None, stream=None) -> None:
@@ -620,6 +652,14 @@ def hccl_moe_dequantize_mx(comm, codes, scale, out, limit=None, stream=None) -> 
 def hccl_moe_product_mx(comm, codes, scale, weights, weight_scale, out, inner, offsets=None, stream=None) -> None:
     """codes (rows, bytes) of `inner` elements a row, weights (experts, columns, bytes), each with its scales."""
     fn, a = _call_moe_product_mx(comm, codes, scale, weights, weight_scale, out, inner, offsets, stream)
+    _check(fn(*a))
+
+
+def hccl_moe_layer_mx(comm, router, logits, x, w_in, w_in_scale, w_out, w_out_scale, index, weight, out, bias=None, mask=None, first=0,
+                      workspace=None, stream=None) -> None:
+    """w_in (experts held, 2 * inner, bytes of columns), w_out (experts held, columns, bytes of inner), each with its scales;
+    the experts held are first, first + 1, ..."""
+    fn, a = _call_moe_layer_mx(comm, router, logits, x, w_in, w_in_scale, w_out, w_out_scale, index, weight, out, bias, mask, first, workspace, stream)
     _check(fn(*a))
 
 
@@ -847,6 +887,17 @@ class Comm:
     def bind_moe_product_mx(self, codes, scale, weights, weight_scale, out, inner, offsets=None, stream=None):
         return _bound_operator(self, _call_moe_product_mx(self.handle, codes, scale, weights, weight_scale, out, inner, offsets, stream),
                                codes, scale, weights, weight_scale, out, offsets)
+
+    def moe_layer_mx(self, router, logits, x, w_in, w_in_scale, w_out, w_out_scale, index, weight, out, bias=None, mask=None, first=0,
+                     workspace=None, stream=None):
+        hccl_moe_layer_mx(self.handle, router, logits, x, w_in, w_in_scale, w_out, w_out_scale, index, weight, out, bias, mask, first,
+                          workspace, stream)
+
+    def bind_moe_layer_mx(self, router, logits, x, w_in, w_in_scale, w_out, w_out_scale, index, weight, out, bias=None, mask=None, first=0,
+                          workspace=None, stream=None):
+        return _bound_operator(self, _call_moe_layer_mx(self.handle, router, logits, x, w_in, w_in_scale, w_out, w_out_scale, index, weight, out,
+                                                        bias, mask, first, workspace, stream),
+                               logits, x, w_in, w_in_scale, w_out, w_out_scale, index, weight, out, bias, mask, workspace)
 
     def triggered(self, wait=None, done=None):
         """Context manager: the next work packet called inside waits for ``wait`` =

@@ -67,11 +67,12 @@ def silu(x):
 
 
 def layer(x, index, weight, w_in, w_out, first=0):
-    """sum_k weight * W_out silu(gate) up over the held experts first, first + 1, ...; and for each output a bound's parts:
-    the sums of sizes of the terms, of the hidden values' sums, as they enter the result."""
+    """y = sum_k weight * W_out z, z = silu(gate) * up, over the held experts first, first + 1, ... And what errors are measured
+    by: the same sum of sizes; the same of what a change of the gates' and ups' sums by their sums of sizes does to z
+    (|d silu| <= 1.1); and the greatest gate."""
     T, C = x.shape
     F = w_out.shape[2]
-    y, size, spread = np.zeros((T, C)), np.zeros((T, C)), np.zeros((T, C))
+    y, size, spread, greatest = np.zeros((T, C)), np.zeros((T, C)), np.zeros((T, C)), 0.0
     for t in range(T):
         for k in range(index.shape[1]):
             e = index[t, k] - first
@@ -81,9 +82,9 @@ def layer(x, index, weight, w_in, w_out, first=0):
             mag = np.abs(w_in[e]) @ np.abs(x[t])
             g, u = h[:F], h[F:]
             z = silu(g) * u
-            # |d silu / dg| <= 1.1
             dz = 1.1 * mag[:F] * np.abs(u) + np.abs(silu(g)) * mag[F:]
             y[t] += weight[t, k] * (w_out[e] @ z)
             size[t] += abs(weight[t, k]) * (np.abs(w_out[e]) @ np.abs(z))
             spread[t] += abs(weight[t, k]) * (np.abs(w_out[e]) @ dz)
-    return y, size, spread
+            greatest = max(greatest, np.abs(g).max(initial=0))
+    return y, size, spread, greatest

@@ -113,7 +113,67 @@ def test_refused_inside_a_group(comm):
     H.hccl_group_end(comm.handle)
 
 
-@pytest.mark.parametrize("name", ["quantize_mx", "dispatch_mx", "dequantize_mx", "product_mx"])
+def _layer(T=5, E=8, K=2, C=41, F=12, held=8, dt=torch.float32, **kw):
+    args = dict(router=H.hccl_router_init(experts=E, top_k=K), logits=torch.zeros(T, E), x=torch.zeros(T, C, dtype=dt), w_in=_u8(held, 2 * F, (C + 1) // 2),
+                w_in_scale=_u8(held, 2 * F, (C + 31) // 32), w_out=_u8(held, C, (F + 1) // 2), w_out_scale=_u8(held, C, (F + 31) // 32),
+                index=torch.zeros(T, K, dtype=torch.int32), weight=torch.zeros(T, K), out=torch.zeros(T, C, dtype=dt),
+                workspace=torch.zeros(max(1, H.hccl_moe_layer_mx_bytes(min(T, 64), K, C, F, held)), dtype=U8))
+    return {**args, **kw}
+
+
+def test_layers_that_pass_the_checks(comm):
+    comm.moe_layer_mx(**_layer())
+    comm.moe_layer_mx(**_layer(T=64, dt=torch.bfloat16, bias=torch.zeros(8), mask=torch.ones(64, dtype=torch.bool)))
+    comm.moe_layer_mx(**_layer(held=3, first=5, logits=torch.zeros(5, 8, dtype=torch.float16)))
+    comm.moe_layer_mx(**_layer(T=0))
+    comm.moe_layer_mx(**_layer(F=0, workspace=None))
+    comm.moe_layer_mx(**_layer(C=0))
+    wide = _u8(8, 24, 30)
+    comm.moe_layer_mx(**_layer(w_in=wide[..., :21]))
+    H.hccl_moe_layer_mx(comm.handle, **_layer())
+    comm.bind_moe_layer_mx(**_layer())()
+
+
+def test_layers_that_are_refused(comm):
+    _refused(1, comm.moe_layer_mx, **_layer(T=65))
+    _refused(1, comm.moe_layer_mx, **_layer(held=3, first=6))
+    _refused(1, comm.moe_layer_mx, **_layer(held=9))
+    _refused(1, comm.moe_layer_mx, **_layer(first=-1, held=3))
+    _refused(1, comm.moe_layer_mx, **_layer(workspace=None))
+    _refused(1, comm.moe_layer_mx, **_layer(workspace=_u8(H.hccl_moe_layer_mx_bytes(5, 2, 41, 12, 8) - 1)))
+    a = _layer()
+    a["router"].scale = float("inf")
+    _refused(1, comm.moe_layer_mx, **a)
+    for over in ("logits", "x", "w_in", "w_in_scale", "w_out", "w_out_scale", "index", "weight", "out", "bias", "mask"):
+        a = _layer(bias=torch.zeros(8), mask=torch.zeros(5, dtype=U8))
+        if over == "workspace":
+            continue
+        # results or workspace over an input, or over each other
+        n = H.hccl_moe_layer_mx_bytes(5, 2, 41, 12, 8)
+        both = _u8(n + 8192)
+        t = a[over]
+        size = t.numel() * t.element_size()
+        a[over] = both[:size].view(t.dtype).view(t.shape)
+        a["workspace"] = both[size // 4 * 4 - (4 if size % 4 == 0 else 0):][:n]
+        _refused(1, comm.moe_layer_mx, **a)
+    a = _layer()
+    a["out"] = a["x"]
+    _refused(1, comm.moe_layer_mx, **a)
+    lib = H.load()
+    import ctypes
+    n = ctypes.c_size_t(0)
+    for bad in ((65, 2, 8, 8, 8), (5, 0, 8, 8, 8), (5, 33, 8, 8, 8), (5, 2, 1 << 31, 8, 8), (5, 2, 8, 1 << 30, 8), (5, 2, 8, 8, 0), (5, 2, 8, 8, 1025)):
+        assert lib.hccl_moe_layer_mx_bytes(*bad, ctypes.byref(n)) == 1
+    assert lib.hccl_moe_layer_mx_bytes(5, 2, 8, 8, 8, None) == 1
+    for change in (dict(x=torch.zeros(5, 42)), dict(x=torch.zeros(4, 41)), dict(out=torch.zeros(5, 41, dtype=torch.float16)), dict(w_in=_u8(8, 23, 21)),
+                   dict(w_in=_u8(8, 24, 20)), dict(w_in_scale=_u8(8, 24, 1)), dict(w_out=_u8(7, 41, 6)), dict(w_out=_u8(8, 40, 6)), dict(w_out_scale=_u8(8, 41, 2)),
+                   dict(w_out=_u8(16, 41, 6)[::2]), dict(index=torch.zeros(5, 3, dtype=torch.int32)), dict(weight=torch.zeros(5, 2, dtype=torch.float64)),
+                   dict(mask=torch.ones(4, dtype=U8)), dict(bias=torch.zeros(7)), dict(workspace=_u8(100000)[::2]), dict(logits=torch.zeros(5, 9))):
+        with pytest.raises(ValueError):
+            comm.moe_layer_mx(**_layer(**change))
+
+
+@pytest.mark.parametrize("name", ["quantize_mx", "dispatch_mx", "dequantize_mx", "product_mx", "layer_mx"])
 def test_functions_and_methods_have_one_signature(name):
     function, method, bind = (list(inspect.signature(f).parameters.values())[1:] for f in (
         getattr(H, f"hccl_moe_{name}"), getattr(H.Comm, f"moe_{name}"), getattr(H.Comm, f"bind_moe_{name}")))
