@@ -147,21 +147,22 @@ __global__ __launch_bounds__(W * 64) void hccl_moe_product_mx_few_kernel(Product
 }
 
 // Many rows a segment: BM rows by BN columns a block, in WM x WN waves, k in steps of 64 bytes (128 elements, four blocks)
-// through four LDS buffers: one is multiplied while the next three are filled, by loads that go to LDS directly
-// (DIRECT: 1 for rows, 2 for weights that are 16-byte aligned) or through registers (any alignment, and the
-// last step of an inner size that is no multiple of 128, where codes past the end are zero).
+// through four LDS buffers, three steps ahead: by loads that go to LDS directly (DIRECT: rows and weights are 16-byte
+// aligned) or through registers (any alignment, and the last step of an inner size that is no multiple of 128, where codes
+// past the end are zero).
+//
+// A wave reads a step's fragments and their scales from LDS, waits for them, and multiplies them. With two GROUPS, waves
+// 0 to 3 and 4 to 7, which share the SIMDs, the second is half a step behind: one reads while the other multiplies, and
+// barriers between the halves keep it so. With one, other blocks on the CU fill the gap. Reads are one block of assembly
+// with its wait: the compiler, which cannot tell which loads to LDS a read depends on, would have each wait for all of them.
 //
 // LDS holds a row's 64 bytes as 4 chunks of 16; chunk c of row r lies in slot c ^ (r / 4 & 3), so that the
 // 16 lanes served together, which read one chunk of 16 rows, use different banks. A direct load writes its 64 lanes one
-// after the other, so a lane reads the chunk that belongs in its slot.
+// after the other, so a lane reads the chunk that belongs in its slot. The lanes' halves take chunks 0 and 2 in a step's
+// first part and 1 and 3 in its second, so that a half's two scale bytes are neighbours.
 //
 // Scales: a thread has one row, of the tile's rows or columns, whose next 16 scale bytes (four steps) it reads into a
-// register four steps ahead and puts into LDS two steps before they count, there being two such buffers. A step's four
-// bytes of a row are one 32-bit word; a lane moves it down by its half's chunk, and the instructions take byte 0 or 2.
-//
-// Fragments are read one part (32 of the 64 bytes) ahead of the matrix instructions. The barrier stands
-// inside a step's last part: by then all its fragments have been read, so the next step's buffer can be
-// read and the old one refilled while that part is still being multiplied.
+// register four steps ahead and puts into LDS three steps before they count, there being two such buffers.
 constexpr uint32_t kStep = 64;
 constexpr uint32_t kBuffers = 4;
 constexpr uint32_t kBand = 4;
@@ -170,6 +171,7 @@ typedef __attribute__((address_space(3))) void* lds_ptr;
 
 template <int N>
 __device__ __forceinline__ void wait_loads() {  // until at most N loads are on their way, and LDS is done
+    static_assert(N < 16, "the counter's low bits");
     __builtin_amdgcn_s_waitcnt(0x70 | N);
 }
 // A barrier that leaves loads to LDS in flight; nothing that touches memory moves across it.
@@ -178,13 +180,61 @@ __device__ __forceinline__ void meet() {
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
+__device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(lds_ptr)p; }
+__device__ __forceinline__ void lds_write(uint32_t at, const v4u& v) { asm volatile("ds_write_b128 %0, %1" ::"v"(at), "v"(v) : "memory"); }
 
-template <int BM, int BN, int WM, int WN, int DIRECT>
+// A step's fragments of a wave: TM of rows, TN of columns, two parts each, and their scales, 16 bits each.
+template <int TM, int TN>
+struct Fragments {
+    v4i a[2][TM], b[2][TN];
+    uint32_t sa[TM], sb[TN];
+};
+// (the distance of fragments is 32 rows: 2048 bytes of codes, 512 of scales)
+__device__ __forceinline__ void read_fragments(Fragments<4, 2>& f, uint32_t a0, uint32_t a1, uint32_t b0, uint32_t b1, uint32_t sa, uint32_t sb) {
+    asm volatile(
+        "ds_read_b128 %0, %18\n\tds_read_b128 %8, %20\n\tds_read_b128 %9, %20 offset:2048\n\t"
+        "ds_read_u16 %12, %22\n\tds_read_u16 %13, %22 offset:512\n\tds_read_u16 %14, %22 offset:1024\n\tds_read_u16 %15, %22 offset:1536\n\t"
+        "ds_read_u16 %16, %23\n\tds_read_u16 %17, %23 offset:512\n\t"
+        "ds_read_b128 %1, %18 offset:2048\n\tds_read_b128 %2, %18 offset:4096\n\tds_read_b128 %3, %18 offset:6144\n\t"
+        "ds_read_b128 %4, %19\n\tds_read_b128 %10, %21\n\tds_read_b128 %11, %21 offset:2048\n\t"
+        "ds_read_b128 %5, %19 offset:2048\n\tds_read_b128 %6, %19 offset:4096\n\tds_read_b128 %7, %19 offset:6144\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(f.a[0][0]), "=&v"(f.a[0][1]), "=&v"(f.a[0][2]), "=&v"(f.a[0][3]), "=&v"(f.a[1][0]), "=&v"(f.a[1][1]), "=&v"(f.a[1][2]), "=&v"(f.a[1][3]),
+          "=&v"(f.b[0][0]), "=&v"(f.b[0][1]), "=&v"(f.b[1][0]), "=&v"(f.b[1][1]),
+          "=&v"(f.sa[0]), "=&v"(f.sa[1]), "=&v"(f.sa[2]), "=&v"(f.sa[3]), "=&v"(f.sb[0]), "=&v"(f.sb[1])
+        : "v"(a0), "v"(a1), "v"(b0), "v"(b1), "v"(sa), "v"(sb)
+        : "memory");
+}
+__device__ __forceinline__ void read_fragments(Fragments<2, 2>& f, uint32_t a0, uint32_t a1, uint32_t b0, uint32_t b1, uint32_t sa, uint32_t sb) {
+    asm volatile(
+        "ds_read_b128 %0, %12\n\tds_read_b128 %4, %14\n\tds_read_b128 %5, %14 offset:2048\n\t"
+        "ds_read_u16 %8, %16\n\tds_read_u16 %9, %16 offset:512\n\tds_read_u16 %10, %17\n\tds_read_u16 %11, %17 offset:512\n\t"
+        "ds_read_b128 %1, %12 offset:2048\n\tds_read_b128 %2, %13\n\tds_read_b128 %6, %15\n\tds_read_b128 %7, %15 offset:2048\n\t"
+        "ds_read_b128 %3, %13 offset:2048\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(f.a[0][0]), "=&v"(f.a[0][1]), "=&v"(f.a[1][0]), "=&v"(f.a[1][1]), "=&v"(f.b[0][0]), "=&v"(f.b[0][1]), "=&v"(f.b[1][0]), "=&v"(f.b[1][1]),
+          "=&v"(f.sa[0]), "=&v"(f.sa[1]), "=&v"(f.sb[0]), "=&v"(f.sb[1])
+        : "v"(a0), "v"(a1), "v"(b0), "v"(b1), "v"(sa), "v"(sb)
+        : "memory");
+}
+__device__ __forceinline__ void read_fragments(Fragments<2, 1>& f, uint32_t a0, uint32_t a1, uint32_t b0, uint32_t b1, uint32_t sa, uint32_t sb) {
+    asm volatile(
+        "ds_read_b128 %0, %9\n\tds_read_b128 %4, %11\n\t"
+        "ds_read_u16 %6, %13\n\tds_read_u16 %7, %13 offset:512\n\tds_read_u16 %8, %14\n\t"
+        "ds_read_b128 %1, %9 offset:2048\n\tds_read_b128 %2, %10\n\tds_read_b128 %5, %12\n\tds_read_b128 %3, %10 offset:2048\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(f.a[0][0]), "=&v"(f.a[0][1]), "=&v"(f.a[1][0]), "=&v"(f.a[1][1]), "=&v"(f.b[0][0]), "=&v"(f.b[1][0]), "=&v"(f.sa[0]), "=&v"(f.sa[1]), "=&v"(f.sb[0])
+        : "v"(a0), "v"(a1), "v"(b0), "v"(b1), "v"(sa), "v"(sb)
+        : "memory");
+}
+
+template <int BM, int BN, int WM, int WN, int GROUPS, bool DIRECT>
 __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_mx_many_kernel(ProductMxArgs a, uint32_t nblocks) {
     constexpr int W = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
     constexpr int LA = BM / 16 / W, LB = BN / 16 / W, LN = LA + LB;  // loads a wave makes for a step: 16 rows each
-    static_assert(BM % (16 * W) == 0 && BN % (16 * W) == 0 && 3 * LN < 16, "whole loads, and a counter that holds them");
+    static_assert(BM % (16 * W) == 0 && BN % (16 * W) == 0 && 2 * LN < 16, "whole loads, and a counter that holds them");
     static_assert(BM + BN <= W * 64, "a thread has the scales of one row");
+    static_assert(GROUPS == 1 || W == 8, "two groups of a wave a SIMD");
     constexpr uint32_t kBuffer = (BM + BN) * kStep, kScales = (BM + BN) * 16;
     __shared__ __attribute__((aligned(256))) char lds[kBuffers * kBuffer];
     __shared__ __attribute__((aligned(256))) char lds_scale[2 * kScales];
@@ -213,11 +263,10 @@ __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_mx_many_kernel(
 
     // where this lane's part of each load comes from, and where in a buffer each load goes
     const uint32_t lrow = lane >> 2, chunk = ((lane & 3) ^ (lrow >> 2)) * 16;
+    auto source = [&](int i) { return i < LA ? a.a + row_of((w * LA + i) * 16 + lrow) * a.lda : a.b + col_of((w * LB + i - LA) * 16 + lrow) * a.ldb; };
     const uint8_t* src[LN];
 #pragma unroll
-    for (int i = 0; i < LA; ++i) src[i] = a.a + row_of((w * LA + i) * 16 + lrow) * a.lda + chunk;
-#pragma unroll
-    for (int i = 0; i < LB; ++i) src[LA + i] = a.b + col_of((w * LB + i) * 16 + lrow) * a.ldb + chunk;
+    for (int i = 0; i < LN; ++i) src[i] = source(i) + chunk;
     auto slot = [&](uint32_t s, int i) { return lds + (s % kBuffers) * kBuffer + (i < LA ? (w * LA + i) * 16 : BM + (w * LB + i - LA) * 16) * kStep; };
     const uint8_t* scale_src = threadIdx.x < BM ? a.a_scale + row_of(threadIdx.x) * a.ldas : a.b_scale + col_of(threadIdx.x < BM + BN ? threadIdx.x - BM : 0) * a.ldbs;
     const uint32_t scale_bytes = threadIdx.x < BM + BN ? (a.inner + kMxBlock - 1) / kMxBlock : 0;
@@ -234,142 +283,144 @@ __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_mx_many_kernel(
     // Waves of the same rows are neighbours, and so on different SIMDs: where an end of a segment leaves
     // waves without rows, those that have some share out the matrix units.
     const uint32_t wm = w / WN, wn = w % WN;
-    constexpr bool kAll = DIRECT == 3;
-    auto direct = [](int i) { return (DIRECT & (i < LA ? 1 : 2)) != 0; };
-    v4u held[2][LN];  // on their way through registers: steps of either parity
-    v4u held_scale;   // scales of four steps, on their way
-    // Load i of those that bring in step s. INNER: it and the steps before it are whole.
-    auto fetch = [&](uint32_t s, int parity, auto inner, int i) {
-        if (direct(i) && (inner.value || s < whole_steps)) {
+    const bool second = GROUPS == 2 && w >= 4;
+    v4u held[LN];    // on their way through registers
+    v4u held_scale;  // scales of four steps, on their way
+    auto put = [&](uint32_t s, int i, const v4u& v) { lds_write(lds_address(slot(s, i)) + lane * 16, v); };
+    // Load i of those that bring in step s, a whole one; through registers, the one before goes to its buffer meanwhile.
+    auto fetch = [&](uint32_t s, int i) {
+        if constexpr (DIRECT) {
             __builtin_amdgcn_global_load_lds((const HCCL_AS1 void*)(src[i] + (uint64_t)s * kStep), (lds_ptr)slot(s, i), 16, 0, 0);
-        } else if (inner.value || s < steps) {
-            const v4u v = inner.value || s < whole_steps ? load16<1>(src[i] + (uint64_t)s * kStep) : i < LA ? load_codes<true, true>(src[i] - chunk, s * kStep + chunk, a.inner)
-                                                                                                                  : load_codes<true, false>(src[i] - chunk, s * kStep + chunk, a.inner);
-            if (direct(i)) *(v4u*)(slot(s, i) + lane * 16) = v;
-            else held[parity][i] = v;
+        } else {
+            put(s - 1, i, held[i]);
+            held[i] = load16<1>(src[i] + (uint64_t)s * kStep);
         }
     };
-    auto fetch_all = [&](uint32_t s, int parity, auto inner) {
-#pragma unroll
-        for (int i = 0; i < LN; ++i) fetch(s, parity, inner, i);
-    };
-    auto put = [&](uint32_t s, int parity) {  // what registers hold of step s goes to its buffer
-#pragma unroll
+    auto bring = [&](uint32_t s) {  // any step, at once
+#pragma unroll 1
         for (int i = 0; i < LN; ++i)
-            if (!direct(i)) *(v4u*)(slot(s, i) + lane * 16) = held[parity][i];
+            put(s, i, i < LA ? load_codes<true, true>(source(i), s * kStep + chunk, a.inner) : load_codes<true, false>(source(i), s * kStep + chunk, a.inner));
+    };
+    // What is left to bring in when step s + 3 is none of the whole ones any more: once, before step s, when the buffers of
+    // the steps before s are free and few registers are in use.
+    auto finish = [&] {
+        if (whole_steps < 3) return;  // (all of it was brought in at the beginning)
+        if constexpr (!DIRECT) {
+#pragma unroll
+            for (int i = 0; i < LN; ++i) put(whole_steps - 1, i, held[i]);
+        }
+        if (whole_steps < steps) bring(whole_steps);
     };
     auto fetch_scales = [&](uint32_t four) { held_scale = load_bytes<false>(scale_src, four * 16, scale_bytes); };
     auto put_scales = [&](uint32_t four) {
-        if (BM + BN == W * 64 || threadIdx.x < BM + BN) *(v4u*)(lds_scale + (four & 1) * kScales + threadIdx.x * 16) = held_scale;
+        if (BM + BN == W * 64 || threadIdx.x < BM + BN) lds_write(lds_address(lds_scale) + (four & 1) * kScales + threadIdx.x * 16, held_scale);
     };
     // In the second of four steps s: the scales of the next four go to LDS, those after them on their way.
     auto stage = [&](uint32_t s) {
+        if ((s & 3) != 1) return;
         put_scales(s / 4 + 1);
         fetch_scales(s / 4 + 2);
     };
-    v4i va[2][TM], vb[2][TN];
-    uint32_t sa[2][TM], sb[2][TN];
-    auto read = [&](uint32_t s, uint32_t part, int i) {  // fragment i of a part, in the order of their use
-        const uint32_t at = (s % kBuffers) * kBuffer + ((part * 2 + (lane >> 5)) ^ (lane >> 2 & 3)) * 16 + (lane & 31) * kStep;
-        if (i == 0) va[part][0] = *(const v4i*)(lds + wm * TM * 32 * kStep + at);
-        else if (i <= TN) vb[part][i - 1] = *(const v4i*)(lds + (BM + (wn * TN + i - 1) * 32) * kStep + at);
-        else va[part][i - TN] = *(const v4i*)(lds + (wm * TM + i - TN) * 32 * kStep + at);
+
+    // a lane's places in a buffer: its row of the wave's first fragment, the chunk of its half
+    const uint32_t place = (lane & 31) * kStep + ((lane >> 5) * 2 ^ (lane >> 2 & 3)) * 16;
+    const uint32_t at_a = lds_address(lds) + wm * TM * 32 * kStep + place, at_b = lds_address(lds) + (BM + wn * TN * 32) * kStep + place;
+    const uint32_t at_sa = lds_address(lds_scale) + (wm * TM * 32 + (lane & 31)) * 16 + (lane >> 5) * 2;
+    const uint32_t at_sb = at_sa + (BM + wn * TN * 32 - wm * TM * 32) * 16;
+    Fragments<TM, TN> f;
+    auto read = [&](uint32_t s) {
+        const uint32_t at = (s % kBuffers) * kBuffer, at_scale = (s / 4 & 1) * kScales + (s & 3) * 4;
+        read_fragments(f, at_a + at, (at_a ^ 16) + at, at_b + at, (at_b ^ 16) + at, at_sa + at_scale, at_sb + at_scale);
     };
-    auto read_scale = [&](uint32_t s, int parity, int i) {
-        const char* at = lds_scale + (s / 4 & 1) * kScales + (s & 3) * 4 + (lane & 31) * 16;
-        if (i < TN) sb[parity][i] = *(const uint32_t*)(at + (BM + (wn * TN + i) * 32) * 16) >> (lane >> 5) * 8;
-        else sa[parity][i - TN] = *(const uint32_t*)(at + (wm * TM + i - TN) * 32 * 16) >> (lane >> 5) * 8;
-    };
-    // A part's matrix instructions, one after the other, each followed by a load or a read or two: a wave
-    // that makes its loads in one go waits for the units that take them, and its SIMD with it.
-    constexpr int kMfmas = TM * TN, kReads = TM + TN, kFirst = kMfmas >= 8 ? 2 : 1;
-    auto multiply = [&](auto part, int parity, int from, int to, auto between) {
-        constexpr int P = decltype(part)::value;
+    // A step's matrix instructions, with the loads that bring in step s + 3 (INNER: a whole one) between them: a wave that makes
+    // its loads in one go waits for the units that take them, and its SIMD with it.
+    auto multiply = [&](uint32_t s, auto inner) {
+        constexpr int kMfmas = 2 * TM * TN;
+        int next = 0;
 #pragma unroll
-        for (int i = from; i < to; ++i) {
-            acc[i % TN][i / TN] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(whole(vb[P][i % TN]), whole(va[P][i / TN]), acc[i % TN][i / TN], kFp4, kFp4,
-                                                                                2 * P, sb[parity][i % TN], 2 * P, sa[parity][i / TN]);
+        for (int i = 0; i < kMfmas; ++i) {
+            const int x = i / TN % TM, y = i % TN;
+            if (i < kMfmas / 2)
+                acc[y][x] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(whole(f.b[0][y]), whole(f.a[0][x]), acc[y][x], kFp4, kFp4, 0, f.sb[y], 0, f.sa[x]);
+            else
+                acc[y][x] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(whole(f.b[1][y]), whole(f.a[1][x]), acc[y][x], kFp4, kFp4, 1, f.sb[y], 1, f.sa[x]);
             __builtin_amdgcn_sched_barrier(0);
-            between(i);
+            if (inner.value)
+                for (; next < LN && next * kMfmas < (i + 1) * LN; ++next) fetch(s + 3, next);
             __builtin_amdgcn_sched_barrier(0);
         }
-    };
-    // Those of n operations that go behind instruction i, spread over `slots` of them from `from` on.
-    auto spread = [](int i, int from, int slots, int n, auto f) {
-        const int at = i - from;
-        if (at < 0 || at >= slots) return;
+        // (here, and not sunk behind what follows)
 #pragma unroll
-        for (int r = at * n / slots; r < (at + 1) * n / slots; ++r) f(r);
+        for (int y = 0; y < TN; ++y)
+#pragma unroll
+            for (int x = 0; x < TM; ++x) {
+                // (in the registers where the compiler has them: blocks of 4 waves may have accumulation registers)
+                if constexpr (W == 8) asm volatile("" : "+v"(acc[y][x]));
+                else asm volatile("" : "+a"(acc[y][x]));
+            }
     };
-    // reads end two instructions before the part does, so that they are there when the next one begins
-    constexpr int kReadSlots = kMfmas >= 8 ? kMfmas - kFirst - 2 : kMfmas >= 4 ? 2 : 1;
-    const std::integral_constant<int, 0> first_part;
-    const std::integral_constant<int, 1> second_part;
-    // Step s + 1 has landed for all waves, and all have read step s, whose buffer step s + 4 takes. Loads of
-    // the steps s + 2 and s + 3 stay on their way (where all are direct loads; where some pass through registers,
-    // step s + 2 is needed there, and only those of step s + 3 do).
-    auto land = [&](uint32_t s, int parity, auto inner) {
-        if (inner.value || s + 2 < steps) put(s + 2, parity);
-        if (DIRECT == 0) __builtin_amdgcn_s_waitcnt(0xc07f);  // LDS alone
-        else if (inner.value || s + 3 < whole_steps) wait_loads<kAll ? 2 * LN : LN>();
-        else wait_loads<0>();
-        meet();
+    auto load_only = [&](uint32_t s, auto inner) {  // the same of a wave without rows
+        if (inner.value) {
+#pragma unroll
+            for (int i = 0; i < LN; ++i) fetch(s + 3, i);
+        }
     };
-    auto step = [&](uint32_t s, int phase, auto inner) {
-        const int parity = phase & 1;
-        multiply(first_part, parity, 0, kMfmas, [&](int i) {
-            spread(i, kFirst - 1, kReadSlots, kReads, [&](int r) { read(s, 1, r); });
-            spread(i, kFirst - 1, kMfmas - kFirst + 1, LN, [&](int r) { fetch(s + 3, parity ^ 1, inner, r); });
-        });
-        multiply(second_part, parity, 0, kFirst, [](int) {});
-        if (inner.value ? phase == 1 : (s & 3) == 1) stage(s);
-        land(s, parity, inner);
-        const bool more = inner.value || s + 1 < steps;
-        multiply(second_part, parity, kFirst, kMfmas, [&](int i) {
-            if (more) spread(i, kFirst, kReadSlots, 2 * kReads, [&](int r) {
-                if (r & 1) read(s + 1, 0, r / 2);
-                else read_scale(s + 1, parity ^ 1, r / 2);
-            });
-        });
-    };
-    auto idle = [&](uint32_t s, int phase, auto inner) {  // a step of a wave without rows: brings in its part for the others
-        const int parity = phase & 1;
-        fetch_all(s + 3, parity ^ 1, inner);
-        if (inner.value ? phase == 1 : (s & 3) == 1) stage(s);
-        land(s, parity, inner);
-    };
-    auto walk = [&](auto each) {
+    // The first group waits for its loads of step s + 1 at the end of step s, those of two further steps being on their
+    // way; the second, half a step later, when it has made those of one.
+    auto walk = [&](auto reading, auto working) {
+        auto pass = [&](uint32_t s, auto inner) {
+            reading(s);
+            if constexpr (GROUPS == 2) {
+                if (second && DIRECT) {
+                    if (inner.value) wait_loads<LN>();
+                    else wait_loads<0>();
+                }
+                meet();
+            }
+            working(s, inner);
+            stage(s);
+            if (!second || !DIRECT) {
+                if (!DIRECT) __builtin_amdgcn_s_waitcnt(0xc07f);  // LDS alone
+                else if (inner.value) wait_loads<2 * LN>();
+                else wait_loads<0>();
+            } else {
+                __builtin_amdgcn_s_waitcnt(0xc07f);
+            }
+            if (inner.value || !second || s + 1 < steps) meet();  // (the last barrier is the first group's)
+        };
+        if (second) meet();
         uint32_t s = 0;
-        for (; s + 6 < whole_steps; s += 4) {
-            each(s, 0, std::true_type());
-            each(s + 1, 1, std::true_type());
-            each(s + 2, 2, std::true_type());
-            each(s + 3, 3, std::true_type());
-        }
 #pragma unroll 1
-        for (; s < steps; s += 2) {
-            each(s, 0, std::false_type());
-            if (s + 1 < steps) each(s + 1, 1, std::false_type());
-        }
+        for (; s + 3 < whole_steps; ++s) pass(s, std::true_type());
+        finish();
+#pragma unroll 1
+        for (; s < steps; ++s) pass(s, std::false_type());
     };
     if (steps) {
-        const std::false_type any;
         fetch_scales(0);
-        fetch_all(0, 0, any), fetch_all(1, 1, any);
+        if constexpr (DIRECT) {
+            const uint32_t n = whole_steps < 3 ? whole_steps : 3;
+            for (uint32_t s = 0; s < n; ++s)
+#pragma unroll
+                for (int i = 0; i < LN; ++i) fetch(s, i);
+        } else {
+            if (whole_steps > 0) bring(0);
+            if (whole_steps > 1) bring(1);
+            if (whole_steps > 2) {
+#pragma unroll
+                for (int i = 0; i < LN; ++i) held[i] = load16<1>(src[i] + 2 * kStep);
+            }
+        }
+        if (whole_steps < 3 && whole_steps < steps) bring(whole_steps);
         put_scales(0);
-        put(0, 0);
-        if (steps > 1) put(1, 1);
-        fetch_all(2, 0, any);
         fetch_scales(1);
         wait_loads<0>();
         meet();
         if (rows.first + wm * TM * 32 >= rows.end) {
-            walk(idle);
+            walk([](uint32_t) {}, load_only);
             return;
         }
-#pragma unroll
-        for (int r = 0; r < kReads; ++r) read(0, 0, r), read_scale(0, 0, r);
-        walk(step);
+        walk(read, multiply);
     }
 
     // The wave's TM x TN blocks leave through its own part of LDS, as rows of TN * 32 results: lanes that hold
@@ -380,7 +431,7 @@ __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_mx_many_kernel(
         constexpr uint32_t kLine = TN * 32 * ES, kChunks = kLine / 16;  // bytes of a row
         constexpr int kRowsEach = kBuffers * kBuffer / W / kLine >= TM * 32 ? TM : kBuffers * kBuffer / W / kLine / 32;  // blocks of 32 rows at a time
         static_assert(kRowsEach >= 1 && TM % kRowsEach == 0, "a block of rows fits");
-        // (nothing reads the buffers after the last step's barrier)
+        // (nothing reads the buffers any more: the last barrier is behind the last read)
         char* mine = lds + w * (kBuffers * kBuffer / W);
         const uint32_t c0 = n0 + wn * TN * 32;
 #pragma unroll
@@ -422,17 +473,15 @@ __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_mx_many_kernel(
     });
 }
 
-template <int BM, int BN, int WM, int WN>
+template <int BM, int BN, int WM, int WN, int GROUPS>
 hipError_t launch_many(const ProductMxArgs& a, hipStream_t s) {
     const uint32_t nblocks = (a.cols + BN - 1) / BN, threads = WM * WN * 64;
     const uint64_t blocks = most_tiles(a, BM) * nblocks;
     if (blocks + 8 > 0xffffffffull / threads) return hipErrorInvalidConfiguration;
     const dim3 grid((uint32_t)((blocks + 7) / 8 * 8));
-    const int direct = (((uintptr_t)a.a | a.lda) % 16 == 0 ? 1 : 0) | (((uintptr_t)a.b | a.ldb) % 16 == 0 ? 2 : 0);
-    if (direct == 3) hipLaunchKernelGGL((hccl_moe_product_mx_many_kernel<BM, BN, WM, WN, 3>), grid, dim3(threads), 0, s, a, nblocks);
-    else if (direct == 2) hipLaunchKernelGGL((hccl_moe_product_mx_many_kernel<BM, BN, WM, WN, 2>), grid, dim3(threads), 0, s, a, nblocks);
-    else if (direct == 1) hipLaunchKernelGGL((hccl_moe_product_mx_many_kernel<BM, BN, WM, WN, 1>), grid, dim3(threads), 0, s, a, nblocks);
-    else hipLaunchKernelGGL((hccl_moe_product_mx_many_kernel<BM, BN, WM, WN, 0>), grid, dim3(threads), 0, s, a, nblocks);
+    const bool direct = (((uintptr_t)a.a | a.lda | (uintptr_t)a.b | a.ldb) % 16) == 0;
+    if (direct) hipLaunchKernelGGL((hccl_moe_product_mx_many_kernel<BM, BN, WM, WN, GROUPS, true>), grid, dim3(threads), 0, s, a, nblocks);
+    else hipLaunchKernelGGL((hccl_moe_product_mx_many_kernel<BM, BN, WM, WN, GROUPS, false>), grid, dim3(threads), 0, s, a, nblocks);
     return hipGetLastError();
 }
 
@@ -452,10 +501,10 @@ hipError_t launch_product_mx(const ProductMxArgs& a, int cus, hipStream_t s) {
         return (a.offsets ? a.rows / bm + (spread + 1) / 2 : (a.rows + bm - 1) / bm) * ((a.cols + bn - 1) / bn);
     };
     const uint64_t most = a.inner >= kMxBlock ? (uint64_t)cus * 3 / 4 : ~0ull;  // (tiles want 16 bytes of codes a row)
-    if (each >= 128 && blocks(256, 256) >= most) return launch_many<256, 256, 2, 4>(a, s);
-    if (each >= 32 && blocks(128, 128) >= most) return launch_many<128, 128, 2, 2>(a, s);
-    if (each >= 16 && blocks(64, 128) >= most) return launch_many<64, 128, 1, 4>(a, s);
-    if (each > 64 && a.inner >= kMxBlock && blocks(64, 64) >= (uint64_t)cus / 2) return launch_many<64, 64, 1, 2>(a, s);
+    if (each >= 128 && blocks(256, 256) >= most) return launch_many<256, 256, 2, 4, 2>(a, s);
+    if (each >= 32 && blocks(128, 128) >= most) return launch_many<128, 128, 2, 2, 1>(a, s);
+    if (each >= 16 && blocks(64, 128) >= most) return launch_many<64, 128, 1, 4, 1>(a, s);
+    if (each > 64 && a.inner >= kMxBlock && blocks(64, 64) >= (uint64_t)cus / 2) return launch_many<64, 64, 1, 2, 1>(a, s);
     if (a.offsets ? each <= 8 : a.rows <= 16) {
         const uint64_t tiles = a.offsets ? a.rows / 16 + spread : 1, cols16 = (a.cols + 15) / 16;
         if (tiles * (cols16 / 4) >= (uint64_t)cus) return launch_few<1, 4, 4, 2>(a, s);
