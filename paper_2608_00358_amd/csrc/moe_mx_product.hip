@@ -147,24 +147,24 @@ __global__ __launch_bounds__(W * 64) void hccl_moe_product_mx_few_kernel(Product
 }
 
 // Many rows a segment: BM rows by BN columns a block, in WM x WN waves, k in steps of 64 bytes (128 elements, four blocks)
-// through four LDS buffers, three steps ahead: by loads that go to LDS directly (DIRECT: rows and weights are 16-byte
-// aligned) or through registers (any alignment, and the last step of an inner size that is no multiple of 128, where codes
-// past the end are zero).
+// through BUFFERS LDS buffers: one is multiplied while the others are filled, by loads that go to LDS directly (DIRECT:
+// rows and weights are 16-byte aligned) or through registers (any alignment, and the last step of an inner size that is no
+// multiple of 128, where codes past the end are zero).
 //
-// A wave reads a step's fragments and their scales from LDS, waits for them, and multiplies them. With two GROUPS, waves
-// 0 to 3 and 4 to 7, which share the SIMDs, the second is half a step behind: one reads while the other multiplies, and
-// barriers between the halves keep it so. With one, other blocks on the CU fill the gap. Reads are one block of assembly
-// with its wait: the compiler, which cannot tell which loads to LDS a read depends on, would have each wait for all of them.
+// A wave reads a step's fragments from LDS, waits for them, and multiplies them. With two GROUPS, waves 0 to 3 and 4 to 7,
+// which share the SIMDs, the second is half a step behind: one reads while the other multiplies, and barriers between the
+// halves keep it so. With one, other blocks on the CU fill the gap. Reads are one block of assembly with its wait: the
+// compiler, which cannot tell which loads to LDS a read depends on, would have each wait for all of them.
 //
 // LDS holds a row's 64 bytes as 4 chunks of 16; chunk c of row r lies in slot c ^ (r / 4 & 3), so that the
 // 16 lanes served together, which read one chunk of 16 rows, use different banks. A direct load writes its 64 lanes one
 // after the other, so a lane reads the chunk that belongs in its slot. The lanes' halves take chunks 0 and 2 in a step's
 // first part and 1 and 3 in its second, so that a half's two scale bytes are neighbours.
 //
-// Scales: a thread has one row, of the tile's rows or columns, whose next 16 scale bytes (four steps) it reads into a
-// register four steps ahead and puts into LDS three steps before they count, there being two such buffers.
+// Scales: a thread has kRows rows, of the tile's rows or columns, whose next 16 scale bytes (four steps) it reads into a
+// register a step after those before went to LDS, each half's 8 bytes together. A wave has its fragments' scales of four
+// steps in registers, so one buffer does.
 constexpr uint32_t kStep = 64;
-constexpr uint32_t kBuffers = 4;
 constexpr uint32_t kBand = 4;
 
 typedef __attribute__((address_space(3))) void* lds_ptr;
@@ -183,61 +183,75 @@ __device__ __forceinline__ void meet() {
 __device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(lds_ptr)p; }
 __device__ __forceinline__ void lds_write(uint32_t at, const v4u& v) { asm volatile("ds_write_b128 %0, %1" ::"v"(at), "v"(v) : "memory"); }
 
-// A step's fragments of a wave: TM of rows, TN of columns, two parts each, and their scales, 16 bits each.
+// A step's fragments of a wave: TM of rows, TN of columns, two parts each; and the scales of four steps, 16 bits each.
 template <int TM, int TN>
 struct Fragments {
     v4i a[2][TM], b[2][TN];
-    uint32_t sa[TM], sb[TN];
+    v2u sa[TM], sb[TN];
 };
 // (the distance of fragments is 32 rows: 2048 bytes of codes, 512 of scales)
-__device__ __forceinline__ void read_fragments(Fragments<4, 2>& f, uint32_t a0, uint32_t a1, uint32_t b0, uint32_t b1, uint32_t sa, uint32_t sb) {
+__device__ __forceinline__ void read_codes(Fragments<4, 2>& f, uint32_t a0, uint32_t a1, uint32_t b0, uint32_t b1) {
     asm volatile(
-        "ds_read_b128 %0, %18\n\tds_read_b128 %8, %20\n\tds_read_b128 %9, %20 offset:2048\n\t"
-        "ds_read_u16 %12, %22\n\tds_read_u16 %13, %22 offset:512\n\tds_read_u16 %14, %22 offset:1024\n\tds_read_u16 %15, %22 offset:1536\n\t"
-        "ds_read_u16 %16, %23\n\tds_read_u16 %17, %23 offset:512\n\t"
-        "ds_read_b128 %1, %18 offset:2048\n\tds_read_b128 %2, %18 offset:4096\n\tds_read_b128 %3, %18 offset:6144\n\t"
-        "ds_read_b128 %4, %19\n\tds_read_b128 %10, %21\n\tds_read_b128 %11, %21 offset:2048\n\t"
-        "ds_read_b128 %5, %19 offset:2048\n\tds_read_b128 %6, %19 offset:4096\n\tds_read_b128 %7, %19 offset:6144\n\t"
-        "s_waitcnt lgkmcnt(0)"
+        "ds_read_b128 %0, %12\n\tds_read_b128 %8, %14\n\tds_read_b128 %9, %14 offset:2048\n\tds_read_b128 %1, %12 offset:2048\n\t"
+        "ds_read_b128 %2, %12 offset:4096\n\tds_read_b128 %3, %12 offset:6144\n\tds_read_b128 %4, %13\n\tds_read_b128 %10, %15\n\t"
+        "ds_read_b128 %11, %15 offset:2048\n\tds_read_b128 %5, %13 offset:2048\n\tds_read_b128 %6, %13 offset:4096\n\t"
+        "ds_read_b128 %7, %13 offset:6144\n\ts_waitcnt lgkmcnt(0)"
         : "=&v"(f.a[0][0]), "=&v"(f.a[0][1]), "=&v"(f.a[0][2]), "=&v"(f.a[0][3]), "=&v"(f.a[1][0]), "=&v"(f.a[1][1]), "=&v"(f.a[1][2]), "=&v"(f.a[1][3]),
-          "=&v"(f.b[0][0]), "=&v"(f.b[0][1]), "=&v"(f.b[1][0]), "=&v"(f.b[1][1]),
-          "=&v"(f.sa[0]), "=&v"(f.sa[1]), "=&v"(f.sa[2]), "=&v"(f.sa[3]), "=&v"(f.sb[0]), "=&v"(f.sb[1])
-        : "v"(a0), "v"(a1), "v"(b0), "v"(b1), "v"(sa), "v"(sb)
+          "=&v"(f.b[0][0]), "=&v"(f.b[0][1]), "=&v"(f.b[1][0]), "=&v"(f.b[1][1])
+        : "v"(a0), "v"(a1), "v"(b0), "v"(b1)
         : "memory");
 }
-__device__ __forceinline__ void read_fragments(Fragments<2, 2>& f, uint32_t a0, uint32_t a1, uint32_t b0, uint32_t b1, uint32_t sa, uint32_t sb) {
+__device__ __forceinline__ void read_codes(Fragments<2, 2>& f, uint32_t a0, uint32_t a1, uint32_t b0, uint32_t b1) {
     asm volatile(
-        "ds_read_b128 %0, %12\n\tds_read_b128 %4, %14\n\tds_read_b128 %5, %14 offset:2048\n\t"
-        "ds_read_u16 %8, %16\n\tds_read_u16 %9, %16 offset:512\n\tds_read_u16 %10, %17\n\tds_read_u16 %11, %17 offset:512\n\t"
-        "ds_read_b128 %1, %12 offset:2048\n\tds_read_b128 %2, %13\n\tds_read_b128 %6, %15\n\tds_read_b128 %7, %15 offset:2048\n\t"
-        "ds_read_b128 %3, %13 offset:2048\n\t"
+        "ds_read_b128 %0, %8\n\tds_read_b128 %4, %10\n\tds_read_b128 %5, %10 offset:2048\n\tds_read_b128 %1, %8 offset:2048\n\t"
+        "ds_read_b128 %2, %9\n\tds_read_b128 %6, %11\n\tds_read_b128 %7, %11 offset:2048\n\tds_read_b128 %3, %9 offset:2048\n\t"
         "s_waitcnt lgkmcnt(0)"
-        : "=&v"(f.a[0][0]), "=&v"(f.a[0][1]), "=&v"(f.a[1][0]), "=&v"(f.a[1][1]), "=&v"(f.b[0][0]), "=&v"(f.b[0][1]), "=&v"(f.b[1][0]), "=&v"(f.b[1][1]),
-          "=&v"(f.sa[0]), "=&v"(f.sa[1]), "=&v"(f.sb[0]), "=&v"(f.sb[1])
-        : "v"(a0), "v"(a1), "v"(b0), "v"(b1), "v"(sa), "v"(sb)
+        : "=&v"(f.a[0][0]), "=&v"(f.a[0][1]), "=&v"(f.a[1][0]), "=&v"(f.a[1][1]), "=&v"(f.b[0][0]), "=&v"(f.b[0][1]), "=&v"(f.b[1][0]), "=&v"(f.b[1][1])
+        : "v"(a0), "v"(a1), "v"(b0), "v"(b1)
         : "memory");
 }
-__device__ __forceinline__ void read_fragments(Fragments<2, 1>& f, uint32_t a0, uint32_t a1, uint32_t b0, uint32_t b1, uint32_t sa, uint32_t sb) {
+__device__ __forceinline__ void read_codes(Fragments<2, 1>& f, uint32_t a0, uint32_t a1, uint32_t b0, uint32_t b1) {
     asm volatile(
-        "ds_read_b128 %0, %9\n\tds_read_b128 %4, %11\n\t"
-        "ds_read_u16 %6, %13\n\tds_read_u16 %7, %13 offset:512\n\tds_read_u16 %8, %14\n\t"
-        "ds_read_b128 %1, %9 offset:2048\n\tds_read_b128 %2, %10\n\tds_read_b128 %5, %12\n\tds_read_b128 %3, %10 offset:2048\n\t"
+        "ds_read_b128 %0, %6\n\tds_read_b128 %4, %8\n\tds_read_b128 %1, %6 offset:2048\n\t"
+        "ds_read_b128 %2, %7\n\tds_read_b128 %5, %9\n\tds_read_b128 %3, %7 offset:2048\n\t"
         "s_waitcnt lgkmcnt(0)"
-        : "=&v"(f.a[0][0]), "=&v"(f.a[0][1]), "=&v"(f.a[1][0]), "=&v"(f.a[1][1]), "=&v"(f.b[0][0]), "=&v"(f.b[1][0]), "=&v"(f.sa[0]), "=&v"(f.sa[1]), "=&v"(f.sb[0])
-        : "v"(a0), "v"(a1), "v"(b0), "v"(b1), "v"(sa), "v"(sb)
+        : "=&v"(f.a[0][0]), "=&v"(f.a[0][1]), "=&v"(f.a[1][0]), "=&v"(f.a[1][1]), "=&v"(f.b[0][0]), "=&v"(f.b[1][0])
+        : "v"(a0), "v"(a1), "v"(b0), "v"(b1)
         : "memory");
+}
+template <int TM, int TN>
+__device__ __forceinline__ void read_scales(Fragments<TM, TN>& f, uint32_t a, uint32_t b) {
+    static_assert((TM == 4 && TN == 2) || (TM == 2 && TN <= 2), "the fragments above");
+    if constexpr (TM == 4)
+        asm volatile("ds_read_b64 %0, %6\n\tds_read_b64 %1, %6 offset:512\n\tds_read_b64 %2, %6 offset:1024\n\tds_read_b64 %3, %6 offset:1536\n\t"
+                     "ds_read_b64 %4, %7\n\tds_read_b64 %5, %7 offset:512\n\ts_waitcnt lgkmcnt(0)"
+                     : "=&v"(f.sa[0]), "=&v"(f.sa[1]), "=&v"(f.sa[2]), "=&v"(f.sa[3]), "=&v"(f.sb[0]), "=&v"(f.sb[1])
+                     : "v"(a), "v"(b)
+                     : "memory");
+    else if constexpr (TN == 2)
+        asm volatile("ds_read_b64 %0, %4\n\tds_read_b64 %1, %4 offset:512\n\tds_read_b64 %2, %5\n\tds_read_b64 %3, %5 offset:512\n\t"
+                     "s_waitcnt lgkmcnt(0)"
+                     : "=&v"(f.sa[0]), "=&v"(f.sa[1]), "=&v"(f.sb[0]), "=&v"(f.sb[1])
+                     : "v"(a), "v"(b)
+                     : "memory");
+    else
+        asm volatile("ds_read_b64 %0, %3\n\tds_read_b64 %1, %3 offset:512\n\tds_read_b64 %2, %4\n\ts_waitcnt lgkmcnt(0)"
+                     : "=&v"(f.sa[0]), "=&v"(f.sa[1]), "=&v"(f.sb[0])
+                     : "v"(a), "v"(b)
+                     : "memory");
 }
 
-template <int BM, int BN, int WM, int WN, int GROUPS, bool DIRECT>
-__global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_mx_many_kernel(ProductMxArgs a, uint32_t nblocks) {
+template <int BM, int BN, int WM, int WN, int GROUPS, int BUFFERS, bool DIRECT>
+__global__ __launch_bounds__(WM * WN * 64, 2) void hccl_moe_product_mx_many_kernel(ProductMxArgs a, uint32_t nblocks) {
     constexpr int W = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
     constexpr int LA = BM / 16 / W, LB = BN / 16 / W, LN = LA + LB;  // loads a wave makes for a step: 16 rows each
-    static_assert(BM % (16 * W) == 0 && BN % (16 * W) == 0 && 2 * LN < 16, "whole loads, and a counter that holds them");
-    static_assert(BM + BN <= W * 64, "a thread has the scales of one row");
+    constexpr uint32_t kAhead = BUFFERS - 1;
+    static_assert(BM % (16 * W) == 0 && BN % (16 * W) == 0 && (BUFFERS - 2) * LN < 16, "whole loads, and a counter that holds them");
     static_assert(GROUPS == 1 || W == 8, "two groups of a wave a SIMD");
-    constexpr uint32_t kBuffer = (BM + BN) * kStep, kScales = (BM + BN) * 16;
-    __shared__ __attribute__((aligned(256))) char lds[kBuffers * kBuffer];
-    __shared__ __attribute__((aligned(256))) char lds_scale[2 * kScales];
+    constexpr int kRows = (BM + BN + W * 64 - 1) / (W * 64);
+    constexpr uint32_t kBuffer = (BM + BN) * kStep;
+    __shared__ __attribute__((aligned(256))) char lds[BUFFERS * kBuffer];
+    __shared__ __attribute__((aligned(256))) char lds_scale[(BM + BN) * 16];
     const uint32_t lane = threadIdx.x & 63, w = first_lane(threadIdx.x >> 6);
 
     // Blocks go to the XCDs in turn; each XCD gets neighbouring tiles, in bands of kBand column blocks, so
@@ -267,9 +281,14 @@ __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_mx_many_kernel(
     const uint8_t* src[LN];
 #pragma unroll
     for (int i = 0; i < LN; ++i) src[i] = source(i) + chunk;
-    auto slot = [&](uint32_t s, int i) { return lds + (s % kBuffers) * kBuffer + (i < LA ? (w * LA + i) * 16 : BM + (w * LB + i - LA) * 16) * kStep; };
-    const uint8_t* scale_src = threadIdx.x < BM ? a.a_scale + row_of(threadIdx.x) * a.ldas : a.b_scale + col_of(threadIdx.x < BM + BN ? threadIdx.x - BM : 0) * a.ldbs;
-    const uint32_t scale_bytes = threadIdx.x < BM + BN ? (a.inner + kMxBlock - 1) / kMxBlock : 0;
+    auto slot = [&](uint32_t s, int i) { return lds + (s % BUFFERS) * kBuffer + (i < LA ? (w * LA + i) * 16 : BM + (w * LB + i - LA) * 16) * kStep; };
+    const uint8_t* scale_src[kRows];
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+        const uint32_t at = r * W * 64 + threadIdx.x;
+        scale_src[r] = at < BM ? a.a_scale + row_of(at) * a.ldas : a.b_scale + col_of(at < BM + BN ? at - BM : 0) * a.ldbs;
+    }
+    const uint32_t scale_bytes = (a.inner + kMxBlock - 1) / kMxBlock;
 
     v16f acc[TN][TM];
 #pragma unroll
@@ -284,8 +303,8 @@ __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_mx_many_kernel(
     // waves without rows, those that have some share out the matrix units.
     const uint32_t wm = w / WN, wn = w % WN;
     const bool second = GROUPS == 2 && w >= 4;
-    v4u held[LN];    // on their way through registers
-    v4u held_scale;  // scales of four steps, on their way
+    v4u held[LN];           // on their way through registers
+    v4u held_scale[kRows];  // scales of four steps, on their way
     auto put = [&](uint32_t s, int i, const v4u& v) { lds_write(lds_address(slot(s, i)) + lane * 16, v); };
     // Load i of those that bring in step s, a whole one; through registers, the one before goes to its buffer meanwhile.
     auto fetch = [&](uint32_t s, int i) {
@@ -301,52 +320,44 @@ __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_mx_many_kernel(
         for (int i = 0; i < LN; ++i)
             put(s, i, i < LA ? load_codes<true, true>(source(i), s * kStep + chunk, a.inner) : load_codes<true, false>(source(i), s * kStep + chunk, a.inner));
     };
-    // What is left to bring in when step s + 3 is none of the whole ones any more: once, before step s, when the buffers of
-    // the steps before s are free and few registers are in use.
-    auto finish = [&] {
-        if (whole_steps < 3) return;  // (all of it was brought in at the beginning)
-        if constexpr (!DIRECT) {
+    auto fetch_scales = [&](uint32_t four) {
 #pragma unroll
-            for (int i = 0; i < LN; ++i) put(whole_steps - 1, i, held[i]);
+        for (int r = 0; r < kRows; ++r) held_scale[r] = load_bytes<false>(scale_src[r], four * 16, scale_bytes);
+    };
+    auto put_scales = [&] {
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            const v4u& v = held_scale[r];
+            const v4u halves = {__builtin_amdgcn_perm(v[1], v[0], 0x05040100u), __builtin_amdgcn_perm(v[3], v[2], 0x05040100u),
+                                __builtin_amdgcn_perm(v[1], v[0], 0x07060302u), __builtin_amdgcn_perm(v[3], v[2], 0x07060302u)};
+            const uint32_t at = r * W * 64 + threadIdx.x;
+            if ((r + 1) * W * 64 <= BM + BN || at < BM + BN) lds_write(lds_address(lds_scale) + at * 16, halves);
         }
-        if (whole_steps < steps) bring(whole_steps);
-    };
-    auto fetch_scales = [&](uint32_t four) { held_scale = load_bytes<false>(scale_src, four * 16, scale_bytes); };
-    auto put_scales = [&](uint32_t four) {
-        if (BM + BN == W * 64 || threadIdx.x < BM + BN) lds_write(lds_address(lds_scale) + (four & 1) * kScales + threadIdx.x * 16, held_scale);
-    };
-    // In the second of four steps s: the scales of the next four go to LDS, those after them on their way.
-    auto stage = [&](uint32_t s) {
-        if ((s & 3) != 1) return;
-        put_scales(s / 4 + 1);
-        fetch_scales(s / 4 + 2);
     };
 
     // a lane's places in a buffer: its row of the wave's first fragment, the chunk of its half
     const uint32_t place = (lane & 31) * kStep + ((lane >> 5) * 2 ^ (lane >> 2 & 3)) * 16;
     const uint32_t at_a = lds_address(lds) + wm * TM * 32 * kStep + place, at_b = lds_address(lds) + (BM + wn * TN * 32) * kStep + place;
-    const uint32_t at_sa = lds_address(lds_scale) + (wm * TM * 32 + (lane & 31)) * 16 + (lane >> 5) * 2;
+    const uint32_t at_sa = lds_address(lds_scale) + (wm * TM * 32 + (lane & 31)) * 16 + (lane >> 5) * 8;
     const uint32_t at_sb = at_sa + (BM + wn * TN * 32 - wm * TM * 32) * 16;
     Fragments<TM, TN> f;
-    auto read = [&](uint32_t s) {
-        const uint32_t at = (s % kBuffers) * kBuffer, at_scale = (s / 4 & 1) * kScales + (s & 3) * 4;
-        read_fragments(f, at_a + at, (at_a ^ 16) + at, at_b + at, (at_b ^ 16) + at, at_sa + at_scale, at_sb + at_scale);
-    };
-    // A step's matrix instructions, with the loads that bring in step s + 3 (INNER: a whole one) between them: a wave that makes
-    // its loads in one go waits for the units that take them, and its SIMD with it.
-    auto multiply = [&](uint32_t s, auto inner) {
-        constexpr int kMfmas = 2 * TM * TN;
+    // A step's matrix instructions, with the loads that bring in step s + kAhead (INNER: a whole one) between them: a wave that
+    // makes its loads in one go waits for the units that take them, and its SIMD with it. PHASE: the step's place among four.
+    auto multiply = [&](uint32_t s, auto phase, auto inner) {
+        constexpr int kMfmas = 2 * TM * TN, P = decltype(phase)::value;
         int next = 0;
 #pragma unroll
         for (int i = 0; i < kMfmas; ++i) {
             const int x = i / TN % TM, y = i % TN;
             if (i < kMfmas / 2)
-                acc[y][x] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(whole(f.b[0][y]), whole(f.a[0][x]), acc[y][x], kFp4, kFp4, 0, f.sb[y], 0, f.sa[x]);
+                acc[y][x] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(whole(f.b[0][y]), whole(f.a[0][x]), acc[y][x], kFp4, kFp4, P % 2 * 2, f.sb[y][P / 2], P % 2 * 2,
+                                                                            f.sa[x][P / 2]);
             else
-                acc[y][x] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(whole(f.b[1][y]), whole(f.a[1][x]), acc[y][x], kFp4, kFp4, 1, f.sb[y], 1, f.sa[x]);
+                acc[y][x] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(whole(f.b[1][y]), whole(f.a[1][x]), acc[y][x], kFp4, kFp4, P % 2 * 2 + 1, f.sb[y][P / 2],
+                                                                            P % 2 * 2 + 1, f.sa[x][P / 2]);
             __builtin_amdgcn_sched_barrier(0);
             if (inner.value)
-                for (; next < LN && next * kMfmas < (i + 1) * LN; ++next) fetch(s + 3, next);
+                for (; next < LN && next * kMfmas < (i + 1) * LN; ++next) fetch(s + kAhead, next);
             __builtin_amdgcn_sched_barrier(0);
         }
         // (here, and not sunk behind what follows)
@@ -354,73 +365,102 @@ __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_mx_many_kernel(
         for (int y = 0; y < TN; ++y)
 #pragma unroll
             for (int x = 0; x < TM; ++x) {
-                // (in the registers where the compiler has them: blocks of 4 waves may have accumulation registers)
-                if constexpr (W == 8) asm volatile("" : "+v"(acc[y][x]));
+                if constexpr (TM * TN >= 8) asm volatile("" : "+v"(acc[y][x]));
                 else asm volatile("" : "+a"(acc[y][x]));
             }
     };
-    auto load_only = [&](uint32_t s, auto inner) {  // the same of a wave without rows
-        if (inner.value) {
-#pragma unroll
-            for (int i = 0; i < LN; ++i) fetch(s + 3, i);
+    // One step. ON: the wave has rows. Loads of step s + 1 have to be there for all waves when the first group reads it: that
+    // group waits for its own at the end of step s, when those of the steps behind may be on their way, and the second in the
+    // middle of it, when it has made one step's less.
+    auto pass = [&](uint32_t s, auto phase, auto on, auto inner) {
+        constexpr int P = decltype(phase)::value;
+        if (on.value) {
+            const uint32_t at = (s % BUFFERS) * kBuffer;
+            if (P == 0) read_scales(f, at_sa, at_sb);
+            read_codes(f, at_a + at, (at_a ^ 16) + at, at_b + at, (at_b ^ 16) + at);
         }
-    };
-    // The first group waits for its loads of step s + 1 at the end of step s, those of two further steps being on their
-    // way; the second, half a step later, when it has made those of one.
-    auto walk = [&](auto reading, auto working) {
-        auto pass = [&](uint32_t s, auto inner) {
-            reading(s);
-            if constexpr (GROUPS == 2) {
-                if (second && DIRECT) {
-                    if (inner.value) wait_loads<LN>();
-                    else wait_loads<0>();
-                }
-                meet();
-            }
-            working(s, inner);
-            stage(s);
-            if (!second || !DIRECT) {
-                if (!DIRECT) __builtin_amdgcn_s_waitcnt(0xc07f);  // LDS alone
-                else if (inner.value) wait_loads<2 * LN>();
+        if constexpr (GROUPS == 2) {
+            if (second && DIRECT) {
+                if (inner.value) wait_loads<(BUFFERS - 3) * LN>();
                 else wait_loads<0>();
-            } else {
-                __builtin_amdgcn_s_waitcnt(0xc07f);
             }
-            if (inner.value || !second || s + 1 < steps) meet();  // (the last barrier is the first group's)
-        };
+            meet();
+        }
+        if (!inner.value) {  // what is left to bring in
+            if (!DIRECT && s + kAhead - 1 < whole_steps) {
+#pragma unroll
+                for (int i = 0; i < LN; ++i) put(s + kAhead - 1, i, held[i]);
+            }
+            if (s + kAhead < whole_steps) {
+#pragma unroll
+                for (int i = 0; i < LN; ++i) {
+                    if constexpr (DIRECT) fetch(s + kAhead, i);
+                    else held[i] = load16<1>(src[i] + (uint64_t)(s + kAhead) * kStep);
+                }
+            } else if (s + kAhead == whole_steps && whole_steps < steps) {
+                bring(whole_steps);
+            }
+        }
+        if (P == 1) {  // every wave has the scales of these four steps
+            put_scales();
+            fetch_scales(s / 4 + 2);
+        }
+        if (on.value) multiply(s, phase, inner);
+        else if (inner.value) {
+#pragma unroll
+            for (int i = 0; i < LN; ++i) fetch(s + kAhead, i);
+        }
+        if (!DIRECT || second) __builtin_amdgcn_s_waitcnt(0xc07f);  // LDS alone
+        else if (inner.value) wait_loads<(BUFFERS - 2) * LN>();
+        else wait_loads<0>();
+        if (inner.value || !second || s + 1 < steps) meet();  // (the last barrier is the first group's)
+    };
+    auto walk = [&](auto on) {
+        const std::integral_constant<int, 0> p0;
+        const std::integral_constant<int, 1> p1;
+        const std::integral_constant<int, 2> p2;
+        const std::integral_constant<int, 3> p3;
         if (second) meet();
         uint32_t s = 0;
 #pragma unroll 1
-        for (; s + 3 < whole_steps; ++s) pass(s, std::true_type());
-        finish();
+        for (; s + 3 + kAhead < whole_steps; s += 4) {
+            pass(s, p0, on, std::true_type());
+            pass(s + 1, p1, on, std::true_type());
+            pass(s + 2, p2, on, std::true_type());
+            pass(s + 3, p3, on, std::true_type());
+        }
 #pragma unroll 1
-        for (; s < steps; ++s) pass(s, std::false_type());
+        for (; s < steps; s += 4) {
+            pass(s, p0, on, std::false_type());
+            if (s + 1 < steps) pass(s + 1, p1, on, std::false_type());
+            if (s + 2 < steps) pass(s + 2, p2, on, std::false_type());
+            if (s + 3 < steps) pass(s + 3, p3, on, std::false_type());
+        }
     };
     if (steps) {
         fetch_scales(0);
         if constexpr (DIRECT) {
-            const uint32_t n = whole_steps < 3 ? whole_steps : 3;
+            const uint32_t n = whole_steps < kAhead ? whole_steps : kAhead;
             for (uint32_t s = 0; s < n; ++s)
 #pragma unroll
                 for (int i = 0; i < LN; ++i) fetch(s, i);
         } else {
-            if (whole_steps > 0) bring(0);
-            if (whole_steps > 1) bring(1);
-            if (whole_steps > 2) {
+            for (uint32_t s = 0; s < kAhead - 1 && s < whole_steps; ++s) bring(s);
+            if (whole_steps >= kAhead) {
 #pragma unroll
-                for (int i = 0; i < LN; ++i) held[i] = load16<1>(src[i] + 2 * kStep);
+                for (int i = 0; i < LN; ++i) held[i] = load16<1>(src[i] + (kAhead - 1) * kStep);
             }
         }
-        if (whole_steps < 3 && whole_steps < steps) bring(whole_steps);
-        put_scales(0);
+        if (whole_steps < kAhead && whole_steps < steps) bring(whole_steps);
+        put_scales();
         fetch_scales(1);
         wait_loads<0>();
         meet();
         if (rows.first + wm * TM * 32 >= rows.end) {
-            walk([](uint32_t) {}, load_only);
+            walk(std::false_type());
             return;
         }
-        walk(read, multiply);
+        walk(std::true_type());
     }
 
     // The wave's TM x TN blocks leave through its own part of LDS, as rows of TN * 32 results: lanes that hold
@@ -429,10 +469,10 @@ __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_mx_many_kernel(
         constexpr int DT = decltype(type)::value;
         constexpr int ES = kSize<DT>;
         constexpr uint32_t kLine = TN * 32 * ES, kChunks = kLine / 16;  // bytes of a row
-        constexpr int kRowsEach = kBuffers * kBuffer / W / kLine >= TM * 32 ? TM : kBuffers * kBuffer / W / kLine / 32;  // blocks of 32 rows at a time
+        constexpr int kRowsEach = BUFFERS * kBuffer / W / kLine >= TM * 32 ? TM : BUFFERS * kBuffer / W / kLine / 32;  // blocks of 32 rows at a time
         static_assert(kRowsEach >= 1 && TM % kRowsEach == 0, "a block of rows fits");
         // (nothing reads the buffers any more: the last barrier is behind the last read)
-        char* mine = lds + w * (kBuffers * kBuffer / W);
+        char* mine = lds + w * (BUFFERS * kBuffer / W);
         const uint32_t c0 = n0 + wn * TN * 32;
 #pragma unroll
         for (int x0 = 0; x0 < TM; x0 += kRowsEach) {
@@ -473,15 +513,15 @@ __global__ __launch_bounds__(WM * WN * 64) void hccl_moe_product_mx_many_kernel(
     });
 }
 
-template <int BM, int BN, int WM, int WN, int GROUPS>
+template <int BM, int BN, int WM, int WN, int GROUPS, int BUFFERS>
 hipError_t launch_many(const ProductMxArgs& a, hipStream_t s) {
     const uint32_t nblocks = (a.cols + BN - 1) / BN, threads = WM * WN * 64;
     const uint64_t blocks = most_tiles(a, BM) * nblocks;
     if (blocks + 8 > 0xffffffffull / threads) return hipErrorInvalidConfiguration;
     const dim3 grid((uint32_t)((blocks + 7) / 8 * 8));
     const bool direct = (((uintptr_t)a.a | a.lda | (uintptr_t)a.b | a.ldb) % 16) == 0;
-    if (direct) hipLaunchKernelGGL((hccl_moe_product_mx_many_kernel<BM, BN, WM, WN, GROUPS, true>), grid, dim3(threads), 0, s, a, nblocks);
-    else hipLaunchKernelGGL((hccl_moe_product_mx_many_kernel<BM, BN, WM, WN, GROUPS, false>), grid, dim3(threads), 0, s, a, nblocks);
+    if (direct) hipLaunchKernelGGL((hccl_moe_product_mx_many_kernel<BM, BN, WM, WN, GROUPS, BUFFERS, true>), grid, dim3(threads), 0, s, a, nblocks);
+    else hipLaunchKernelGGL((hccl_moe_product_mx_many_kernel<BM, BN, WM, WN, GROUPS, BUFFERS, false>), grid, dim3(threads), 0, s, a, nblocks);
     return hipGetLastError();
 }
 
@@ -501,10 +541,10 @@ hipError_t launch_product_mx(const ProductMxArgs& a, int cus, hipStream_t s) {
         return (a.offsets ? a.rows / bm + (spread + 1) / 2 : (a.rows + bm - 1) / bm) * ((a.cols + bn - 1) / bn);
     };
     const uint64_t most = a.inner >= kMxBlock ? (uint64_t)cus * 3 / 4 : ~0ull;  // (tiles want 16 bytes of codes a row)
-    if (each >= 128 && blocks(256, 256) >= most) return launch_many<256, 256, 2, 4, 2>(a, s);
-    if (each >= 32 && blocks(128, 128) >= most) return launch_many<128, 128, 2, 2, 1>(a, s);
-    if (each >= 16 && blocks(64, 128) >= most) return launch_many<64, 128, 1, 4, 1>(a, s);
-    if (each > 64 && a.inner >= kMxBlock && blocks(64, 64) >= (uint64_t)cus / 2) return launch_many<64, 64, 1, 2, 1>(a, s);
+    if (each >= 128 && blocks(256, 256) >= most) return launch_many<256, 256, 2, 4, 2, 4>(a, s);
+    if (each >= 32 && blocks(128, 128) >= most) return launch_many<128, 128, 2, 2, 1, 3>(a, s);
+    if (each >= 16 && blocks(64, 128) >= most) return launch_many<64, 128, 1, 4, 1, 3>(a, s);
+    if (each > 64 && a.inner >= kMxBlock && blocks(64, 64) >= (uint64_t)cus / 2) return launch_many<64, 64, 1, 2, 1, 3>(a, s);
     if (a.offsets ? each <= 8 : a.rows <= 16) {
         const uint64_t tiles = a.offsets ? a.rows / 16 + spread : 1, cols16 = (a.cols + 15) / 16;
         if (tiles * (cols16 / 4) >= (uint64_t)cus) return launch_few<1, 4, 4, 2>(a, s);
