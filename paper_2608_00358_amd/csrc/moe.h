@@ -164,7 +164,7 @@ hipError_t launch_combine_backward(const CombineBackwardArgs& a, hcclDataType_t 
 hipError_t launch_quantize_mx(const QuantizeMxArgs& a, hcclDataType_t dt, bool gated, hipStream_t s);
 hipError_t launch_dequantize_mx(const DequantizeMxArgs& a, hcclDataType_t dt, hipStream_t s);
 hipError_t launch_product_mx(const ProductMxArgs& a, int cus, hipStream_t s);
-hipError_t launch_layer_mx(const LayerMxArgs& a, hcclDataType_t dt, hipStream_t s);
+hipError_t launch_layer_mx(const LayerMxArgs& a, hcclDataType_t dt, int cus, hipStream_t s);
 hipError_t launch_product(const ProductArgs& a, hcclDataType_t dt, int cus, hipStream_t s);
 
 }  // namespace hccl

@@ -611,7 +611,7 @@ hcclResult_t hccl_moe_layer_mx(hcclComm_t comm, const hcclRouter_t* router, cons
         a.held = (uint32_t)held;
         return enqueue(c, [&] {
             const hipError_t e = launch_route(r, logits_dtype, (hipStream_t)stream);
-            return e != hipSuccess || a.cols == 0 ? e : launch_layer_mx(a, dtype, (hipStream_t)stream);
+            return e != hipSuccess || a.cols == 0 ? e : launch_layer_mx(a, dtype, api_cus(comm), (hipStream_t)stream);
         });
     });
 }

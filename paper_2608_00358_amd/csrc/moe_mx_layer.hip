@@ -3,6 +3,8 @@
 // in two launches behind the choice. Tokens keep their own type: codes become 16-bit floats exactly (an e2m1 code times
 // a power of two has two bits), rows that 16-bit floats do not hold are split into two or three that add up to them, and
 // the matrix instructions add up the products in 32 bits. Bound by the weights' bytes.
+#include <type_traits>
+
 #include "moe_mx_device.h"
 
 namespace hccl {
@@ -40,38 +42,128 @@ __device__ __forceinline__ void split8(const float (&x)[8], b8 (&t)[TERMS]) {
     }
 }
 
-// Eight elements of a row at e, as terms; those behind the last are 0.
+// Eight elements of a row as they lie in memory; those behind the last are 0.
+template <int DT>
+struct Raw {
+    v4u v[kSize<DT> / 2];
+};
 template <int DT, bool INSIDE>
-__device__ __forceinline__ void load_terms(const char* row, uint32_t e, uint32_t cols, b8 (&t)[kTerms(DT)]) {
+__device__ __forceinline__ void load_raw(const char* row, uint32_t e, uint32_t cols, Raw<DT>& r) {
     constexpr int ES = kSize<DT>;
+    r.v[0] = INSIDE ? load16<ES>(row + (uint64_t)e * ES) : load_row<ES>(row, e, cols);
+    if constexpr (ES == 4) r.v[1] = INSIDE ? load16<4>(row + (uint64_t)e * 4 + 16) : load_row<4>(row, e + 4, cols);
+}
+template <int DT>
+__device__ __forceinline__ void terms_of(const Raw<DT>& r, b8 (&t)[kTerms(DT)]) {
     if constexpr (DT == hcclBf16) {
-        t[0] = __builtin_bit_cast(b8, INSIDE ? load16<2>(row + (uint64_t)e * 2) : load_row<2>(row, e, cols));
+        t[0] = __builtin_bit_cast(b8, r.v[0]);
     } else {
         float x[8];
-        if constexpr (ES == 2) {
-            widen<DT>(INSIDE ? load16<2>(row + (uint64_t)e * 2) : load_row<2>(row, e, cols), x);
+        if constexpr (DT == hcclFp16) {
+            widen<DT>(r.v[0], x);
         } else {
-            float lo[4], hi[4];
-            widen<DT>(INSIDE ? load16<4>(row + (uint64_t)e * 4) : load_row<4>(row, e, cols), lo);
-            widen<DT>(INSIDE ? load16<4>(row + (uint64_t)e * 4 + 16) : load_row<4>(row, e + 4, cols), hi);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = lo[i], x[4 + i] = hi[i];
+            for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(r.v[0][i]), x[4 + i] = __uint_as_float(r.v[1][i]);
         }
         split8<kTerms(DT)>(x, t);
     }
 }
 
-// The routes of expert e, in their order, into `list` (LDS); their number.
-__device__ __forceinline__ uint32_t list_routes(const LayerMxArgs& a, uint32_t e, uint16_t* list, bool write) {
-    const uint32_t lane = threadIdx.x & 63, routes = a.tokens * a.top_k;
-    uint32_t n = 0;
-    for (uint32_t r0 = 0; r0 < routes; r0 += 64) {
-        const bool mine = r0 + lane < routes && (uint32_t)a.index[r0 + lane] - a.first == e;
-        const uint64_t all = __ballot(mine);
-        if (mine && write) list[n + (uint32_t)__popcll(all & ((1ull << lane) - 1))] = (uint16_t)(r0 + lane);
-        n += (uint32_t)__popcll(all);
+constexpr int kWaves = 8;  // of a block
+constexpr uint32_t kMostRoutes = HCCL_MAX_LAYER_TOKENS * HCCL_MAX_TOP_K;
+constexpr uint32_t kMostEntries = HCCL_MAX_EXPERTS + kMostRoutes / 16;  // (of 4 rows an expert has one at most)
+constexpr int kLists = 8;  // more than the entries that a wave has begun: one a step on its way, one that is multiplied and one ahead
+typedef __attribute__((address_space(3))) void* lds_ptr;
+
+// LDS by assembly: the compiler would have a read or write of its own wait for every load to LDS that is on its way, as it
+// cannot tell that they have nothing to do with each other. Reads have their wait in the block.
+__device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(lds_ptr)p; }
+__device__ __forceinline__ uint32_t lds_u16(const uint16_t* p) {
+    uint32_t v;
+    asm volatile("ds_read_u16 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(v) : "v"(lds_address(p)) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t lds_u32(const void* p) {
+    uint32_t v;
+    asm volatile("ds_read_b32 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(v) : "v"(lds_address(p)) : "memory");
+    return v;
+}
+__device__ __forceinline__ void lds_put16(uint16_t* p, uint32_t v) { asm volatile("ds_write_b16 %0, %1" ::"v"(lds_address(p)), "v"(v) : "memory"); }
+__device__ __forceinline__ void lds_add4(float* p, float x, float y, float z, float w) {
+    asm volatile("ds_add_f32 %0, %1\n\tds_add_f32 %0, %2 offset:4\n\tds_add_f32 %0, %3 offset:8\n\tds_add_f32 %0, %4 offset:12" ::"v"(lds_address(p)), "v"(x), "v"(y), "v"(z),
+                 "v"(w)
+                 : "memory");
+}
+
+// What the blocks of both kernels find out about the choices: the held expert of every route, its weight, and the entries: experts
+// that have a route, with `rows` of their routes each, ascending. An entry is the expert, and the first of its routes << 16.
+// Entries have 4, 8 or 16 rows: the least that the expert of most routes needs, so that hardly ever one takes its weights twice.
+struct Choices {
+    uint16_t expert[kMostRoutes];  // 0xffff without one
+    float weight[kMostRoutes];
+    uint32_t entries[kMostEntries], count[HCCL_MAX_EXPERTS], number, rows;
+    uint16_t lists[kWaves][kLists][16];
+};
+__device__ __forceinline__ void find_choices(const LayerMxArgs& a, Choices& c) {
+    const uint32_t lane = threadIdx.x & 63, w = first_lane(threadIdx.x >> 6), routes = a.tokens * a.top_k;
+    constexpr int kEach = (kMostRoutes + kWaves * 64 - 1) / (kWaves * 64);
+    uint32_t expert[kEach];  // (on their way together)
+    float weight[kEach];
+#pragma unroll
+    for (int n = 0; n < kEach; ++n) {
+        const uint32_t r = n * kWaves * 64 + threadIdx.x;
+        if (r < routes) expert[n] = (uint32_t)a.index[r] - a.first, weight[n] = a.weight[r];
     }
-    return n;
+    for (uint32_t e = threadIdx.x; e < a.held; e += kWaves * 64) c.count[e] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < kEach; ++n) {
+        const uint32_t r = n * kWaves * 64 + threadIdx.x;
+        if (r >= routes) break;
+        c.expert[r] = expert[n] < a.held ? (uint16_t)expert[n] : 0xffffu;
+        c.weight[r] = weight[n];
+        if (expert[n] < a.held) atomicAdd(&c.count[expert[n]], 1u);
+    }
+    __syncthreads();
+    if (w == 0) {
+        uint32_t most = 0, all = 0;
+        for (uint32_t e = lane; e < a.held; e += 64) most = max(most, c.count[e]);
+        most = maxu_lanes<64>(most);
+        const uint32_t shift = most <= 4 ? 2 : most <= 8 ? 3 : 4;
+        for (uint32_t e0 = 0; e0 < a.held; e0 += 64) {
+            uint32_t left = e0 + lane < a.held ? c.count[e0 + lane] : 0, first = 0;
+            // an expert's entries: the first of all experts, then the second of those that have one, ...
+            for (uint64_t mask = __ballot(left > 0); mask; mask = __ballot(left > 0)) {
+                if (left) c.entries[all + (uint32_t)__popcll(mask & ((1ull << lane) - 1))] = e0 + lane | first << 16;
+                all += (uint32_t)__popcll(mask);
+                first += 1u << shift;
+                left = left > 1u << shift ? left - (1u << shift) : 0;
+            }
+        }
+        c.number = all;
+        c.rows = 1u << shift;
+    }
+    __syncthreads();
+}
+// An entry's routes, in their order, into a list of the wave; 0xffff where there are fewer.
+__device__ __forceinline__ void list_entry(const LayerMxArgs& a, Choices& c, uint32_t w, uint32_t entry, uint32_t what) {
+    const uint32_t lane = threadIdx.x & 63, routes = a.tokens * a.top_k, e = what & 0xffffu;
+    uint16_t* list = c.lists[w][entry % kLists];
+    if (lane < 16) lds_put16(list + lane, 0xffffu);
+    uint32_t at = 0u - (what >> 16);
+    for (uint32_t r0 = 0; r0 < routes; r0 += 64) {
+        const bool mine = lds_u16(c.expert + (r0 + lane < routes ? r0 + lane : 0)) == e && r0 + lane < routes;
+        const uint64_t all = __ballot(mine);
+        const uint32_t rank = at + (uint32_t)__popcll(all & ((1ull << lane) - 1));
+        if (mine && rank < 16) lds_put16(list + rank, r0 + lane);
+        at += (uint32_t)__popcll(all);
+    }
+}
+// The route of row r of an entry; the first one's where there are fewer.
+__device__ __forceinline__ uint32_t route_of(Choices& c, uint32_t w, uint32_t entry, uint32_t r) {
+    const uint16_t* list = c.lists[w][entry % kLists];
+    const uint32_t own = lds_u16(list + r), first = lds_u16(list);
+    return own != 0xffffu ? own : first;
 }
 
 // Two blocks of codes of a weight row and their scales.
@@ -91,79 +183,224 @@ __device__ __forceinline__ Codes load_pair(const uint8_t* row, const uint8_t* sc
 }
 __device__ __forceinline__ float power_of(const Codes& c, int h) { return mx_power(h ? c.scale >> 8 : c.scale & 0xffu); }
 
-// Hidden values: a block takes 16 gates and their 16 ups of one expert, for all of its tokens, 16 at a time; its W waves
-// share out the tokens' columns in steps of 256 and join their sums through LDS, in the waves' order.
-template <int DT, int W>
-__global__ __launch_bounds__(W * 64) void hccl_moe_layer_mx_up_kernel(LayerMxArgs a, uint32_t tiles, uint32_t by_route) {
-    constexpr int TERMS = kTerms(DT), PLANES = kPlanes(DT), ES = kSize<DT>;
-    __shared__ v4f part[W][2][64];
-    __shared__ uint16_t list[HCCL_MAX_LAYER_TOKENS];
-    const uint32_t lane = threadIdx.x & 63, w = first_lane(threadIdx.x >> 6), i = lane & 15, q = lane >> 4;
-    const uint32_t slot = blockIdx.x / tiles, f0 = blockIdx.x % tiles * 16;
-    uint32_t e = slot;
-    if (by_route) {  // the block of the first route to an expert takes all of them
-        e = (uint32_t)a.index[slot] - a.first;
-        if (e >= a.held) return;
-    }
-    const uint32_t n = list_routes(a, e, list, w == 0);
-    __syncthreads();
-    if (n == 0 || (by_route && list[0] != slot)) return;
+// How rows reach the matrix instructions, 4 at a time. A lane of 16 holds 8 elements of its row, 8 times for the 64 that its
+// quarter of the wave has of a step. Row r of four is the instruction's column 4 r, and lanes 4 r to 4 r + 3 load four of the
+// 8 pieces, 64 bytes side by side, so that two loads do instead of 8 whose lanes would each be an access of its own; the pieces
+// move on to lane 4 r for their instruction. The other columns have nothing that counts.
+template <int N>
+__device__ __forceinline__ b8 move_down(const b8& v) {  // from N lanes on, of 16
+    if constexpr (N == 0) return v;
+    const v4u w = __builtin_bit_cast(v4u, v);
+    return __builtin_bit_cast(b8, v4u{dpp<0x130 - N>(w[0]), dpp<0x130 - N>(w[1]), dpp<0x130 - N>(w[2]), dpp<0x130 - N>(w[3])});
+}
+// f(which of four pieces) for each
+template <typename F>
+__device__ __forceinline__ void each_piece(F f) {
+    f(std::integral_constant<int, 0>());
+    f(std::integral_constant<int, 1>());
+    f(std::integral_constant<int, 2>());
+    f(std::integral_constant<int, 3>());
+}
 
-    const uint8_t *pw[2], *ps[2];
+// How weights do. 16 lanes hold 16 rows, so a load by each lane of its own would be 64 accesses of 16 bytes. Where rows are
+// 16-byte aligned (and their scales 4-byte), loads go to LDS directly, 8 lanes to a row's 128 bytes of a step, and
+// each lane reads its row's there: chunk c of 16 bytes of row r lies in slot c ^ (r / 2 & 7), on other banks than those of the rows
+// read with it. A step's buffer is SIDES * 16 rows of 128 bytes, and then their 8 scale bytes each (of one side twice: all lanes
+// load, as a branch would hide from the compiler how many loads there are); a wave has as many as steps on their way, of its
+// own, and needs no barrier for them.
+template <int SIDES>
+constexpr uint32_t kSlot = SIDES * 16 * 128 + 256;
+
+template <int SIDES>
+struct Source {  // where a lane's part of the loads comes from
+    const uint8_t* code[SIDES * 2];
+    const uint8_t* scale;
+};
+template <int SIDES>
+__device__ __forceinline__ void load_to_lds(const Source<SIDES>& src, uint32_t s, char* slot) {
 #pragma unroll
-    for (int y = 0; y < 2; ++y) {
-        const uint32_t f = f0 + i < a.inner ? f0 + i : a.inner - 1;
-        const uint64_t row = (uint64_t)e * 2 * a.inner + y * a.inner + f;
-        pw[y] = a.w_in + row * a.ld_in;
-        ps[y] = a.w_in_scale + row * a.ld_in_scale;
-    }
-#pragma unroll 1
-    for (uint32_t x0 = 0; x0 < n; x0 += 16) {
-        const bool on = x0 + i < n;
-        const uint32_t route = list[on ? x0 + i : x0];
-        const char* px = (const char*)a.x + (uint64_t)(route / a.top_k) * a.ldx * ES;
-        v4f acc[2] = {v4f{0, 0, 0, 0}, v4f{0, 0, 0, 0}};
-        auto step = [&](uint32_t k0, auto inside) {
-            constexpr bool INSIDE = decltype(inside)::value;
-            const uint32_t k = k0 + q * 32;
-            const Codes c[2] = {load_pair<INSIDE>(pw[0], ps[0], k, a.cols), load_pair<INSIDE>(pw[1], ps[1], k, a.cols)};
-            b8 t[8][TERMS] = {};
-            if (on) {
+    for (int n = 0; n < SIDES * 2; ++n)
+        __builtin_amdgcn_global_load_lds((const HCCL_AS1 void*)(src.code[n] + (uint64_t)s * 128), (lds_ptr)(slot + n * 1024), 16, 0, 0);
+    __builtin_amdgcn_global_load_lds((const HCCL_AS1 void*)(src.scale + (uint64_t)s * 8), (lds_ptr)(slot + SIDES * 2048), 4, 0, 0);
+}
+// (in one block with the wait, as the compiler would have a read wait for every load to LDS there is)
+__device__ __forceinline__ void read_from_lds(Codes (&c)[1], uint32_t at0, uint32_t at1, uint32_t scale) {
+    asm volatile("ds_read_b128 %0, %3\n\tds_read_b128 %1, %4\n\tds_read_u16 %2, %5\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(c[0].c[0]), "=&v"(c[0].c[1]), "=&v"(c[0].scale)
+                 : "v"(at0), "v"(at1), "v"(scale)
+                 : "memory");
+}
+__device__ __forceinline__ void read_from_lds(Codes (&c)[2], uint32_t at0, uint32_t at1, uint32_t scale) {
+    asm volatile("ds_read_b128 %0, %6\n\tds_read_b128 %1, %7\n\tds_read_b128 %3, %6 offset:2048\n\tds_read_b128 %4, %7 offset:2048\n\t"
+                 "ds_read_u16 %2, %8\n\tds_read_u16 %5, %8 offset:128\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(c[0].c[0]), "=&v"(c[0].c[1]), "=&v"(c[0].scale), "=&v"(c[1].c[0]), "=&v"(c[1].c[1]), "=&v"(c[1].scale)
+                 : "v"(at0), "v"(at1), "v"(scale)
+                 : "memory");
+}
+template <int N>
+__device__ __forceinline__ void wait_loads() {  // until at most N are on their way
+    static_assert(N < 64, "the counter");
+    __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | (N & 48) << 10);
+}
+
+// Both kernels walk along whole steps of 256 elements, kAhead of which are on their way while one is multiplied: with no branch
+// around a load, which would leave the compiler unable to tell how many are, and all of them waited for. So lanes without a
+// row read their first one, steps behind the last are the last once more, and what is left of a row behind its whole steps
+// is a second, plain pass.
+
+// Hidden values. An item is 16 gates and their 16 ups of one expert, for the rows of an entry; `shares` waves of a block
+// take one, each a part of the tokens' columns in steps of 256, and join their sums through LDS, in the waves' order. As many
+// shares as leave the waves least to do in all of their rounds.
+template <int DT, int FOURS, int AHEAD, bool ALIGNED>
+__device__ __forceinline__ void layer_up(const LayerMxArgs& a, Choices& choices, char* buffers, v4f (*part)[2][64]) {
+    constexpr int TERMS = kTerms(DT), PLANES = kPlanes(DT), ES = kSize<DT>;
+    const uint32_t lane = threadIdx.x & 63, w = first_lane(threadIdx.x >> 6), i = lane & 15, q = lane >> 4;
+    const uint32_t ldh = padded(a.inner), tiles = ldh / 16, items = first_lane(choices.number) * tiles;
+    const uint32_t steps = ((a.cols + 1) / 2 + 127) / 128, whole_steps = a.cols / 256;
+    uint32_t shares = 1;
+    {
+        uint32_t least = ~0u;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) load_terms<DT, INSIDE>(px, k * 2 + j * 8, a.cols, t[j]);
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-#pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                    const b8 v = decode8(c[y].c[j / 4][j % 4], power_of(c[y], j / 4));
-#pragma unroll
-                    for (int m = 0; m < TERMS; ++m) acc[y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, t[j][m], acc[y], 0, 0, 0);
-                }
-        };
-        const uint32_t bytes = (a.cols + 1) / 2;
-#pragma unroll 1
-        for (uint32_t k0 = w * 128; k0 < bytes; k0 += W * 128) {
-            if (k0 + 128 <= a.cols / 2) step(k0, std::true_type());
-            else step(k0, std::false_type());
+        for (uint32_t n = 1; n <= kWaves; n *= 2) {  // steps of all rounds (a step's time and a half for each round's beginning and end)
+            const uint32_t each = gridDim.x * (kWaves / n), time = (items + each - 1) / each * (2 * ((steps + n - 1) / n) + 3);
+            if (time < least) least = time, shares = n;
         }
-        if (x0) __syncthreads();  // (the sums of the tokens before have been read)
+    }
+    const uint32_t at_a_time = kWaves / shares, share = w % shares;
+    char* mine = buffers + w * (AHEAD * kSlot<2>);
+    const uint32_t at0 = lds_address(mine) + i * 128 + ((2 * q) ^ (i >> 1 & 7)) * 16, at_scale = lds_address(mine) + 4096 + i * 8 + q * 2;
+    for (uint32_t item0 = blockIdx.x * at_a_time; item0 < items; item0 += gridDim.x * at_a_time) {
+        const bool some = item0 + w / shares < items;
+        const uint32_t item = some ? item0 + w / shares : items - 1, entry = item / tiles, f0 = item % tiles * 16;
+        const uint32_t what = first_lane(lds_u32(choices.entries + entry)), e = what & 0xffffu;
+        list_entry(a, choices, w, entry, what);
+        const char* px[FOURS];
 #pragma unroll
-        for (int y = 0; y < 2; ++y) part[w][y][lane] = acc[y];
-        __syncthreads();
-        if (w == 0 && on) {
-            v4f g = part[0][0][lane], u = part[0][1][lane];
+        for (int r = 0; r < FOURS; ++r) px[r] = (const char*)a.x + (uint64_t)(route_of(choices, w, entry, r * 4 + i / 4) / a.top_k) * a.ldx * ES;
+        auto row_of = [&](int y, uint32_t f) { return (uint64_t)e * 2 * a.inner + y * a.inner + (f < a.inner ? f : a.inner - 1); };
+        const uint8_t *pw[2], *ps[2];
 #pragma unroll
-            for (int v = 1; v < W; ++v) {
-                const v4f gv = part[v][0][lane], uv = part[v][1][lane];
+        for (int y = 0; y < 2; ++y) {
+            pw[y] = a.w_in + row_of(y, f0 + i) * a.ld_in;
+            ps[y] = a.w_in_scale + row_of(y, f0 + i) * a.ld_in_scale;
+        }
+        Source<2> src;
+        if constexpr (ALIGNED) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) g[j] += gv[j], u[j] += uv[j];
+            for (int n = 0; n < 4; ++n) {
+                const uint32_t r = (n & 1) * 8 + (lane >> 3);
+                src.code[n] = a.w_in + row_of(n / 2, f0 + r) * a.ld_in + ((lane & 7) ^ (r >> 1 & 7)) * 16;
             }
-            const uint32_t f = f0 + q * 4, ldh = padded(a.inner);
+            src.scale = a.w_in_scale + row_of(lane >> 5, f0 + (lane >> 1 & 15)) * a.ld_in_scale + (lane & 1) * 4;
+        }
+        v4f acc[FOURS][2];
+#pragma unroll
+        for (int r = 0; r < FOURS; ++r) acc[r][0] = acc[r][1] = v4f{0, 0, 0, 0};
+        Codes c[ALIGNED ? 1 : AHEAD][2];
+        Raw<DT> x[AHEAD][FOURS][2];
+        auto fetch_x = [&](int u, uint32_t s, auto inside) {
+#pragma unroll
+            for (int r = 0; r < FOURS; ++r)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) load_raw<DT, decltype(inside)::value>(px[r], s * 256 + q * 64 + h * 32 + (i & 3) * 8, a.cols, x[u][r][h]);
+        };
+        auto fetch_codes = [&](int u, uint32_t s, auto inside) {
+#pragma unroll
+            for (int y = 0; y < 2; ++y) c[u][y] = load_pair<decltype(inside)::value>(pw[y], ps[y], s * 128 + q * 32, a.cols);
+        };
+        auto fetch = [&](int u, uint32_t s) {
+            if constexpr (ALIGNED) load_to_lds<2>(src, s, mine + u * kSlot<2>);
+            else fetch_codes(u, s, std::true_type());
+            fetch_x(u, s, std::true_type());
+            asm volatile("" ::: "memory");  // (steps' loads are made in the steps' order, which the waits count on)
+        };
+        auto multiply = [&](int u, const Codes (&codes)[2]) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                b8 terms[FOURS][TERMS];
+#pragma unroll
+                for (int r = 0; r < FOURS; ++r) terms_of<DT>(x[u][r][h], terms[r]);
+                each_piece([&](auto j) {
+                    constexpr int J = decltype(j)::value;
+                    const b8 v[2] = {decode8(codes[0].c[h][J], power_of(codes[0], h)), decode8(codes[1].c[h][J], power_of(codes[1], h))};
+#pragma unroll
+                    for (int r = 0; r < FOURS; ++r)
+#pragma unroll
+                        for (int m = 0; m < TERMS; ++m) {
+                            const b8 piece = move_down<J>(terms[r][m]);
+#pragma unroll
+                            for (int y = 0; y < 2; ++y) acc[r][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[y], piece, acc[r][y], 0, 0, 0);
+                        }
+                });
+            }
+        };
+        if (some && share < whole_steps) {
+            const uint32_t n = (whole_steps - share + shares - 1) / shares;  // this wave's steps
+            auto step = [&](uint32_t m) { return share + (m < n ? m : n - 1) * shares; };
+            auto take = [&](int u) {
+                if constexpr (ALIGNED) {
+                    wait_loads<(AHEAD - 1) * (5 + FOURS * ES)>();
+                    const uint32_t at = u * kSlot<2>;
+                    read_from_lds(c[0], at0 + at, (at0 ^ 16) + at, at_scale + at);
+                    // (used from here on, and not sooner, which would be another wait)
+#pragma unroll
+                    for (int r = 0; r < FOURS; ++r)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+#pragma unroll
+                            for (int n = 0; n < ES / 2; ++n) asm volatile("" : "+v"(x[u][r][h].v[n]));
+                    multiply(u, c[0]);
+                } else {
+                    multiply(u, c[u]);
+                }
+            };
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) fetch(u, step(u));
+            uint32_t m = 0;
+#pragma unroll 1
+            for (; m + AHEAD <= n; m += AHEAD) {
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u) {
+                    take(u);
+                    fetch(u, step(m + u + AHEAD));
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < AHEAD - 1; ++u) {
+                if (m + u >= n) break;
+                take(u);
+            }
+            if (ALIGNED) wait_loads<0>();  // (those behind the last step)
+        }
+        if (some && whole_steps < steps && whole_steps % shares == share) {
+            fetch_codes(0, whole_steps, std::false_type());
+            fetch_x(0, whole_steps, std::false_type());
+            multiply(0, c[0]);
+        }
+#pragma unroll
+        for (int r = 0; r < FOURS; ++r) {
+            if (shares > 1) {
+                if (r) __syncthreads();  // (the sums of the four rows before have been read)
+#pragma unroll
+                for (int y = 0; y < 2; ++y) part[w][y][lane] = acc[r][y];
+                __syncthreads();
+                if (share == 0) {
+                    for (uint32_t v = 1; v < shares; ++v)
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) {
+                            const v4f more = part[w + v][y][lane];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) acc[r][y][j] += more[j];
+                        }
+                }
+            }
+            const uint32_t route = lds_u16(choices.lists[w][entry % kLists] + r * 4 + i / 4);
+            if (!some || share != 0 || i % 4 || route == 0xffffu) continue;
+            const uint32_t f = f0 + q * 4;
             uint16_t* to = a.hidden + (uint64_t)route * PLANES * ldh + f;
             float h[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) h[j] = f + j < a.inner ? mx_gate(g[j], u[j]) : 0.0f;
+            for (int j = 0; j < 4; ++j) h[j] = f + j < a.inner ? mx_gate(acc[r][0][j], acc[r][1][j]) : 0.0f;
 #pragma unroll
             for (int p = 0; p < PLANES; ++p) {
                 uint32_t b[4];
@@ -176,116 +413,220 @@ __global__ __launch_bounds__(W * 64) void hccl_moe_layer_mx_up_kernel(LayerMxArg
                 *gptr<typename Loose<2>::x2>(to + (uint64_t)p * ldh) = typename Loose<2>::x2{b[0] | b[1] << 16, b[2] | b[3] << 16};
             }
         }
+        if (shares > 1) __syncthreads();
     }
 }
 
-// Results: a block takes 16 columns of all tokens. Its W waves share out the experts that have a token, and where those are
-// fewer the hidden values of each, in steps of 256; a wave adds its weighted results up in its own part of LDS, and
-// these are added up at the end in the waves' order.
-template <int DT, int W>
-__global__ __launch_bounds__(W * 64) void hccl_moe_layer_mx_down_kernel(LayerMxArgs a) {
-    constexpr int PLANES = kPlanes(DT), ES = kSize<DT>;
-    __shared__ float sums[W][HCCL_MAX_LAYER_TOKENS][16];
-    __shared__ uint8_t used[HCCL_MAX_EXPERTS];
-    __shared__ uint16_t experts[HCCL_MAX_EXPERTS], lists[W][HCCL_MAX_LAYER_TOKENS];
-    __shared__ uint32_t number;
+// Steps on their way: as many as registers and LDS hold.
+constexpr int up_ahead(int dt, int fours) { return fours < 4 ? 3 : dt == hcclFp32 ? 1 : 2; }
+constexpr int down_ahead(int dt, int fours) { return fours == 1 ? 4 : fours == 2 ? dt == hcclFp32 ? 2 : 3 : dt == hcclFp32 ? 1 : 2; }
+
+template <int DT, bool ALIGNED>
+__global__ __launch_bounds__(kWaves * 64, 2) void hccl_moe_layer_mx_up_kernel(LayerMxArgs a) {
+    __shared__ Choices choices;
+    __shared__ v4f part[kWaves][2][64];
+    __shared__ __attribute__((aligned(256))) char buffers[ALIGNED ? kWaves * 3 * kSlot<2> : 16];
+    find_choices(a, choices);
+    if (choices.number == 0) return;
+    const uint32_t rows = first_lane(choices.rows);
+    if (rows == 4) layer_up<DT, 1, up_ahead(DT, 1), ALIGNED>(a, choices, buffers, part);
+    else if (rows == 8) layer_up<DT, 2, up_ahead(DT, 2), ALIGNED>(a, choices, buffers, part);
+    else layer_up<DT, 4, up_ahead(DT, 4), ALIGNED>(a, choices, buffers, part);
+}
+
+// Results. A block takes 16 columns of all tokens. The whole steps of all entries, one entry behind the other, are shared out
+// evenly among its waves, and so is what is left of each; a wave adds its weighted results up in its own part of LDS, and these
+// are added up at the end in the waves' order.
+template <int DT, int FOURS, int AHEAD, bool ALIGNED>
+__device__ __forceinline__ void layer_down(const LayerMxArgs& a, Choices& choices, char* buffers, float (*sums)[HCCL_MAX_LAYER_TOKENS][16]) {
+    constexpr int PLANES = kPlanes(DT);
     const uint32_t lane = threadIdx.x & 63, w = first_lane(threadIdx.x >> 6), i = lane & 15, q = lane >> 4;
-    const uint32_t n0 = blockIdx.x * 16, routes = a.tokens * a.top_k;
-    for (uint32_t e = threadIdx.x; e < a.held; e += W * 64) used[e] = 0;
+    const uint32_t n0 = blockIdx.x * 16;
+    const uint32_t ldh = padded(a.inner), whole_steps = a.inner / 256, entries = first_lane(choices.number);
+    char* mine = buffers + w * (AHEAD * kSlot<1>);
+    const uint32_t at0 = lds_address(mine) + i * 128 + ((2 * q) ^ (i >> 1 & 7)) * 16, at_scale = lds_address(mine) + 2048 + i * 8 + q * 2;
+    Codes c[ALIGNED ? 1 : AHEAD][1];
+    b8 hidden[AHEAD][FOURS][2][PLANES];
+    const uint8_t *pw, *ps;
+    Source<1> src;
+    const uint16_t* ph[FOURS];
+    auto look = [&](uint32_t entry) {  // turns the pointers to an entry
+        const uint32_t what = first_lane(lds_u32(choices.entries + entry));
+        const uint64_t first = (uint64_t)(what & 0xffffu) * a.cols;
+        auto row_of = [&](uint32_t r) { return first + (n0 + r < a.cols ? n0 + r : a.cols - 1); };
+        pw = a.w_out + row_of(i) * a.ld_out;
+        ps = a.w_out_scale + row_of(i) * a.ld_out_scale;
+        if constexpr (ALIGNED) {
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                const uint32_t r = n * 8 + (lane >> 3);
+                src.code[n] = a.w_out + row_of(r) * a.ld_out + ((lane & 7) ^ (r >> 1 & 7)) * 16;
+            }
+            src.scale = a.w_out_scale + row_of(lane >> 1 & 15) * a.ld_out_scale + (lane & 1) * 4;
+        }
+        list_entry(a, choices, w, entry, what);
+#pragma unroll
+        for (int r = 0; r < FOURS; ++r) ph[r] = a.hidden + (uint64_t)route_of(choices, w, entry, r * 4 + i / 4) * PLANES * ldh;
+    };
+    auto fetch_h = [&](int u, uint32_t s, auto inside) {
+#pragma unroll
+        for (int r = 0; r < FOURS; ++r)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int p = 0; p < PLANES; ++p) {
+                    const uint32_t k = s * 256 + q * 64 + h * 32 + (i & 3) * 8;
+                    hidden[u][r][h][p] = decltype(inside)::value || k < ldh ? __builtin_bit_cast(b8, load16<2>(ph[r] + (uint64_t)p * ldh + k)) : b8{};
+                }
+    };
+    auto fetch_codes = [&](int u, uint32_t s, auto inside) { c[u][0] = load_pair<decltype(inside)::value>(pw, ps, s * 128 + q * 32, a.inner); };
+    auto fetch = [&](int u, uint32_t s) {
+        if constexpr (ALIGNED) load_to_lds<1>(src, s, mine + u * kSlot<1>);
+        else fetch_codes(u, s, std::true_type());
+        fetch_h(u, s, std::true_type());
+        asm volatile("" ::: "memory");  // (steps' loads are made in the steps' order, which the waits count on)
+    };
+    v4f acc[FOURS];
+    auto clear = [&] {
+#pragma unroll
+        for (int r = 0; r < FOURS; ++r) acc[r] = v4f{0, 0, 0, 0};
+    };
+    auto multiply = [&](int u, const Codes& codes) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            each_piece([&](auto j) {
+                constexpr int J = decltype(j)::value;
+                const b8 v = decode8(codes.c[h][J], power_of(codes, h));
+#pragma unroll
+                for (int r = 0; r < FOURS; ++r)
+#pragma unroll
+                    for (int p = 0; p < PLANES; ++p) acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, move_down<J>(hidden[u][r][h][p]), acc[r], 0, 0, 0);
+            });
+    };
+    auto add = [&](uint32_t entry) {
+#pragma unroll
+        for (int r = 0; r < FOURS; ++r) {
+            const uint32_t route = lds_u16(choices.lists[w][entry % kLists] + r * 4 + i / 4);
+            if (route != 0xffffu && i % 4 == 0) {
+                const float weight = __uint_as_float(lds_u32(choices.weight + route));
+                lds_add4(&sums[w][route / a.top_k][q * 4], weight * acc[r][0], weight * acc[r][1], weight * acc[r][2], weight * acc[r][3]);
+            }
+        }
+        clear();
+    };
+    clear();
+    const uint64_t all = (uint64_t)entries * whole_steps;
+    uint32_t g = (uint32_t)(all * w / kWaves);
+    const uint32_t end = (uint32_t)(all * (w + 1) / kWaves);
+    if (g < end) {
+        uint32_t entry = g / whole_steps, s = g % whole_steps;  // that are multiplied
+        uint32_t next = entry, next_s = s, left = end - g;      // that are read
+        look(next);
+        auto fetch_next = [&](int u) {
+            fetch(u, next_s);
+            if (left > 1) {
+                --left;
+                if (++next_s == whole_steps) next_s = 0, look(++next);
+            }
+        };
+        auto take = [&](int u) {
+            if constexpr (ALIGNED) {
+                wait_loads<(AHEAD - 1) * (3 + FOURS * 2 * PLANES)>();
+                const uint32_t at = u * kSlot<1>;
+                read_from_lds(c[0], at0 + at, (at0 ^ 16) + at, at_scale + at);
+                // (used from here on, and not sooner, which would be another wait)
+#pragma unroll
+                for (int r = 0; r < FOURS; ++r)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int p = 0; p < PLANES; ++p) asm volatile("" : "+v"(hidden[u][r][h][p]));
+                multiply(u, c[0][0]);
+            } else {
+                multiply(u, c[u][0]);
+            }
+            ++g;
+            if (++s == whole_steps || g == end) {
+                add(entry);
+                s = 0, ++entry;
+            }
+        };
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) fetch_next(u);
+#pragma unroll 1
+        while (g + AHEAD <= end) {
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                take(u);
+                fetch_next(u);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD - 1; ++u) {
+            if (g >= end) break;
+            take(u);
+        }
+        if (ALIGNED) wait_loads<0>();  // (those behind the last step)
+    }
+    if (whole_steps * 256 < a.inner) {
+        for (uint32_t entry = w; entry < entries; entry += kWaves) {
+            look(entry);
+            fetch_codes(0, whole_steps, std::false_type());
+            fetch_h(0, whole_steps, std::false_type());
+            multiply(0, c[0][0]);
+            add(entry);
+        }
+    }
+}
+
+template <int DT, bool ALIGNED>
+__global__ __launch_bounds__(kWaves * 64, 2) void hccl_moe_layer_mx_down_kernel(LayerMxArgs a) {
+    constexpr int ES = kSize<DT>;
+    __shared__ Choices choices;
+    __shared__ float sums[kWaves][HCCL_MAX_LAYER_TOKENS][16];
+    __shared__ __attribute__((aligned(256))) char buffers[ALIGNED ? kWaves * 4 * kSlot<1> : 16];
+    const uint32_t lane = threadIdx.x & 63, w = first_lane(threadIdx.x >> 6), n0 = blockIdx.x * 16;
     for (uint32_t r = lane; r < a.tokens * 16; r += 64) sums[w][r / 16][r % 16] = 0.0f;
+    find_choices(a, choices);
+    const uint32_t rows = first_lane(choices.rows);
+    if (rows == 4) layer_down<DT, 1, down_ahead(DT, 1), ALIGNED>(a, choices, buffers, sums);
+    else if (rows == 8) layer_down<DT, 2, down_ahead(DT, 2), ALIGNED>(a, choices, buffers, sums);
+    else layer_down<DT, 4, down_ahead(DT, 4), ALIGNED>(a, choices, buffers, sums);
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // (LDS alone: the compiler does not know of the sums' additions)
     __syncthreads();
-    for (uint32_t r = threadIdx.x; r < routes; r += W * 64) {
-        const uint32_t e = (uint32_t)a.index[r] - a.first;
-        if (e < a.held) used[e] = 1;
-    }
-    __syncthreads();
-    if (w == 0) {
-        uint32_t all = 0;
-        for (uint32_t e0 = 0; e0 < a.held; e0 += 64) {
-            const bool some = e0 + lane < a.held && used[e0 + lane];
-            const uint64_t mask = __ballot(some);
-            if (some) experts[all + (uint32_t)__popcll(mask & ((1ull << lane) - 1))] = (uint16_t)(e0 + lane);
-            all += (uint32_t)__popcll(mask);
-        }
-        number = all;
-    }
-    __syncthreads();
-    const uint32_t some = first_lane(number), ldh = padded(a.inner), steps = (ldh + 255) / 256;
-    uint32_t shares = some && some < W ? W / some : 1;  // of an expert's hidden values
-    shares = shares < steps ? shares : steps;
-    for (uint32_t unit = w; unit < some * shares; unit += W) {
-        const uint32_t e = first_lane(experts[unit / shares]), share = unit % shares;
-        const uint32_t n = list_routes(a, e, lists[w], true);
-        const uint32_t col = n0 + i < a.cols ? n0 + i : a.cols - 1;
-        const uint8_t* pw = a.w_out + ((uint64_t)e * a.cols + col) * a.ld_out;
-        const uint8_t* ps = a.w_out_scale + ((uint64_t)e * a.cols + col) * a.ld_out_scale;
-#pragma unroll 1
-        for (uint32_t x0 = 0; x0 < n; x0 += 16) {
-            const bool on = x0 + i < n;
-            const uint32_t route = lists[w][on ? x0 + i : x0];
-            const uint16_t* ph = a.hidden + (uint64_t)route * PLANES * ldh;
-            v4f acc = v4f{0, 0, 0, 0};
-            auto step = [&](uint32_t k0, auto inside) {
-                constexpr bool INSIDE = decltype(inside)::value;
-                const uint32_t k = k0 + q * 32;
-                const Codes c = load_pair<INSIDE>(pw, ps, k, a.inner);
-                b8 t[8][PLANES] = {};
-                if (on) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-#pragma unroll
-                        for (int p = 0; p < PLANES; ++p)
-                            if (INSIDE || k * 2 + j * 8 < ldh) t[j][p] = __builtin_bit_cast(b8, load16<2>(ph + (uint64_t)p * ldh + k * 2 + j * 8));
-                }
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const b8 v = decode8(c.c[j / 4][j % 4], power_of(c, j / 4));
-#pragma unroll
-                    for (int p = 0; p < PLANES; ++p) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, t[j][p], acc, 0, 0, 0);
-                }
-            };
-            const uint32_t bytes = (a.inner + 1) / 2;
-#pragma unroll 1
-            for (uint32_t k0 = share * 128; k0 < bytes; k0 += shares * 128) {
-                if (k0 + 128 <= a.inner / 2) step(k0, std::true_type());
-                else step(k0, std::false_type());
-            }
-            if (on) {
-                const float weight = a.weight[route];
-                float* to = &sums[w][route / a.top_k][q * 4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) to[j] += weight * acc[j];
-            }
-        }
-    }
-    __syncthreads();
-    for (uint32_t r = threadIdx.x; r < a.tokens * 16; r += W * 64) {
+    for (uint32_t r = threadIdx.x; r < a.tokens * 16; r += kWaves * 64) {
         const uint32_t t = r / 16, n = n0 + r % 16;
         if (n >= a.cols) continue;
         float y = sums[0][t][r % 16];
 #pragma unroll
-        for (int v = 1; v < W; ++v) y += sums[v][t][r % 16];
+        for (int v = 1; v < kWaves; ++v) y += sums[v][t][r % 16];
         store1<ES>((char*)a.out + (t * a.ldo + n) * ES, narrow1<DT>(y));
     }
 }
 
-constexpr int kUpWaves = 4, kDownWaves = 16;
+bool aligned(const uint8_t* codes, uint64_t ld, const uint8_t* scale, uint64_t ld_scale) {
+    return ((uintptr_t)codes | ld) % 16 == 0 && ((uintptr_t)scale | ld_scale) % 4 == 0;
+}
 
 template <int DT>
-hipError_t layer_type(const LayerMxArgs& a, hipStream_t s) {
-    const uint32_t routes = a.tokens * a.top_k, tiles = ((a.inner + 31) / 32 * 32) / 16;
-    const bool by_route = routes <= a.held;
-    const uint64_t up = (uint64_t)(by_route ? routes : a.held) * tiles, down = ((uint64_t)a.cols + 15) / 16;
-    if (up * kUpWaves * 64 > 0xffffffffull || down * kDownWaves * 64 > 0xffffffffull) return hipErrorInvalidConfiguration;
-    if (up) hipLaunchKernelGGL((hccl_moe_layer_mx_up_kernel<DT, kUpWaves>), dim3((uint32_t)up), dim3(kUpWaves * 64), 0, s, a, tiles, by_route ? 1u : 0u);
-    hipLaunchKernelGGL((hccl_moe_layer_mx_down_kernel<DT, kDownWaves>), dim3((uint32_t)down), dim3(kDownWaves * 64), 0, s, a);
+hipError_t layer_type(const LayerMxArgs& a, int cus, hipStream_t s) {
+    const uint64_t routes = a.tokens * a.top_k, items = routes * ((a.inner + 31) / 32 * 2);  // at most
+    const uint64_t down = ((uint64_t)a.cols + 15) / 16;
+    if (down * kWaves * 64 > 0xffffffffull || items > 0x7fffffffull) return hipErrorInvalidConfiguration;
+    const dim3 block(kWaves * 64), up_grid((uint32_t)(items < (uint64_t)cus ? items : (uint64_t)cus)), down_grid((uint32_t)down);
+    if (items) {
+        if (aligned(a.w_in, a.ld_in, a.w_in_scale, a.ld_in_scale)) hipLaunchKernelGGL((hccl_moe_layer_mx_up_kernel<DT, true>), up_grid, block, 0, s, a);
+        else hipLaunchKernelGGL((hccl_moe_layer_mx_up_kernel<DT, false>), up_grid, block, 0, s, a);
+    }
+    if (aligned(a.w_out, a.ld_out, a.w_out_scale, a.ld_out_scale)) hipLaunchKernelGGL((hccl_moe_layer_mx_down_kernel<DT, true>), down_grid, block, 0, s, a);
+    else hipLaunchKernelGGL((hccl_moe_layer_mx_down_kernel<DT, false>), down_grid, block, 0, s, a);
     return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_layer_mx(const LayerMxArgs& a, hcclDataType_t dt, hipStream_t s) {
-    return dt == hcclBf16 ? layer_type<hcclBf16>(a, s) : dt == hcclFp16 ? layer_type<hcclFp16>(a, s) : layer_type<hcclFp32>(a, s);
+hipError_t launch_layer_mx(const LayerMxArgs& a, hcclDataType_t dt, int cus, hipStream_t s) {
+    return dt == hcclBf16 ? layer_type<hcclBf16>(a, cus, s) : dt == hcclFp16 ? layer_type<hcclFp16>(a, cus, s) : layer_type<hcclFp32>(a, cus, s);
 }
 
 }  // namespace hccl

@@ -74,7 +74,8 @@ class Case:
 @pytest.mark.parametrize("T,E,K,C,F", [
     (1, 1, 1, 1, 1), (1, 8, 2, 32, 16), (1, 64, 4, 512, 256), (2, 4, 4, 33, 17), (3, 60, 2, 100, 40), (5, 60, 6, 1003, 117), (8, 128, 8, 256, 96), (16, 8, 2, 130, 64),
     (17, 8, 2, 255, 31), (32, 16, 4, 64, 160), (33, 2, 2, 96, 48), (64, 4, 1, 80, 24), (64, 1, 1, 300, 33), (64, 32, 8, 48, 80), (7, 1024, 32, 40, 20),
-    (64, 1024, 32, 17, 9), (4, 3, 3, 2050, 513), (2, 5, 1, 7, 1100)])
+    (64, 1024, 32, 17, 9), (4, 3, 3, 2050, 513), (2, 5, 1, 7, 1100), (9, 40, 6, 304, 288), (11, 30, 4, 768, 256), (30, 12, 3, 256, 320), (5, 16, 3, 1024, 1280),
+    (40, 6, 3, 544, 512), (1, 200, 16, 3000, 270)])
 def test_layer(comm, T, E, K, C, F, dt):
     rng = np.random.default_rng(T + E + C)
     Case(rng, T, E, K, C, F, dt, renormalize=True).run(comm).check()
