@@ -41,6 +41,63 @@ __device__ __forceinline__ void load8(const char* row, uint64_t e, uint64_t cols
     }
 }
 
+// The scale byte of the lane's quad, and the codes of its 8 values.
+template <int DT, bool GATED>
+__device__ __forceinline__ void encode(float (&x)[8], const float (&up)[8], uint32_t& b, uint32_t& codes) {
+    if constexpr (GATED) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = mx_gate(x[i], up[i]);
+    }
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+    top = max(top, dpp<kQuadSwap>(top));
+    top = max(top, dpp<kQuadHalf>(top));
+    b = mx_scale(top);
+    codes = b == 255u ? 0u : mx_encode(x, mx_power(b));
+}
+
+// Rows that are whole units: a wave is at one row, whose places are on their way with it. Its codes go through LDS, so that a
+// lane stores 16 bytes of them and not 4, and its scales are one store. (8 192 x 4 096 bf16 to 4 rows each: by 4 bytes, with the
+// places looked up before each store, 43 us.)
+constexpr uint32_t kWide = 4;  // units
+template <int DT, bool GATED>
+__global__ __launch_bounds__(kThreads) void hccl_moe_quantize_mx_wide_kernel(QuantizeMxArgs a) {
+    constexpr int ES = kSize<DT>;
+    __shared__ uint32_t all_codes[kWaves][kWide * 64];
+    __shared__ uint8_t all_scales[kWaves][kWide * 16];
+    const uint32_t lane = threadIdx.x & 63, w = first_lane(threadIdx.x >> 6), pieces = a.blocks / (kWide * 16);
+    const uint32_t id = blockIdx.x * kWaves + w, t = id / pieces, b0 = id % pieces * (kWide * 16);
+    const uint64_t rows = a.limit && *a.limit < (int64_t)a.rows ? (*a.limit < 0 ? 0 : (uint64_t)*a.limit) : a.rows;
+    if (t >= rows) return;
+    const uint32_t mine = !a.row ? t : lane < a.top_k ? (uint32_t)a.row[(uint64_t)t * a.top_k + lane] : ~0u;
+    const char* src = (const char*)a.x + t * a.ldx * ES;
+    float x[kWide][8], up[kWide][8];
+#pragma unroll
+    for (uint32_t u = 0; u < kWide; ++u) {
+        const uint64_t e = (b0 + u * 16) * kMxBlock + lane * 8;
+        load8<DT>(src, e, a.cols, x[u]);
+        if constexpr (GATED) load8<DT>(src + a.cols * ES, e, a.cols, up[u]);
+    }
+#pragma unroll
+    for (uint32_t u = 0; u < kWide; ++u) {
+        uint32_t b, codes;
+        encode<DT, GATED>(x[u], up[u], b, codes);
+        all_codes[w][u * 64 + lane] = codes;
+        if (lane % 4 == 0) all_scales[w][u * 16 + lane / 4] = (uint8_t)b;
+    }
+    // (a wave's own part of LDS, which it reads in the order of its writes)
+    const v4u codes = *(const v4u*)&all_codes[w][lane * 4];
+    const uint32_t scales = *(const uint32_t*)&all_scales[w][lane % 16 * 4];
+    const uint32_t copies = a.row ? a.top_k : 1u;
+    for (uint32_t k = 0; k < copies; ++k) {
+        const uint32_t r = a.row ? at_lane(mine, k) : t;
+        if (r >= a.capacity) continue;
+        store16<1>(a.codes + r * a.ldq + b0 * 16 + lane * 16, codes);
+        if (lane < 16) *gptr<typename Loose<1>::x1>(a.scale + r * a.lds + b0 + lane * 4) = scales;
+    }
+}
+
 template <int DT, bool GATED>
 __global__ __launch_bounds__(kThreads) void hccl_moe_quantize_mx_kernel(QuantizeMxArgs a) {
     constexpr int ES = kSize<DT>;
@@ -48,6 +105,7 @@ __global__ __launch_bounds__(kThreads) void hccl_moe_quantize_mx_kernel(Quantize
     const uint64_t rows = a.limit && *a.limit < (int64_t)a.rows ? (*a.limit < 0 ? 0 : (uint64_t)*a.limit) : a.rows;
     float x[kUnits][8], up[kUnits][8];
     Place p[kUnits];
+    uint32_t first[kUnits];  // places, on their way with the rows: the first, and others as they are needed
 #pragma unroll
     for (uint32_t u = 0; u < kUnits; ++u) {
         p[u] = place(unit0 + u, a.blocks);
@@ -56,24 +114,17 @@ __global__ __launch_bounds__(kThreads) void hccl_moe_quantize_mx_kernel(Quantize
         if (p[u].t < rows) {
             load8<DT>(src, e, a.cols, x[u]);
             if constexpr (GATED) load8<DT>(src + a.cols * ES, e, a.cols, up[u]);
+            first[u] = a.row ? (uint32_t)a.row[(uint64_t)p[u].t * a.top_k] : p[u].t;
         }
     }
 #pragma unroll
     for (uint32_t u = 0; u < kUnits; ++u) {
         if (p[u].t >= rows) continue;  // (a quad's lanes are of one row)
-        if constexpr (GATED) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[u][i] = mx_gate(x[u][i], up[u][i]);
-        }
-        uint32_t top = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[u][i]) & 0x7fffffffu);
-        top = max(top, dpp<kQuadSwap>(top));
-        top = max(top, dpp<kQuadHalf>(top));
-        const uint32_t b = mx_scale(top);
-        const uint32_t codes = b == 255u ? 0u : mx_encode(x[u], mx_power(b));
+        uint32_t b, codes;
+        encode<DT, GATED>(x[u], up[u], b, codes);
         const uint32_t e = p[u].b * kMxBlock + lane % 4 * 8, left = (uint32_t)a.cols > e ? (uint32_t)a.cols - e : 0;
         auto put = [&](uint32_t r) {
+            if (r >= a.capacity) return;
             uint8_t* dst = a.codes + r * a.ldq + e / 2;
             if (left >= 7) {
                 *gptr<typename Loose<1>::x1>(dst) = codes;
@@ -84,15 +135,11 @@ __global__ __launch_bounds__(kThreads) void hccl_moe_quantize_mx_kernel(Quantize
             }
             if (lane % 4 == 0) *gptr<uint8_t>(a.scale + r * a.lds + p[u].b) = (uint8_t)b;
         };
-        if (!a.row) {
-            put(p[u].t);
-            continue;
-        }
+        put(first[u]);
+        if (!a.row) continue;
         const int32_t* row = a.row + (uint64_t)p[u].t * a.top_k;
-        for (uint32_t k = 0; k < a.top_k; ++k) {
-            const uint32_t r = (uint32_t)row[k];
-            if (r < a.capacity) put(r);
-        }
+#pragma unroll 4
+        for (uint32_t k = 1; k < a.top_k; ++k) put((uint32_t)row[k]);
     }
 }
 
@@ -156,6 +203,15 @@ hipError_t by_type(hcclDataType_t dt, F f) {
 hipError_t launch_quantize_mx(const QuantizeMxArgs& a, hcclDataType_t dt, bool gated, hipStream_t s) {
     const uint32_t grid = grid_of(a.rows, a.blocks);
     if (!grid) return hipErrorInvalidConfiguration;
+    if (a.cols % (kWide * 16 * kMxBlock) == 0) {
+        const uint64_t waves = a.rows * (a.blocks / (kWide * 16));
+        const dim3 wide((uint32_t)((waves + kWaves - 1) / kWaves));
+        return by_type(dt, [&](auto type) {
+            constexpr int DT = decltype(type)::value;
+            if (gated) hipLaunchKernelGGL((hccl_moe_quantize_mx_wide_kernel<DT, true>), wide, dim3(kThreads), 0, s, a);
+            else hipLaunchKernelGGL((hccl_moe_quantize_mx_wide_kernel<DT, false>), wide, dim3(kThreads), 0, s, a);
+        });
+    }
     return by_type(dt, [&](auto type) {
         constexpr int DT = decltype(type)::value;
         if (gated) hipLaunchKernelGGL((hccl_moe_quantize_mx_kernel<DT, true>), dim3(grid), dim3(kThreads), 0, s, a);
