@@ -183,15 +183,28 @@ __device__ __forceinline__ Codes load_pair(const uint8_t* row, const uint8_t* sc
 }
 __device__ __forceinline__ float power_of(const Codes& c, int h) { return mx_power(h ? c.scale >> 8 : c.scale & 0xffu); }
 
-// How rows reach the matrix instructions, 4 at a time. A lane of 16 holds 8 elements of its row, 8 times for the 64 that its
-// quarter of the wave has of a step. Row r of four is the instruction's column 4 r, and lanes 4 r to 4 r + 3 load four of the
-// 8 pieces, 64 bytes side by side, so that two loads do instead of 8 whose lanes would each be an access of its own; the pieces
-// move on to lane 4 r for their instruction. The other columns have nothing that counts.
-template <int N>
-__device__ __forceinline__ b8 move_down(const b8& v) {  // from N lanes on, of 16
-    if constexpr (N == 0) return v;
-    const v4u w = __builtin_bit_cast(v4u, v);
-    return __builtin_bit_cast(b8, v4u{dpp<0x130 - N>(w[0]), dpp<0x130 - N>(w[1]), dpp<0x130 - N>(w[2]), dpp<0x130 - N>(w[3])});
+// How rows reach the matrix instructions. A lane of 16 holds 8 elements of its row, 8 times for the 64 that its quarter of the
+// wave has of a step. Lanes 4 r to 4 r + 3 load four of the 8 pieces of row r of every four rows, 64 bytes side by side, so
+// that two loads do for them instead of 8 whose lanes would each be an access of its own. For an instruction the piece moves from
+// its lane to lane 4 r + g, g the four that the row is one of, so that up to 16 rows are 16 columns of one instruction. Columns
+// of rows that are not there have nothing that counts.
+constexpr uint32_t row_of_lane(uint32_t i) { return i % 4 * 4 + i / 4; }
+template <int J, int FOURS, int N>
+__device__ __forceinline__ b8 piece(const b8 (&t)[FOURS][N], int n, uint32_t lane) {
+    constexpr int kAll = J * 0x55;  // the quad's lane J to all of it
+    v4u v = __builtin_bit_cast(v4u, t[0][n]);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = dpp<kAll>(v[k]);
+#pragma unroll
+    for (int g = 1; g < FOURS; ++g) {
+        const v4u u = __builtin_bit_cast(v4u, t[g][n]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t moved = dpp<kAll>(u[k]);
+            v[k] = (lane & 3) == (uint32_t)g ? moved : v[k];
+        }
+    }
+    return __builtin_bit_cast(b8, v);
 }
 // f(which of four pieces) for each
 template <typename F>
@@ -293,9 +306,7 @@ __device__ __forceinline__ void layer_up(const LayerMxArgs& a, Choices& choices,
             }
             src.scale = a.w_in_scale + row_of(lane >> 5, f0 + (lane >> 1 & 15)) * a.ld_in_scale + (lane & 1) * 4;
         }
-        v4f acc[FOURS][2];
-#pragma unroll
-        for (int r = 0; r < FOURS; ++r) acc[r][0] = acc[r][1] = v4f{0, 0, 0, 0};
+        v4f acc[2] = {v4f{0, 0, 0, 0}, v4f{0, 0, 0, 0}};
         Codes c[ALIGNED ? 1 : AHEAD][2];
         Raw<DT> x[AHEAD][FOURS][2];
         auto fetch_x = [&](int u, uint32_t s, auto inside) {
@@ -324,13 +335,11 @@ __device__ __forceinline__ void layer_up(const LayerMxArgs& a, Choices& choices,
                     constexpr int J = decltype(j)::value;
                     const b8 v[2] = {decode8(codes[0].c[h][J], power_of(codes[0], h)), decode8(codes[1].c[h][J], power_of(codes[1], h))};
 #pragma unroll
-                    for (int r = 0; r < FOURS; ++r)
+                    for (int m = 0; m < TERMS; ++m) {
+                        const b8 rows = piece<J>(terms, m, lane);
 #pragma unroll
-                        for (int m = 0; m < TERMS; ++m) {
-                            const b8 piece = move_down<J>(terms[r][m]);
-#pragma unroll
-                            for (int y = 0; y < 2; ++y) acc[r][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[y], piece, acc[r][y], 0, 0, 0);
-                        }
+                        for (int y = 0; y < 2; ++y) acc[y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[y], rows, acc[y], 0, 0, 0);
+                    }
                 });
             }
         };
@@ -377,43 +386,39 @@ __device__ __forceinline__ void layer_up(const LayerMxArgs& a, Choices& choices,
             fetch_x(0, whole_steps, std::false_type());
             multiply(0, c[0]);
         }
+        if (shares > 1) {
 #pragma unroll
-        for (int r = 0; r < FOURS; ++r) {
-            if (shares > 1) {
-                if (r) __syncthreads();  // (the sums of the four rows before have been read)
+            for (int y = 0; y < 2; ++y) part[w][y][lane] = acc[y];
+            __syncthreads();
+            if (share == 0) {
+                for (uint32_t v = 1; v < shares; ++v)
 #pragma unroll
-                for (int y = 0; y < 2; ++y) part[w][y][lane] = acc[r][y];
-                __syncthreads();
-                if (share == 0) {
-                    for (uint32_t v = 1; v < shares; ++v)
+                    for (int y = 0; y < 2; ++y) {
+                        const v4f more = part[w + v][y][lane];
 #pragma unroll
-                        for (int y = 0; y < 2; ++y) {
-                            const v4f more = part[w + v][y][lane];
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) acc[r][y][j] += more[j];
-                        }
-                }
+                        for (int j = 0; j < 4; ++j) acc[y][j] += more[j];
+                    }
             }
-            const uint32_t route = lds_u16(choices.lists[w][entry % kLists] + r * 4 + i / 4);
-            if (!some || share != 0 || i % 4 || route == 0xffffu) continue;
-            const uint32_t f = f0 + q * 4;
-            uint16_t* to = a.hidden + (uint64_t)route * PLANES * ldh + f;
-            float h[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) h[j] = f + j < a.inner ? mx_gate(acc[r][0][j], acc[r][1][j]) : 0.0f;
-#pragma unroll
-            for (int p = 0; p < PLANES; ++p) {
-                uint32_t b[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    // (the last of two planes is rounded, after which 2^-16 of the value is missing at most; three are exact)
-                    b[j] = p == 1 && PLANES == 2 ? narrow1<hcclBf16>(h[j]) : __float_as_uint(h[j]) >> 16;
-                    h[j] -= __uint_as_float(b[j] << 16);
-                }
-                *gptr<typename Loose<2>::x2>(to + (uint64_t)p * ldh) = typename Loose<2>::x2{b[0] | b[1] << 16, b[2] | b[3] << 16};
-            }
+            __syncthreads();
         }
-        if (shares > 1) __syncthreads();
+        const uint32_t route = lds_u16(choices.lists[w][entry % kLists] + row_of_lane(i));
+        if (!some || share != 0 || route == 0xffffu) continue;
+        const uint32_t f = f0 + q * 4;
+        uint16_t* to = a.hidden + (uint64_t)route * PLANES * ldh + f;
+        float h[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) h[j] = f + j < a.inner ? mx_gate(acc[0][j], acc[1][j]) : 0.0f;
+#pragma unroll
+        for (int p = 0; p < PLANES; ++p) {
+            uint32_t b[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                // (the last of two planes is rounded, after which 2^-16 of the value is missing at most; three are exact)
+                b[j] = p == 1 && PLANES == 2 ? narrow1<hcclBf16>(h[j]) : __float_as_uint(h[j]) >> 16;
+                h[j] -= __uint_as_float(b[j] << 16);
+            }
+            *gptr<typename Loose<2>::x2>(to + (uint64_t)p * ldh) = typename Loose<2>::x2{b[0] | b[1] << 16, b[2] | b[3] << 16};
+        }
     }
 }
 
@@ -486,35 +491,31 @@ __device__ __forceinline__ void layer_down(const LayerMxArgs& a, Choices& choice
         fetch_h(u, s, std::true_type());
         asm volatile("" ::: "memory");  // (steps' loads are made in the steps' order, which the waits count on)
     };
-    v4f acc[FOURS];
-    auto clear = [&] {
-#pragma unroll
-        for (int r = 0; r < FOURS; ++r) acc[r] = v4f{0, 0, 0, 0};
-    };
+    v4f acc = v4f{0, 0, 0, 0};
     auto multiply = [&](int u, const Codes& codes) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < 2; ++h) {
+            b8 planes[FOURS][PLANES];
+#pragma unroll
+            for (int r = 0; r < FOURS; ++r)
+#pragma unroll
+                for (int p = 0; p < PLANES; ++p) planes[r][p] = hidden[u][r][h][p];
             each_piece([&](auto j) {
                 constexpr int J = decltype(j)::value;
                 const b8 v = decode8(codes.c[h][J], power_of(codes, h));
 #pragma unroll
-                for (int r = 0; r < FOURS; ++r)
-#pragma unroll
-                    for (int p = 0; p < PLANES; ++p) acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, move_down<J>(hidden[u][r][h][p]), acc[r], 0, 0, 0);
+                for (int p = 0; p < PLANES; ++p) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, piece<J>(planes, p, lane), acc, 0, 0, 0);
             });
+        }
     };
     auto add = [&](uint32_t entry) {
-#pragma unroll
-        for (int r = 0; r < FOURS; ++r) {
-            const uint32_t route = lds_u16(choices.lists[w][entry % kLists] + r * 4 + i / 4);
-            if (route != 0xffffu && i % 4 == 0) {
-                const float weight = __uint_as_float(lds_u32(choices.weight + route));
-                lds_add4(&sums[w][route / a.top_k][q * 4], weight * acc[r][0], weight * acc[r][1], weight * acc[r][2], weight * acc[r][3]);
-            }
+        const uint32_t route = lds_u16(choices.lists[w][entry % kLists] + row_of_lane(i));
+        if (route != 0xffffu) {
+            const float weight = __uint_as_float(lds_u32(choices.weight + route));
+            lds_add4(&sums[w][route / a.top_k][q * 4], weight * acc[0], weight * acc[1], weight * acc[2], weight * acc[3]);
         }
-        clear();
+        acc = v4f{0, 0, 0, 0};
     };
-    clear();
     const uint64_t all = (uint64_t)entries * whole_steps;
     uint32_t g = (uint32_t)(all * w / kWaves);
     const uint32_t end = (uint32_t)(all * (w + 1) / kWaves);
