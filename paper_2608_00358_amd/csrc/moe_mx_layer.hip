@@ -73,11 +73,9 @@ constexpr int kWaves = 8;  // of a block
 constexpr uint32_t kMostRoutes = HCCL_MAX_LAYER_TOKENS * HCCL_MAX_TOP_K;
 constexpr uint32_t kMostEntries = HCCL_MAX_EXPERTS + kMostRoutes / 16;  // (of 4 rows an expert has one at most)
 constexpr int kLists = 8;  // more than the entries that a wave has begun: one a step on its way, one that is multiplied and one ahead
-typedef __attribute__((address_space(3))) void* lds_ptr;
 
 // LDS by assembly: the compiler would have a read or write of its own wait for every load to LDS that is on its way, as it
 // cannot tell that they have nothing to do with each other. Reads have their wait in the block.
-__device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(lds_ptr)p; }
 __device__ __forceinline__ uint32_t lds_u16(const uint16_t* p) {
     uint32_t v;
     asm volatile("ds_read_u16 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(v) : "v"(lds_address(p)) : "memory");
@@ -166,21 +164,6 @@ __device__ __forceinline__ uint32_t route_of(Choices& c, uint32_t w, uint32_t en
     return own != 0xffffu ? own : first;
 }
 
-// Two blocks of codes of a weight row and their scales.
-struct Codes {
-    v4u c[2];
-    uint32_t scale;
-};
-template <bool INSIDE>
-__device__ __forceinline__ Codes load_pair(const uint8_t* row, const uint8_t* scales, uint32_t k, uint32_t cols) {
-    typedef uint16_t loose __attribute__((aligned(1)));
-    const uint32_t b = k / 16, blocks = (cols + kMxBlock - 1) / kMxBlock;
-    Codes r;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) r.c[h] = INSIDE ? load16<1>(row + k + 16 * h) : load_codes<false, true>(row, k + 16 * h, cols);
-    r.scale = INSIDE || b + 2 <= blocks ? *gptr<loose>(scales + b) : b < blocks ? *gptr<uint8_t>(scales + b) : 0u;
-    return r;
-}
 __device__ __forceinline__ float power_of(const Codes& c, int h) { return mx_power(h ? c.scale >> 8 : c.scale & 0xffu); }
 
 // How rows reach the matrix instructions. A lane of 16 holds 8 elements of its row, 8 times for the 64 that its quarter of the
@@ -215,47 +198,6 @@ __device__ __forceinline__ void each_piece(F f) {
     f(std::integral_constant<int, 3>());
 }
 
-// How weights do. 16 lanes hold 16 rows, so a load by each lane of its own would be 64 accesses of 16 bytes. Where rows are
-// 16-byte aligned (and their scales 4-byte), loads go to LDS directly, 8 lanes to a row's 128 bytes of a step, and
-// each lane reads its row's there: chunk c of 16 bytes of row r lies in slot c ^ (r / 2 & 7), on other banks than those of the rows
-// read with it. A step's buffer is SIDES * 16 rows of 128 bytes, and then their 8 scale bytes each (of one side twice: all lanes
-// load, as a branch would hide from the compiler how many loads there are); a wave has as many as steps on their way, of its
-// own, and needs no barrier for them.
-template <int SIDES>
-constexpr uint32_t kSlot = SIDES * 16 * 128 + 256;
-
-template <int SIDES>
-struct Source {  // where a lane's part of the loads comes from
-    const uint8_t* code[SIDES * 2];
-    const uint8_t* scale;
-};
-template <int SIDES>
-__device__ __forceinline__ void load_to_lds(const Source<SIDES>& src, uint32_t s, char* slot) {
-#pragma unroll
-    for (int n = 0; n < SIDES * 2; ++n)
-        __builtin_amdgcn_global_load_lds((const HCCL_AS1 void*)(src.code[n] + (uint64_t)s * 128), (lds_ptr)(slot + n * 1024), 16, 0, 0);
-    __builtin_amdgcn_global_load_lds((const HCCL_AS1 void*)(src.scale + (uint64_t)s * 8), (lds_ptr)(slot + SIDES * 2048), 4, 0, 0);
-}
-// (in one block with the wait, as the compiler would have a read wait for every load to LDS there is)
-__device__ __forceinline__ void read_from_lds(Codes (&c)[1], uint32_t at0, uint32_t at1, uint32_t scale) {
-    asm volatile("ds_read_b128 %0, %3\n\tds_read_b128 %1, %4\n\tds_read_u16 %2, %5\n\ts_waitcnt lgkmcnt(0)"
-                 : "=&v"(c[0].c[0]), "=&v"(c[0].c[1]), "=&v"(c[0].scale)
-                 : "v"(at0), "v"(at1), "v"(scale)
-                 : "memory");
-}
-__device__ __forceinline__ void read_from_lds(Codes (&c)[2], uint32_t at0, uint32_t at1, uint32_t scale) {
-    asm volatile("ds_read_b128 %0, %6\n\tds_read_b128 %1, %7\n\tds_read_b128 %3, %6 offset:2048\n\tds_read_b128 %4, %7 offset:2048\n\t"
-                 "ds_read_u16 %2, %8\n\tds_read_u16 %5, %8 offset:128\n\ts_waitcnt lgkmcnt(0)"
-                 : "=&v"(c[0].c[0]), "=&v"(c[0].c[1]), "=&v"(c[0].scale), "=&v"(c[1].c[0]), "=&v"(c[1].c[1]), "=&v"(c[1].scale)
-                 : "v"(at0), "v"(at1), "v"(scale)
-                 : "memory");
-}
-template <int N>
-__device__ __forceinline__ void wait_loads() {  // until at most N are on their way
-    static_assert(N < 64, "the counter");
-    __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | (N & 48) << 10);
-}
-
 // Both kernels walk along whole steps of 256 elements, kAhead of which are on their way while one is multiplied: with no branch
 // around a load, which would leave the compiler unable to tell how many are, and all of them waited for. So lanes without a
 // row read their first one, steps behind the last are the last once more, and what is left of a row behind its whole steps
@@ -281,7 +223,7 @@ __device__ __forceinline__ void layer_up(const LayerMxArgs& a, Choices& choices,
     }
     const uint32_t at_a_time = kWaves / shares, share = w % shares;
     char* mine = buffers + w * (AHEAD * kSlot<2>);
-    const uint32_t at0 = lds_address(mine) + i * 128 + ((2 * q) ^ (i >> 1 & 7)) * 16, at_scale = lds_address(mine) + 4096 + i * 8 + q * 2;
+    const uint32_t at0 = lds_address(mine) + code_place(lane), at_scale = lds_address(mine) + scale_place(2, lane);
     for (uint32_t item0 = blockIdx.x * at_a_time; item0 < items; item0 += gridDim.x * at_a_time) {
         const bool some = item0 + w / shares < items;
         const uint32_t item = some ? item0 + w / shares : items - 1, entry = item / tiles, f0 = item % tiles * 16;
@@ -298,14 +240,7 @@ __device__ __forceinline__ void layer_up(const LayerMxArgs& a, Choices& choices,
             ps[y] = a.w_in_scale + row_of(y, f0 + i) * a.ld_in_scale;
         }
         Source<2> src;
-        if constexpr (ALIGNED) {
-#pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                const uint32_t r = (n & 1) * 8 + (lane >> 3);
-                src.code[n] = a.w_in + row_of(n / 2, f0 + r) * a.ld_in + ((lane & 7) ^ (r >> 1 & 7)) * 16;
-            }
-            src.scale = a.w_in_scale + row_of(lane >> 5, f0 + (lane >> 1 & 15)) * a.ld_in_scale + (lane & 1) * 4;
-        }
+        if constexpr (ALIGNED) src = source_of<2>(a.w_in, a.ld_in, a.w_in_scale, a.ld_in_scale, [&](uint32_t y, uint32_t r) { return row_of(y, f0 + r); });
         v4f acc[2] = {v4f{0, 0, 0, 0}, v4f{0, 0, 0, 0}};
         Codes c[ALIGNED ? 1 : AHEAD][2];
         Raw<DT> x[AHEAD][FOURS][2];
@@ -348,7 +283,7 @@ __device__ __forceinline__ void layer_up(const LayerMxArgs& a, Choices& choices,
             auto step = [&](uint32_t m) { return share + (m < n ? m : n - 1) * shares; };
             auto take = [&](int u) {
                 if constexpr (ALIGNED) {
-                    wait_loads<(AHEAD - 1) * (5 + FOURS * ES)>();
+                    wait_steps<(AHEAD - 1) * (kSlotLoads<2> + FOURS * ES)>();
                     const uint32_t at = u * kSlot<2>;
                     read_from_lds(c[0], at0 + at, (at0 ^ 16) + at, at_scale + at);
                     // (used from here on, and not sooner, which would be another wait)
@@ -379,7 +314,7 @@ __device__ __forceinline__ void layer_up(const LayerMxArgs& a, Choices& choices,
                 if (m + u >= n) break;
                 take(u);
             }
-            if (ALIGNED) wait_loads<0>();  // (those behind the last step)
+            if (ALIGNED) wait_steps<0>();  // (those behind the last step)
         }
         if (some && whole_steps < steps && whole_steps % shares == share) {
             fetch_codes(0, whole_steps, std::false_type());
@@ -449,7 +384,7 @@ __device__ __forceinline__ void layer_down(const LayerMxArgs& a, Choices& choice
     const uint32_t n0 = blockIdx.x * 16;
     const uint32_t ldh = padded(a.inner), whole_steps = a.inner / 256, entries = first_lane(choices.number);
     char* mine = buffers + w * (AHEAD * kSlot<1>);
-    const uint32_t at0 = lds_address(mine) + i * 128 + ((2 * q) ^ (i >> 1 & 7)) * 16, at_scale = lds_address(mine) + 2048 + i * 8 + q * 2;
+    const uint32_t at0 = lds_address(mine) + code_place(lane), at_scale = lds_address(mine) + scale_place(1, lane);
     Codes c[ALIGNED ? 1 : AHEAD][1];
     b8 hidden[AHEAD][FOURS][2][PLANES];
     const uint8_t *pw, *ps;
@@ -461,14 +396,7 @@ __device__ __forceinline__ void layer_down(const LayerMxArgs& a, Choices& choice
         auto row_of = [&](uint32_t r) { return first + (n0 + r < a.cols ? n0 + r : a.cols - 1); };
         pw = a.w_out + row_of(i) * a.ld_out;
         ps = a.w_out_scale + row_of(i) * a.ld_out_scale;
-        if constexpr (ALIGNED) {
-#pragma unroll
-            for (int n = 0; n < 2; ++n) {
-                const uint32_t r = n * 8 + (lane >> 3);
-                src.code[n] = a.w_out + row_of(r) * a.ld_out + ((lane & 7) ^ (r >> 1 & 7)) * 16;
-            }
-            src.scale = a.w_out_scale + row_of(lane >> 1 & 15) * a.ld_out_scale + (lane & 1) * 4;
-        }
+        if constexpr (ALIGNED) src = source_of<1>(a.w_out, a.ld_out, a.w_out_scale, a.ld_out_scale, [&](uint32_t, uint32_t r) { return row_of(r); });
         list_entry(a, choices, w, entry, what);
 #pragma unroll
         for (int r = 0; r < FOURS; ++r) ph[r] = a.hidden + (uint64_t)route_of(choices, w, entry, r * 4 + i / 4) * PLANES * ldh;
@@ -532,7 +460,7 @@ __device__ __forceinline__ void layer_down(const LayerMxArgs& a, Choices& choice
         };
         auto take = [&](int u) {
             if constexpr (ALIGNED) {
-                wait_loads<(AHEAD - 1) * (3 + FOURS * 2 * PLANES)>();
+                wait_steps<(AHEAD - 1) * (kSlotLoads<1> + FOURS * 2 * PLANES)>();
                 const uint32_t at = u * kSlot<1>;
                 read_from_lds(c[0], at0 + at, (at0 ^ 16) + at, at_scale + at);
                 // (used from here on, and not sooner, which would be another wait)
@@ -567,7 +495,7 @@ __device__ __forceinline__ void layer_down(const LayerMxArgs& a, Choices& choice
             if (g >= end) break;
             take(u);
         }
-        if (ALIGNED) wait_loads<0>();  // (those behind the last step)
+        if (ALIGNED) wait_steps<0>();  // (those behind the last step)
     }
     if (whole_steps * 256 < a.inner) {
         for (uint32_t entry = w; entry < entries; entry += kWaves) {

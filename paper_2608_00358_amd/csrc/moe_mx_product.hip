@@ -49,13 +49,14 @@ __device__ __forceinline__ void store_four(const ProductMxArgs& a, uint64_t m, u
 }
 
 // Few rows a segment: 16 MB rows by 16 NB columns a block, whose W waves share out the k axis in steps of 128 bytes
-// (256 elements) and join their sums through LDS, in the waves' order. Weights go from memory to registers: each is used
-// by one block only. A lane reads 32 neighbouring bytes of a row, two blocks, and their two scale bytes; four lanes
-// the 128 bytes of a step. The loads of U steps are on their way together.
-template <int MB, int NB, int W, int U>
+// (256 elements) and join their sums through LDS, in the waves' order. Each weight is used by one wave only, and comes by
+// loads to LDS of its own (ALIGNED), or to registers. A lane has 32 neighbouring bytes of a row, two blocks, and their
+// two scale bytes; four lanes the 128 bytes of a step.
+template <int MB, int NB, int W, bool ALIGNED>
 __global__ __launch_bounds__(W * 64) void hccl_moe_product_mx_few_kernel(ProductMxArgs a, uint32_t nblocks) {
     constexpr uint32_t BM = 16 * MB, BN = 16 * NB;
-    __shared__ v4f part[W][MB * NB][64];
+    constexpr uint32_t kOwn = ALIGNED && kSlot<NB> > MB * NB * 1024 ? kSlot<NB> : MB * NB * 1024;  // LDS of a wave: a step, then its sums
+    __shared__ __attribute__((aligned(256))) char lds[W * kOwn];
     const uint32_t lane = threadIdx.x & 63, w = first_lane(threadIdx.x >> 6);
     const uint32_t tile = blockIdx.x / nblocks, n0 = blockIdx.x % nblocks * BN;
     Rows rows;
@@ -81,62 +82,89 @@ __global__ __launch_bounds__(W * 64) void hccl_moe_product_mx_few_kernel(Product
     for (int x = 0; x < MB; ++x)
 #pragma unroll
         for (int y = 0; y < NB; ++y) acc[x][y] = v4f{0, 0, 0, 0};
-    v4i va[U][MB][2], vb[U][NB][2];
-    uint32_t ra[U][MB], rb[U][NB];
+    char* mine = lds + w * kOwn;
+    struct Step {
+        v4i a[MB][2];
+        uint32_t sa[MB];
+        Codes b[NB];
+    };
     const uint32_t blocks = (a.inner + kMxBlock - 1) / kMxBlock;
-    auto scales = [&](const uint8_t* p, uint32_t b, auto inside) -> uint32_t {  // of the blocks b and b + 1
+    auto fetch_rows = [&](Step& f, uint32_t s, auto inside) {  // INSIDE: the step lies inside the rows
+        constexpr bool INSIDE = decltype(inside)::value;
         typedef uint16_t loose __attribute__((aligned(1)));
-        if (inside.value || b + 2 <= blocks) return *gptr<loose>(p + b);
-        return b < blocks ? *gptr<uint8_t>(p + b) : 0u;
-    };
-    auto fetch = [&](int u, uint32_t k0, auto inside) {  // INSIDE: the step lies inside the rows
-        const uint32_t k = k0 + q * 32;
+        const uint32_t k = s * 128 + q * 32, b = k / 16;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int x = 0; x < MB; ++x) {
 #pragma unroll
-            for (int y = 0; y < NB; ++y) vb[u][y][h] = inside.value ? (v4i)load16<1>(pb[y] + k + 16 * h) : (v4i)load_codes<false, false>(pb[y], k + 16 * h, a.inner);
-#pragma unroll
-            for (int x = 0; x < MB; ++x) va[u][x][h] = inside.value ? (v4i)load16<1>(pa[x] + k + 16 * h) : (v4i)load_codes<false, true>(pa[x], k + 16 * h, a.inner);
+            for (int h = 0; h < 2; ++h) f.a[x][h] = (v4i)(INSIDE ? load16<1>(pa[x] + k + 16 * h) : load_codes<false, true>(pa[x], k + 16 * h, a.inner));
+            f.sa[x] = INSIDE || b + 2 <= blocks ? *gptr<loose>(sa[x] + b) : b < blocks ? *gptr<uint8_t>(sa[x] + b) : 0u;
         }
-#pragma unroll
-        for (int y = 0; y < NB; ++y) rb[u][y] = scales(sb[y], k / 16, inside);
-#pragma unroll
-        for (int x = 0; x < MB; ++x) ra[u][x] = scales(sa[x], k / 16, inside);
     };
-    auto multiply = [&](int u) {
+    auto fetch_weights = [&](Step& f, uint32_t s, auto inside) {
+#pragma unroll
+        for (int y = 0; y < NB; ++y) f.b[y] = load_pair<decltype(inside)::value>(pb[y], sb[y], s * 128 + q * 32, a.inner);
+    };
+    auto multiply = [&](const Step& f) {
 #pragma unroll
         for (int x = 0; x < MB; ++x)
 #pragma unroll
             for (int y = 0; y < NB; ++y) {
-                acc[x][y] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(whole(vb[u][y][0]), whole(va[u][x][0]), acc[x][y], kFp4, kFp4, 0, rb[u][y], 0, ra[u][x]);
-                acc[x][y] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(whole(vb[u][y][1]), whole(va[u][x][1]), acc[x][y], kFp4, kFp4, 1, rb[u][y], 1, ra[u][x]);
+                acc[x][y] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(whole((v4i)f.b[y].c[0]), whole(f.a[x][0]), acc[x][y], kFp4, kFp4, 0, f.b[y].scale, 0, f.sa[x]);
+                acc[x][y] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(whole((v4i)f.b[y].c[1]), whole(f.a[x][1]), acc[x][y], kFp4, kFp4, 1, f.b[y].scale, 1, f.sa[x]);
             }
     };
-    const uint32_t bytes = a.inner / 2, all = (a.inner + 1) / 2;  // (whole bytes)
-    uint32_t k0 = w * 128;
-    for (; k0 + (U - 1) * (W * 128) + 128 <= bytes; k0 += U * (W * 128)) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) fetch(u, k0 + u * (W * 128), std::true_type());
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int u = 0; u < U; ++u) multiply(u);
-    }
+    const uint32_t steps = ((a.inner + 1) / 2 + 127) / 128, whole_steps = a.inner / 256;
+    uint32_t s = w;
+    if constexpr (ALIGNED) {
+        const Source<NB> src = source_of<NB>(a.b, a.ldb, a.b_scale, a.ldbs, [&](uint32_t y, uint32_t r) {
+            const uint64_t n = n0 + y * 16 + r;
+            return (uint64_t)rows.expert * a.cols + (n < a.cols ? n : a.cols - 1);
+        });
+        const uint32_t at0 = lds_address(mine) + code_place(lane), at_scale = lds_address(mine) + scale_place(NB, lane);
 #pragma unroll 1
-    for (; k0 < all; k0 += W * 128) {
-        if (k0 + 128 <= bytes) fetch(0, k0, std::true_type());
-        else fetch(0, k0, std::false_type());
-        multiply(0);
+        for (; s < whole_steps; s += W) {
+            Step f;
+            load_to_lds<NB>(src, s, mine);
+            fetch_rows(f, s, std::true_type());
+            wait_steps<0>();
+            read_from_lds(f.b, at0, at0 ^ 16, at_scale);
+            multiply(f);
+        }
+    } else {
+        Step f[2];
+        for (; s + W < whole_steps; s += 2 * W) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                fetch_weights(f[u], s + u * W, std::true_type());
+                fetch_rows(f[u], s + u * W, std::true_type());
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int u = 0; u < 2; ++u) multiply(f[u]);
+        }
+        if (s < whole_steps) {
+            fetch_weights(f[0], s, std::true_type());
+            fetch_rows(f[0], s, std::true_type());
+            multiply(f[0]);
+        }
     }
+    if (whole_steps < steps && whole_steps % W == w) {
+        Step f;
+        fetch_weights(f, whole_steps, std::false_type());
+        fetch_rows(f, whole_steps, std::false_type());
+        multiply(f);
+    }
+    v4f* sums = (v4f*)mine;
 #pragma unroll
     for (int x = 0; x < MB; ++x)
 #pragma unroll
-        for (int y = 0; y < NB; ++y) part[w][x * NB + y][lane] = acc[x][y];
+        for (int y = 0; y < NB; ++y) sums[(x * NB + y) * 64 + lane] = acc[x][y];
     __syncthreads();
     for (uint32_t p = w; p < MB * NB; p += W) {
-        v4f sum = part[0][p][lane];
+        v4f sum = ((const v4f*)lds)[p * 64 + lane];
 #pragma unroll
         for (int v = 1; v < W; ++v) {
-            const v4f more = part[v][p][lane];
+            const v4f more = ((const v4f*)(lds + v * kOwn))[p * 64 + lane];
 #pragma unroll
             for (int j = 0; j < 4; ++j) sum[j] += more[j];
         }
@@ -167,8 +195,6 @@ __global__ __launch_bounds__(W * 64) void hccl_moe_product_mx_few_kernel(Product
 constexpr uint32_t kStep = 64;
 constexpr uint32_t kBand = 4;
 
-typedef __attribute__((address_space(3))) void* lds_ptr;
-
 template <int N>
 __device__ __forceinline__ void wait_loads() {  // until at most N loads are on their way, and LDS is done
     static_assert(N < 16, "the counter's low bits");
@@ -180,7 +206,6 @@ __device__ __forceinline__ void meet() {
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
-__device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(lds_ptr)p; }
 __device__ __forceinline__ void lds_write(uint32_t at, const v4u& v) { asm volatile("ds_write_b128 %0, %1" ::"v"(at), "v"(v) : "memory"); }
 
 // A step's fragments of a wave: TM of rows, TN of columns, two parts each; and the scales of four steps, 16 bits each.
@@ -525,11 +550,14 @@ hipError_t launch_many(const ProductMxArgs& a, hipStream_t s) {
     return hipGetLastError();
 }
 
-template <int MB, int NB, int W, int U>
+template <int MB, int NB, int W>
 hipError_t launch_few(const ProductMxArgs& a, hipStream_t s) {
     const uint64_t nblocks = (a.cols + 16 * NB - 1) / (16 * NB), tiles = most_tiles(a, 16 * MB);
     if (tiles * nblocks > 0xffffffffull / (W * 64)) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL((hccl_moe_product_mx_few_kernel<MB, NB, W, U>), dim3((uint32_t)(tiles * nblocks)), dim3(W * 64), 0, s, a, (uint32_t)nblocks);
+    const dim3 grid((uint32_t)(tiles * nblocks)), block(W * 64);
+    const bool aligned = (((uintptr_t)a.b | a.ldb) % 16 | ((uintptr_t)a.b_scale | a.ldbs) % 4) == 0;
+    if (aligned) hipLaunchKernelGGL((hccl_moe_product_mx_few_kernel<MB, NB, W, true>), grid, block, 0, s, a, (uint32_t)nblocks);
+    else hipLaunchKernelGGL((hccl_moe_product_mx_few_kernel<MB, NB, W, false>), grid, block, 0, s, a, (uint32_t)nblocks);
     return hipGetLastError();
 }
 
@@ -547,14 +575,14 @@ hipError_t launch_product_mx(const ProductMxArgs& a, int cus, hipStream_t s) {
     if (each > 64 && a.inner >= kMxBlock && blocks(64, 64) >= (uint64_t)cus / 2) return launch_many<64, 64, 1, 2, 1, 3>(a, s);
     if (a.offsets ? each <= 8 : a.rows <= 16) {
         const uint64_t tiles = a.offsets ? a.rows / 16 + spread : 1, cols16 = (a.cols + 15) / 16;
-        if (tiles * (cols16 / 4) >= (uint64_t)cus) return launch_few<1, 4, 4, 2>(a, s);
-        if (tiles * (cols16 / 2) >= (uint64_t)cus) return launch_few<1, 2, 4, 4>(a, s);
-        return launch_few<1, 1, 16, 2>(a, s);
+        if (tiles * (cols16 / 4) >= (uint64_t)cus) return launch_few<1, 4, 2>(a, s);
+        if (tiles * (cols16 / 2) >= (uint64_t)cus) return launch_few<1, 2, 4>(a, s);
+        return launch_few<1, 1, 8>(a, s);
     }
     const uint64_t tiles = a.offsets ? a.rows / 32 + spread : (a.rows + 31) / 32, cols16 = (a.cols + 15) / 16;
-    if (tiles * (cols16 / 4) >= (uint64_t)cus) return launch_few<2, 4, 4, 2>(a, s);
-    if (tiles * (cols16 / 2) >= (uint64_t)cus) return launch_few<2, 2, 8, 2>(a, s);
-    return launch_few<2, 1, 16, 2>(a, s);
+    if (tiles * (cols16 / 4) >= (uint64_t)cus) return launch_few<2, 4, 2>(a, s);
+    if (tiles * (cols16 / 2) >= (uint64_t)cus) return launch_few<2, 2, 4>(a, s);
+    return launch_few<2, 1, 4>(a, s);
 }
 
 }  // namespace hccl
