@@ -357,21 +357,19 @@ __device__ __forceinline__ void layer_up(const LayerMxArgs& a, Choices& choices,
     }
 }
 
-// Steps on their way: as many as registers and LDS hold.
-constexpr int up_ahead(int dt, int fours) { return fours < 4 ? 3 : dt == hcclFp32 ? 1 : 2; }
-constexpr int down_ahead(int dt, int fours) { return fours == 1 ? 4 : fours == 2 ? dt == hcclFp32 ? 2 : 3 : dt == hcclFp32 ? 1 : 2; }
+constexpr int steps_ahead(int dt, int fours) { return fours == 4 && dt == hcclFp32 ? 1 : 2; }  // (registers)
 
 template <int DT, bool ALIGNED>
 __global__ __launch_bounds__(kWaves * 64, 2) void hccl_moe_layer_mx_up_kernel(LayerMxArgs a) {
     __shared__ Choices choices;
     __shared__ v4f part[kWaves][2][64];
-    __shared__ __attribute__((aligned(256))) char buffers[ALIGNED ? kWaves * 3 * kSlot<2> : 16];
+    __shared__ __attribute__((aligned(256))) char buffers[ALIGNED ? kWaves * 2 * kSlot<2> : 16];
     find_choices(a, choices);
     if (choices.number == 0) return;
     const uint32_t rows = first_lane(choices.rows);
-    if (rows == 4) layer_up<DT, 1, up_ahead(DT, 1), ALIGNED>(a, choices, buffers, part);
-    else if (rows == 8) layer_up<DT, 2, up_ahead(DT, 2), ALIGNED>(a, choices, buffers, part);
-    else layer_up<DT, 4, up_ahead(DT, 4), ALIGNED>(a, choices, buffers, part);
+    if (rows == 4) layer_up<DT, 1, steps_ahead(DT, 1), ALIGNED>(a, choices, buffers, part);
+    else if (rows == 8) layer_up<DT, 2, steps_ahead(DT, 2), ALIGNED>(a, choices, buffers, part);
+    else layer_up<DT, 4, steps_ahead(DT, 4), ALIGNED>(a, choices, buffers, part);
 }
 
 // Results. A block takes 16 columns of all tokens. The whole steps of all entries, one entry behind the other, are shared out
@@ -513,14 +511,14 @@ __global__ __launch_bounds__(kWaves * 64, 2) void hccl_moe_layer_mx_down_kernel(
     constexpr int ES = kSize<DT>;
     __shared__ Choices choices;
     __shared__ float sums[kWaves][HCCL_MAX_LAYER_TOKENS][16];
-    __shared__ __attribute__((aligned(256))) char buffers[ALIGNED ? kWaves * 4 * kSlot<1> : 16];
+    __shared__ __attribute__((aligned(256))) char buffers[ALIGNED ? kWaves * 2 * kSlot<1> : 16];
     const uint32_t lane = threadIdx.x & 63, w = first_lane(threadIdx.x >> 6), n0 = blockIdx.x * 16;
     for (uint32_t r = lane; r < a.tokens * 16; r += 64) sums[w][r / 16][r % 16] = 0.0f;
     find_choices(a, choices);
     const uint32_t rows = first_lane(choices.rows);
-    if (rows == 4) layer_down<DT, 1, down_ahead(DT, 1), ALIGNED>(a, choices, buffers, sums);
-    else if (rows == 8) layer_down<DT, 2, down_ahead(DT, 2), ALIGNED>(a, choices, buffers, sums);
-    else layer_down<DT, 4, down_ahead(DT, 4), ALIGNED>(a, choices, buffers, sums);
+    if (rows == 4) layer_down<DT, 1, steps_ahead(DT, 1), ALIGNED>(a, choices, buffers, sums);
+    else if (rows == 8) layer_down<DT, 2, steps_ahead(DT, 2), ALIGNED>(a, choices, buffers, sums);
+    else layer_down<DT, 4, steps_ahead(DT, 4), ALIGNED>(a, choices, buffers, sums);
     __builtin_amdgcn_s_waitcnt(0xc07f);  // (LDS alone: the compiler does not know of the sums' additions)
     __syncthreads();
     for (uint32_t r = threadIdx.x; r < a.tokens * 16; r += kWaves * 64) {
