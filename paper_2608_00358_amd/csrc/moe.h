@@ -134,13 +134,16 @@ struct LayerMxArgs {
     const uint8_t* w_in_scale;
     const uint8_t* w_out;
     const uint8_t* w_out_scale;
-    const int32_t* index;  // as routing wrote them
-    const float* weight;
+    int32_t* index;  // the routes
+    float* weight;
     void* out;
     uint16_t* hidden;  // [route][plane][inner padded to 32], bf16 planes whose sum is the hidden value
     uint64_t ldx, ld_in, ld_in_scale, ld_out, ld_out_scale, ldo;
     uint32_t tokens, top_k, cols, inner;
     uint32_t first, held;  // experts whose weights are there
+    RouteArgs route;       // what the routes are made of
+    hcclDataType_t logits_type;
+    uint32_t routes;  // the first kernel makes them (set by launch_layer_mx)
 };
 
 struct ProductArgs {

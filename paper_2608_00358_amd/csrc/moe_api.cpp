@@ -586,8 +586,9 @@ hcclResult_t hccl_moe_layer_mx(hcclComm_t comm, const hcclRouter_t* router, cons
         c.list(index, routes, 4, true, "index").list(weight, routes, 4, true, "weight").rows(out, tokens, cols, ldo, es, true, "out");
         if (need) c.that(workspace != nullptr && workspace_bytes >= need, "workspace too small (hccl_moe_layer_mx_bytes)").list(workspace, need / 4, 4, true, "workspace");
         if (!c.ok() || tokens == 0) return c.result();
-        const RouteArgs r = route_args(*router, logits, ldl, tokens, bias, mask, index, weight);
         LayerMxArgs a{};
+        a.route = route_args(*router, logits, ldl, tokens, bias, mask, index, weight);
+        a.logits_type = logits_dtype;
         a.x = x;
         a.w_in = w_in;
         a.w_in_scale = w_in_scale;
@@ -609,10 +610,7 @@ hcclResult_t hccl_moe_layer_mx(hcclComm_t comm, const hcclRouter_t* router, cons
         a.inner = (uint32_t)inner;
         a.first = (uint32_t)first;
         a.held = (uint32_t)held;
-        return enqueue(c, [&] {
-            const hipError_t e = launch_route(r, logits_dtype, (hipStream_t)stream);
-            return e != hipSuccess || a.cols == 0 ? e : launch_layer_mx(a, dtype, api_cus(comm), (hipStream_t)stream);
-        });
+        return enqueue(c, [&] { return launch_layer_mx(a, dtype, api_cus(comm), (hipStream_t)stream); });
     });
 }
 

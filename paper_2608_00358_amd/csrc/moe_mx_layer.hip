@@ -1,11 +1,12 @@
 // moe_mx_layer.hip -- a whole mixture-of-experts layer for few tokens, with weights in microscaled 4-bit floats:
 //   h_tk = silu(G_e x_t) * (U_e x_t),   y_t = sum_k w_tk D_e h_tk,   e = the token's choice k
-// in two launches behind the choice. Tokens keep their own type: codes become 16-bit floats exactly (an e2m1 code times
+// in two launches, the first of which makes the choice too. Tokens keep their own type: codes become 16-bit floats exactly (an e2m1 code times
 // a power of two has two bits), rows that 16-bit floats do not hold are split into two or three that add up to them, and
 // the matrix instructions add up the products in 32 bits. Bound by the weights' bytes.
 #include <type_traits>
 
 #include "moe_mx_device.h"
+#include "moe_route_device.h"
 
 namespace hccl {
 namespace {
@@ -102,25 +103,62 @@ struct Choices {
     uint32_t entries[kMostEntries], count[HCCL_MAX_EXPERTS], number, rows;
     uint16_t lists[kWaves][kLists][16];
 };
-__device__ __forceinline__ void find_choices(const LayerMxArgs& a, Choices& c) {
+// ROUTES: and makes them, where the launch found that it may (LayerMxArgs::routes), for rounds that every block does over again
+// while it would wait for the routes; block 0 stores them. A launch less: 24 tokens 32 -> 27 us, one token by itself 28.1 ->
+// 27.1 us, and 14.3 us as before in a row of calls, whose launches overlap. 16 lanes a token keep it at one pass for 32 tokens;
+// more experts than 128, 17 choices or groups would not fit those, and are a launch of their own.
+constexpr int kRouteLanes = 16, kRouteEach = 8;  // a token's lanes, experts of each
+constexpr uint32_t kRouteValues = kWaves * 64 * kRouteEach;
+template <bool ROUTES>
+__device__ __forceinline__ void find_choices(const LayerMxArgs& a, Choices& c, float* values) {
     const uint32_t lane = threadIdx.x & 63, w = first_lane(threadIdx.x >> 6), routes = a.tokens * a.top_k;
-    constexpr int kEach = (kMostRoutes + kWaves * 64 - 1) / (kWaves * 64);
-    uint32_t expert[kEach];  // (on their way together)
-    float weight[kEach];
-#pragma unroll
-    for (int n = 0; n < kEach; ++n) {
-        const uint32_t r = n * kWaves * 64 + threadIdx.x;
-        if (r < routes) expert[n] = (uint32_t)a.index[r] - a.first, weight[n] = a.weight[r];
-    }
+    auto note = [&](uint32_t r, int32_t index, float weight) {
+        const uint32_t e = (uint32_t)index - a.first;
+        c.expert[r] = e < a.held ? (uint16_t)e : 0xffffu;
+        c.weight[r] = weight;
+        if (e < a.held) atomicAdd(&c.count[e], 1u);
+    };
     for (uint32_t e = threadIdx.x; e < a.held; e += kWaves * 64) c.count[e] = 0;
-    __syncthreads();
+    if (ROUTES && a.routes) {
+        __syncthreads();
+        const uint32_t sub = threadIdx.x % kRouteLanes, slot = threadIdx.x / kRouteLanes, e0 = sub * kRouteEach;
+        for (uint32_t t0 = 0; t0 < a.tokens; t0 += kWaves * 64 / kRouteLanes) {
+            const uint32_t t = t0 + slot;
+            const bool on = t < a.tokens;
+            float l[kRouteEach], bias[kRouteEach] = {};
+            if (a.route.bias) {
 #pragma unroll
-    for (int n = 0; n < kEach; ++n) {
-        const uint32_t r = n * kWaves * 64 + threadIdx.x;
-        if (r >= routes) break;
-        c.expert[r] = expert[n] < a.held ? (uint16_t)expert[n] : 0xffffu;
-        c.weight[r] = weight[n];
-        if (expert[n] < a.held) atomicAdd(&c.count[expert[n]], 1u);
+                for (int j = 0; j < kRouteEach; ++j) bias[j] = a.route.bias[e0 + j < a.route.experts ? e0 + j : 0];
+            }
+            auto load = [&](auto type) {
+                constexpr int DT = decltype(type)::value;
+                load_logits<DT, kRouteEach>((const char*)a.route.logits + t * a.route.ld * kSize<DT>, e0, a.route.experts, on, l);
+            };
+            if (a.logits_type == hcclBf16) load(std::integral_constant<int, hcclBf16>());
+            else if (a.logits_type == hcclFp16) load(std::integral_constant<int, hcclFp16>());
+            else load(std::integral_constant<int, hcclFp32>());
+            route_token<kRouteLanes, kRouteEach, false, false>(a.route, t, sub, on, l, bias, values + slot * (kRouteLanes * kRouteEach), nullptr, [&](int32_t index, float weight) {
+                const uint32_t r = t * a.top_k + sub;
+                note(r, index, weight);
+                if (blockIdx.x == 0) a.index[r] = index, a.weight[r] = weight;
+            });
+        }
+    } else {
+        constexpr int kEach = (kMostRoutes + kWaves * 64 - 1) / (kWaves * 64);
+        int32_t index[kEach];  // (on their way together)
+        float weight[kEach];
+#pragma unroll
+        for (int n = 0; n < kEach; ++n) {
+            const uint32_t r = n * kWaves * 64 + threadIdx.x;
+            if (r < routes) index[n] = a.index[r], weight[n] = a.weight[r];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < kEach; ++n) {
+            const uint32_t r = n * kWaves * 64 + threadIdx.x;
+            if (r >= routes) break;
+            note(r, index[n], weight[n]);
+        }
     }
     __syncthreads();
     if (w == 0) {
@@ -364,7 +402,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void hccl_moe_layer_mx_up_kernel(La
     __shared__ Choices choices;
     __shared__ v4f part[kWaves][2][64];
     __shared__ __attribute__((aligned(256))) char buffers[ALIGNED ? kWaves * 2 * kSlot<2> : 16];
-    find_choices(a, choices);
+    static_assert(sizeof(part) >= kRouteValues * sizeof(float), "room for the logits of a round");
+    find_choices<true>(a, choices, (float*)part);
     if (choices.number == 0) return;
     const uint32_t rows = first_lane(choices.rows);
     if (rows == 4) layer_up<DT, 1, steps_ahead(DT, 1), ALIGNED>(a, choices, buffers, part);
@@ -514,7 +553,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void hccl_moe_layer_mx_down_kernel(
     __shared__ __attribute__((aligned(256))) char buffers[ALIGNED ? kWaves * 2 * kSlot<1> : 16];
     const uint32_t lane = threadIdx.x & 63, w = first_lane(threadIdx.x >> 6), n0 = blockIdx.x * 16;
     for (uint32_t r = lane; r < a.tokens * 16; r += 64) sums[w][r / 16][r % 16] = 0.0f;
-    find_choices(a, choices);
+    find_choices<false>(a, choices, nullptr);
     const uint32_t rows = first_lane(choices.rows);
     if (rows == 4) layer_down<DT, 1, steps_ahead(DT, 1), ALIGNED>(a, choices, buffers, sums);
     else if (rows == 8) layer_down<DT, 2, steps_ahead(DT, 2), ALIGNED>(a, choices, buffers, sums);
@@ -536,10 +575,15 @@ bool aligned(const uint8_t* codes, uint64_t ld, const uint8_t* scale, uint64_t l
 }
 
 template <int DT>
-hipError_t layer_type(const LayerMxArgs& a, int cus, hipStream_t s) {
-    const uint64_t routes = a.tokens * a.top_k, items = routes * ((a.inner + 31) / 32 * 2);  // at most
+hipError_t layer_type(LayerMxArgs a, int cus, hipStream_t s) {
+    const uint64_t routes = a.cols ? a.tokens * a.top_k : 0, items = routes * ((a.inner + 31) / 32 * 2);  // at most
     const uint64_t down = ((uint64_t)a.cols + 15) / 16;
     if (down * kWaves * 64 > 0xffffffffull || items > 0x7fffffffull) return hipErrorInvalidConfiguration;
+    a.routes = items && a.route.experts <= kRouteLanes * kRouteEach && a.top_k <= kRouteLanes && a.route.top_groups == a.route.groups;
+    if (!a.routes) {
+        const hipError_t e = launch_route(a.route, a.logits_type, s);
+        if (e != hipSuccess || a.cols == 0) return e;
+    }
     const dim3 block(kWaves * 64), up_grid((uint32_t)(items < (uint64_t)cus ? items : (uint64_t)cus)), down_grid((uint32_t)down);
     if (items) {
         if (aligned(a.w_in, a.ld_in, a.w_in_scale, a.ld_in_scale)) hipLaunchKernelGGL((hccl_moe_layer_mx_up_kernel<DT, true>), up_grid, block, 0, s, a);

@@ -260,6 +260,42 @@ def test_calls_on_two_streams_at_once(comm):
     assert all(torch.equal(case.out.view, w) for case, w in zip(cases, want))
 
 
+@pytest.mark.parametrize("ldt", TYPES)
+@pytest.mark.parametrize("T,E,K,options", [
+    (1, 1, 1, {}), (1, 128, 16, {}), (33, 128, 16, {}), (64, 127, 5, {}), (3, 129, 8, {}), (5, 64, 17, {}), (32, 7, 7, {}), (40, 96, 6, {"groups": 8, "top_groups": 3}),
+    (40, 96, 6, {"groups": 8, "top_groups": 8}), (9, 64, 4, {"groups": 4, "top_groups": 2, "group_top": 2})])
+def test_routes_are_those_of_the_router_alone(comm, T, E, K, options, ldt):
+    """Whichever kernel makes them: equal logits, tokens whose logits are masked in part or all, a bias, padding tokens.
+
+    The weights' sums of up to E terms may be added up in another order: each is off by E 2^-24 of itself at most, and the few
+    roundings behind it by 2^-24 each.
+    """
+    rng = np.random.default_rng(13)
+    for score in ("softmax", "sigmoid"):
+        for renormalize in (False, True):
+            for biased in (False, True):
+                case = Case(rng, T, E, K, 64, 32, "bf16", ldt=ldt, score=score, renormalize=renormalize, scale=1.5, **options)
+                logits = case.logits
+                logits.copy_((logits * 2).round() / 2)  # (many are equal)
+                for t, v in ((2, -INF), (4, float("nan")), (6, INF), (8, -1e4)):
+                    if t < T:
+                        logits[t, :: 1 if t in (2, 8) else 3] = v
+                if biased:
+                    logits[logits == INF] = 1.0
+                bias = torch.from_numpy(rng.integers(-2, 3, E).astype(np.float32) / 4).to(DEV) if biased else None
+                case.mask = (rng.random(T) < 0.8).astype(np.uint8)
+                mask = torch.from_numpy(case.mask).to(DEV)
+                index, weight = torch.empty(T, K, dtype=torch.int32, device=DEV), torch.empty(T, K, device=DEV)
+                comm.moe_route(case.router, logits, index, weight, bias=bias, mask=mask)
+                case.run(comm, bias=bias)
+                torch.cuda.synchronize()
+                for room in (case.index, case.weight, case.out, case.space):
+                    room.check()
+                assert torch.equal(case.index.view, index)
+                want, got = weight.double(), case.weight.view.double()
+                assert bool(((got - want).abs() <= (2 * E + 16) * 2.0 ** -24 * want.abs() + 1e-37).all())
+
+
 def test_nothing_to_do(comm):
     rng = np.random.default_rng(12)
     Case(rng, 0, 4, 2, 64, 32, "bf16").run(comm)
