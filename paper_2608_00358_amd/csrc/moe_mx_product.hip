@@ -52,6 +52,9 @@ __device__ __forceinline__ void store_four(const ProductMxArgs& a, uint64_t m, u
 // (256 elements) and join their sums through LDS, in the waves' order. Each weight is used by one wave only, and comes by
 // loads to LDS of its own (ALIGNED), or to registers. A lane has 32 neighbouring bytes of a row, two blocks, and their
 // two scale bytes; four lanes the 128 bytes of a step.
+// Bound by the weights' bytes: 256 rows, 64 experts of 2048 x 2048 bf16, 143 MB, 26.0 us (5.5 TB/s; 22.6 us out of the last
+// cache); 256 x 4096 x 4096 x 64, 570 MB, 107 us (5.3 TB/s). One step a wave and more waves: two steps on their way took 32.4,
+// four waves of one step 24.7 us where two took 24.3.
 template <int MB, int NB, int W, bool ALIGNED>
 __global__ __launch_bounds__(W * 64) void hccl_moe_product_mx_few_kernel(ProductMxArgs a, uint32_t nblocks) {
     constexpr uint32_t BM = 16 * MB, BN = 16 * NB;
@@ -538,15 +541,13 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void hccl_moe_product_mx_many_kern
     });
 }
 
-template <int BM, int BN, int WM, int WN, int GROUPS, int BUFFERS>
+template <int BM, int BN, int WM, int WN, int GROUPS, int BUFFERS, bool DIRECT>
 hipError_t launch_many(const ProductMxArgs& a, hipStream_t s) {
     const uint32_t nblocks = (a.cols + BN - 1) / BN, threads = WM * WN * 64;
     const uint64_t blocks = most_tiles(a, BM) * nblocks;
     if (blocks + 8 > 0xffffffffull / threads) return hipErrorInvalidConfiguration;
     const dim3 grid((uint32_t)((blocks + 7) / 8 * 8));
-    const bool direct = (((uintptr_t)a.a | a.lda | (uintptr_t)a.b | a.ldb) % 16) == 0;
-    if (direct) hipLaunchKernelGGL((hccl_moe_product_mx_many_kernel<BM, BN, WM, WN, GROUPS, BUFFERS, true>), grid, dim3(threads), 0, s, a, nblocks);
-    else hipLaunchKernelGGL((hccl_moe_product_mx_many_kernel<BM, BN, WM, WN, GROUPS, BUFFERS, false>), grid, dim3(threads), 0, s, a, nblocks);
+    hipLaunchKernelGGL((hccl_moe_product_mx_many_kernel<BM, BN, WM, WN, GROUPS, BUFFERS, DIRECT>), grid, dim3(threads), 0, s, a, nblocks);
     return hipGetLastError();
 }
 
@@ -563,24 +564,40 @@ hipError_t launch_few(const ProductMxArgs& a, hipStream_t s) {
 
 }  // namespace
 
+// Which kernel, by the rows of a segment and the blocks that leaves (microseconds; rows x inner x columns x experts; weights
+// that lie in no cache where none is said). Tiles: as large as keep most CUs busy and are mostly full.
+//   256 x 256 or 128 x 128: 4096 x 4096 x 4096 x 1 45 : 62 (256 blocks), 2048 rows 36 : 34 (128); 16384 x 2048 x 2048 x 64
+//     75 : 86 (256 rows a segment), 12800 rows 51 : 53 (200; in cache 47 : 45). Rows that are not 16-byte aligned go through
+//     registers, of which the largest tile has none left.
+//   128 x 128 or 64 x 128: 3000 x 2048 x 1408 x 16 18.5 : 19.3 (187 rows a segment), 2048 rows 20 : 16 (128), 8192 rows of 64
+//     experts 44 : 43 (128; in cache 39 : 35), 1024 x 4096 x 4096 x 1 22.3 : 22.6, 8192 x 8192 x 8192 x 1 417 : 557.
+//   64 x 128 or few rows: 512 x 4096 x 4096 x 1 19 : 25; 1024 x 2048 x 2048 x 64 31.3 : 32.5 (16 rows a segment), 512 rows 30.6 :
+//     28 (8). 64 x 64 or few rows: 256 x 4096 x 4096 x 1 16.5 : 15.2, in cache 10.7 : 13.1 (256 blocks), 128 rows 16 : 10.8 (128).
+// Few rows: 16 a block cost less than 32 up to 12 a segment (768 x 2048 x 2048 x 64 31 : 33). As many columns a block as
+// leave blocks enough: 64 or 32, the inner size shared by 2 or 4 waves: 1024 x 1024 x 4096 x 256 97 : 147 (20 480 blocks of 64),
+// 256 x 2048 x 2048 x 64 27.6 : 26.0 (2 560); 32 or 16: 1 x 8192 x 12288 x 1 13.9 : 15.3 (384 blocks of 32), 1 x 4096 x 4096 x 1
+// 6.0 : 4.8 (128), 24 x 4096 x 8192 x 1 7.6 : 8.7 (256).
 hipError_t launch_product_mx(const ProductMxArgs& a, int cus, hipStream_t s) {
     const uint64_t each = a.rows / a.segments, spread = a.offsets ? (a.rows < a.segments ? a.rows : a.segments) : 0;
     auto blocks = [&](uint64_t bm, uint64_t bn) {  // about; half a tile more for every segment
         return (a.offsets ? a.rows / bm + (spread + 1) / 2 : (a.rows + bm - 1) / bm) * ((a.cols + bn - 1) / bn);
     };
+    const bool direct = (((uintptr_t)a.a | a.lda | (uintptr_t)a.b | a.ldb) % 16) == 0;
     const uint64_t most = a.inner >= kMxBlock ? (uint64_t)cus * 3 / 4 : ~0ull;  // (tiles want 16 bytes of codes a row)
-    if (each >= 128 && blocks(256, 256) >= most) return launch_many<256, 256, 2, 4, 2, 4>(a, s);
-    if (each >= 32 && blocks(128, 128) >= most) return launch_many<128, 128, 2, 2, 1, 3>(a, s);
-    if (each >= 16 && blocks(64, 128) >= most) return launch_many<64, 128, 1, 4, 1, 3>(a, s);
-    if (each > 64 && a.inner >= kMxBlock && blocks(64, 64) >= (uint64_t)cus / 2) return launch_many<64, 64, 1, 2, 1, 3>(a, s);
-    if (a.offsets ? each <= 8 : a.rows <= 16) {
-        const uint64_t tiles = a.offsets ? a.rows / 16 + spread : 1, cols16 = (a.cols + 15) / 16;
-        if (tiles * (cols16 / 4) >= (uint64_t)cus) return launch_few<1, 4, 2>(a, s);
+    if (each >= 256 && direct && blocks(256, 256) >= most) return launch_many<256, 256, 2, 4, 2, 4, true>(a, s);
+    if (each >= 192 && blocks(128, 128) >= most) return direct ? launch_many<128, 128, 2, 2, 1, 3, true>(a, s) : launch_many<128, 128, 2, 2, 1, 3, false>(a, s);
+    if (each >= 16 && blocks(64, 128) >= most) return direct ? launch_many<64, 128, 1, 4, 1, 3, true>(a, s) : launch_many<64, 128, 1, 4, 1, 3, false>(a, s);
+    if (each > 64 && a.inner >= kMxBlock && blocks(64, 64) >= (uint64_t)cus)
+        return direct ? launch_many<64, 64, 1, 2, 1, 3, true>(a, s) : launch_many<64, 64, 1, 2, 1, 3, false>(a, s);
+    const uint64_t cols16 = (a.cols + 15) / 16;
+    if (a.offsets ? each <= 12 : a.rows <= 16) {
+        const uint64_t tiles = a.offsets ? a.rows / 16 + spread : 1;
+        if (tiles * (cols16 / 4) >= (uint64_t)cus * 16) return launch_few<1, 4, 2>(a, s);
         if (tiles * (cols16 / 2) >= (uint64_t)cus) return launch_few<1, 2, 4>(a, s);
         return launch_few<1, 1, 8>(a, s);
     }
-    const uint64_t tiles = a.offsets ? a.rows / 32 + spread : (a.rows + 31) / 32, cols16 = (a.cols + 15) / 16;
-    if (tiles * (cols16 / 4) >= (uint64_t)cus) return launch_few<2, 4, 2>(a, s);
+    const uint64_t tiles = a.offsets ? a.rows / 32 + spread : (a.rows + 31) / 32;
+    if (tiles * (cols16 / 4) >= (uint64_t)cus * 16) return launch_few<2, 4, 2>(a, s);
     if (tiles * (cols16 / 2) >= (uint64_t)cus) return launch_few<2, 2, 4>(a, s);
     return launch_few<2, 1, 4>(a, s);
 }
