@@ -1,4 +1,4 @@
-"""A mixture-of-experts layer around the exchange, for serving and for training.
+"""A mixture-of-experts layer around the exchange, for serving, for decoding and for training.
 
 serve(): P ranks (P buffers on one GPU) with E / P experts each. Every rank routes its tokens, orders
 their rows by expert as 8-bit codes and counts them for every rank; AllToAllvDynamic takes the codes and
@@ -6,10 +6,14 @@ their scales to the experts with those counts, on the device; the experts multip
 then down, in 8 bits); the rows come back with the same counts, and each token's are added up, weighted.
 Nothing waits for the host between the router and the result.
 
+decode(): the few tokens of a decoding step, which every rank has, so that nothing is exchanged before the
+experts: each rank runs the layer over the experts it holds, with weights in microscaled 4-bit floats, in
+one call, and AllReduce adds up the ranks' results.
+
 train(): the same layer's forward and backward pass on one rank, with experts in the tokens' own type, as
 torch.autograd functions over the operators.
 
-    python examples/moe_layer.py            # both, checked against the layer in 32 bits
+    python examples/moe_layer.py            # all, checked against the layer in 32 bits
 """
 import os
 import sys
@@ -111,6 +115,54 @@ class ServingLayer:
         return self.out
 
 
+# ---- decoding --------------------------------------------------------------------------------------
+
+def weights_in_4_bits(comm, w):
+    """Weights (experts, rows, inner) as codes and scales; and the values that those stand for."""
+    rows, n = w.flatten(0, 1), w.shape[2]
+    codes = torch.empty(rows.shape[0], (n + 1) // 2, device=w.device, dtype=torch.uint8)
+    scale = torch.empty(rows.shape[0], (n + 31) // 32, device=w.device, dtype=torch.uint8)
+    values = torch.empty(rows.shape, device=w.device)
+    comm.moe_quantize_mx(rows, codes, scale)
+    comm.moe_dequantize_mx(codes, scale, values)
+    return codes.unflatten(0, w.shape[:2]), scale.unflatten(0, w.shape[:2]), values.unflatten(0, w.shape[:2])
+
+
+class DecodingLayer:
+    """Weights, buffers and bound calls of the layer for a decoding step of T tokens, E / P experts a rank."""
+
+    def __init__(self, comm, router, w_router, w_in, w_out, tokens):
+        """w_router (E, C); w_in and w_out as weights_in_4_bits gives them: codes and scales."""
+        self.stream = torch.cuda.current_stream()  # which the bound calls keep
+        P, E, K = comm.nranks, router.experts, router.top_k
+        C, F, T, each, dev = w_router.shape[1], w_in[0].shape[1] // 2, tokens, E // P, w_router.device
+
+        def new(*shape, dtype=torch.float32):
+            return torch.empty(shape, device=dev, dtype=dtype)
+
+        self.w_router = w_router
+        self.x, self.logits = new(T, C, dtype=torch.bfloat16), new(T, E)
+        self.parts, self.out = ([new(T, C, dtype=torch.bfloat16) for _ in range(P)] for _ in range(2))
+        self.calls = []
+        for r in range(P):
+            own = slice(r * each, (r + 1) * each)
+            space = new(max(1, H.hccl_moe_layer_mx_bytes(T, K, C, F, each)), dtype=torch.uint8)
+            self.calls.append(comm.bind_moe_layer_mx(router, self.logits, self.x, w_in[0][own], w_in[1][own], w_out[0][own], w_out[1][own],
+                                                     new(T, K, dtype=torch.int32), new(T, K), self.parts[r], first=r * each, workspace=space))
+        self.calls.append(comm.bind_allreduce(self.parts, self.out))
+
+    def __call__(self):
+        """self.x -> self.out (P tensors, all the same), in the order of the current stream"""
+        here = torch.cuda.current_stream()
+        self.stream.wait_stream(here)
+        with torch.cuda.stream(self.stream):
+            torch.mm(self.x.float(), self.w_router.t(), out=self.logits)
+            for call in self.calls:
+                call()
+        here.wait_stream(self.stream)
+        return self.out
+
+
 # ---- training --------------------------------------------------------------------------------------
 
 class Route(torch.autograd.Function):
@@ -187,7 +239,7 @@ def train_step(comm, router, x, w_router, w_in, w_out):
     return Combine.apply(expert_rows(rows, offsets.tolist(), w_in, w_out), weight, row, comm)
 
 
-# ---- both, checked ---------------------------------------------------------------------------------
+# ---- all, checked ----------------------------------------------------------------------------------
 
 def plain_layer(x, router, w_router, w_in, w_out):
     """The layer in 32 bits, every token through its experts."""
@@ -234,6 +286,27 @@ def serve(ranks=8, tokens=48, experts=32, top_k=4, hidden=512, inner=256):
     return worst
 
 
+def decode(ranks=4, tokens=8, experts=32, top_k=4, hidden=512, inner=256):
+    """The relative error of the layer over 4-bit weights against the layer in 32 bits over the same weights."""
+    router = H.hccl_router_init(experts=experts, top_k=top_k, renormalize=True)
+    w_router, w_in, w_out = parameters(3, experts, hidden, inner, torch.float32)
+    with H.Comm(ranks, device=0) as comm:
+        *w_in4, w_in = weights_in_4_bits(comm, w_in)
+        *w_out4, w_out = weights_in_4_bits(comm, w_out)
+        layer = DecodingLayer(comm, router, w_router, w_in4, w_out4, tokens)
+        worst = 0.0
+        for step in range(3):
+            g = torch.Generator(device="cuda:0")
+            g.manual_seed(20 + step)
+            layer.x.copy_(torch.randn(tokens, hidden, generator=g, device="cuda:0"))
+            want = plain_layer(layer.x, router, w_router, w_in, w_out)
+            for out in layer():
+                worst = max(worst, float((out.float() - want).norm() / want.norm()))
+        if comm.async_error() != 0:
+            raise RuntimeError(H.hccl_get_last_error())
+    return worst
+
+
 def train(tokens=200, experts=16, top_k=2, hidden=64, inner=32):
     """The greatest error of the result and of every gradient against the plain layer's, of their size, or
     of 1 where that is less: the router of one choice, renormalised, has weight 1 and no gradient."""
@@ -254,4 +327,5 @@ def train(tokens=200, experts=16, top_k=2, hidden=64, inner=32):
 
 if __name__ == "__main__":
     print(f"serving, 8-bit experts: relative error {serve():.4f} against the layer in 32 bits")
+    print(f"decoding, 4-bit weights: relative error {decode():.4f} against the layer in 32 bits over the same weights")
     print(f"training, result and gradients: relative error {train():.2e}")

@@ -477,7 +477,10 @@ hcclResult_t hccl_comm_trace(hcclComm_t comm, hcclTileTrace_t* out, size_t capac
  * (hccl_moe_plan: the counts of a rank's row are what hccl_alltoallv_dynamic reads), the tokens'
  * rows are copied into that order, or quantised into it (hccl_moe_dispatch), the experts multiply
  * them in 8-bit integers (hccl_moe_product, hccl_moe_quantize), and each token's rows are added up
- * (hccl_moe_combine). Routing, dispatch and combine have their gradients.
+ * (hccl_moe_combine). Routing, dispatch and combine have their gradients. In microscaled 4-bit floats
+ * there are dispatch, quantisation and product too (hccl_moe_dispatch_mx, hccl_moe_quantize_mx,
+ * hccl_moe_product_mx), the way back (hccl_moe_dequantize_mx), and for the few tokens of a decoding step
+ * all of a layer, from logits to results (hccl_moe_layer_mx).
  *
  * They work on one rank's arrays in device memory and name no rank. Unlike a collective they are no
  * work packets: nothing is compiled or kept between calls, they take no trigger and write no
@@ -496,7 +499,8 @@ hcclResult_t hccl_comm_trace(hcclComm_t comm, hcclTileTrace_t* out, size_t capac
  * results are the same in every call. Zero tokens, rows or columns are allowed. A launch's threads are
  * counted in 32 bits: a call that would take more fails with hcclUnsupported and enqueues nothing.
  * Routing takes at least 2^26 - 512 tokens, quantisation (and dispatch in 8 bits) and combine's gradient
- * 2^24 - 1 rows or tokens, dispatch and combine 2^26 - 4 tokens of up to 1 KiB or as many KiB of longer ones.
+ * 2^24 - 1 rows or tokens, dispatch and combine 2^26 - 4 tokens of up to 1 KiB or as many KiB of longer ones;
+ * in 4 bits, rows of 2^31 - 128 blocks of 32 elements in all, and the layer 2^27 - 16 columns.
  */
 #define HCCL_MAX_EXPERTS 1024
 #define HCCL_MAX_TOP_K 32

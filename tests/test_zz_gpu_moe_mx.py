@@ -294,6 +294,21 @@ def test_product_of_every_tile_and_length(comm, tile, inner):
         check_product(comm, random_mx(rng, rows, inner, pad=pa, spad=pa % 4), random_mx(rng, experts, cols, inner, pad=pb, spad=pb % 3), inner, ends, dt, pa)
 
 
+# more of them: tiles that only many columns, or a block for every CU, lead to
+MORE_TILES = {"64x64": (400, 3000, 1), "few 16x64": (90, 24000, 8), "few 32x64": (104, 24000, 8)}
+
+
+@pytest.mark.parametrize("inner", [31, 33, 256, 513, 1000, 1024, 1280])
+@pytest.mark.parametrize("tile", MORE_TILES)
+def test_product_of_more_tiles_and_lengths(comm, tile, inner):
+    rows, cols, experts = MORE_TILES[tile]
+    rng = np.random.default_rng(rows + inner)
+    ends = np.concatenate([[0], np.cumsum(rng.multinomial(rows, rng.dirichlet(np.full(experts, 8.0))))]).tolist() if experts > 1 else None
+    whole = -bytes_of(inner) % 16
+    for pad in (whole, 1 + whole):
+        check_product(comm, random_mx(rng, rows, inner, pad=pad, spad=pad % 4), random_mx(rng, experts, cols, inner, pad=pad, spad=pad % 3), inner, ends, "bf16", pad)
+
+
 def test_product_of_many_segments(comm):
     """More segments than a wave has lanes, in one-row tiles and in large ones, some of them empty."""
     for rows, cols, experts, sources in ((700, 512, 100, 3), (9000, 1024, 70, 2), (20000, 300, 33, 8)):
