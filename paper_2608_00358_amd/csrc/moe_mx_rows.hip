@@ -2,7 +2,8 @@
 //
 // A block of 32 neighbours needs nothing beyond itself: four lanes take one, 8 elements each, find its greatest
 // magnitude among themselves, and store 4 bytes of codes a lane and the block's scale byte. Blocks are numbered
-// through all rows, so that rows of any length fill the waves. All of it is bound by memory.
+// through all rows, so that rows of any length fill the waves. All of it is bound by memory: 3 001 x 2 051 fp32 to codes
+// 7.0 us and back 8.8 us (28 MB each), 32 768 x 4 096 codes to bf16 60 us (340 MB, 5.7 TB/s).
 #include "moe_mx_device.h"
 
 namespace hccl {
@@ -58,8 +59,8 @@ __device__ __forceinline__ void encode(float (&x)[8], const float (&up)[8], uint
 }
 
 // Rows that are whole units: a wave is at one row, whose places are on their way with it. Its codes go through LDS, so that a
-// lane stores 16 bytes of them and not 4, and its scales are one store. (8 192 x 4 096 bf16 to 4 rows each: by 4 bytes, with the
-// places looked up before each store, 43 us.)
+// lane stores 16 bytes of them and not 4, and its scales are one store. (8 192 x 4 096 bf16 to 4 rows each, 139 MB: 35.5 us; by 4 bytes, with the
+// places looked up before each store, 43 us. 16 384 x 4 096 to one row 32 us for 170 MB.)
 constexpr uint32_t kWide = 4;  // units
 template <int DT, bool GATED>
 __global__ __launch_bounds__(kThreads) void hccl_moe_quantize_mx_wide_kernel(QuantizeMxArgs a) {
