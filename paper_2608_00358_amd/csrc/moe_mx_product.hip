@@ -182,8 +182,9 @@ __global__ __launch_bounds__(W * 64) void hccl_moe_product_mx_few_kernel(Product
 // rows and weights are 16-byte aligned) or through registers (any alignment, and the last step of an inner size that is no
 // multiple of 128, where codes past the end are zero).
 //
-// Bound by the matrix units' power and by the starts and ends of tiles, 9 us each of 256 x 256: 8192 x 8192 x 8192 294 us (3.74
-// PFLOP/s), 16384 x 4096 x 4096 through 16 experts 197-201 us (2.8), 2999 x 1407 x 2050 through 12 16-18 us (1.0).
+// Bound by the matrix units' power (codes of 0: 226 and 165 us in the first two) and by the starts and ends of tiles, 9 us each
+// of 256 x 256: 8192 x 8192 x 8192 294-325 us (3.4-3.7 PFLOP/s), 16384 x 4096 x 4096 through 16 experts 194-201 us (2.8), 2999 x
+// 1407 x 2050 through 12 16-18 us (1.0).
 //
 // A wave reads a step's fragments from LDS, waits for them, and multiplies them. With two GROUPS, waves 0 to 3 and 4 to 7,
 // which share the SIMDs, the second is half a step behind: one reads while the other multiplies, and barriers between the
