@@ -260,6 +260,24 @@ def test_calls_on_two_streams_at_once(comm):
     assert all(torch.equal(case.out.view, w) for case, w in zip(cases, want))
 
 
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("T,E,K,C,F", [
+    (1, 4, 2, 128, 128), (3, 8, 2, 384, 128), (9, 6, 3, 128, 640), (24, 16, 4, 640, 384), (33, 4, 2, 1152, 896), (64, 8, 2, 128, 1408), (5, 90, 8, 2176, 384), (2, 3, 1, 896, 256)])
+def test_rows_that_end_with_half_a_step(comm, T, E, K, C, F, dt):
+    """Multiples of 128 elements, aligned, with the last expert's rows at the ends of their arrays; and blocks that are no numbers at
+    the end of one expert's rows."""
+    rng = np.random.default_rng(T + C + F)
+    Case(rng, T, E, K, C, F, dt, renormalize=True).run(comm).check()
+    Case(rng, T, E, K, C, F, dt, held=max(1, E // 2), first=E - max(1, E // 2)).run(comm).check()
+    case = Case(rng, T, E, K, C, F, dt, renormalize=True)
+    case.w_in[1][E - 1, :, -1] = 255  # (the last block of one expert's gates and ups)
+    case.run(comm)
+    torch.cuda.synchronize()
+    index, out = host(case.index.view), host(case.out.view.float())
+    bad = (index == E - 1).any(1)
+    assert np.isnan(out[bad]).all() and np.isfinite(out[~bad]).all()
+
+
 @pytest.mark.parametrize("ldt", TYPES)
 @pytest.mark.parametrize("T,E,K,options", [
     (1, 1, 1, {}), (1, 128, 16, {}), (33, 128, 16, {}), (64, 127, 5, {}), (3, 129, 8, {}), (5, 64, 17, {}), (32, 7, 7, {}), (40, 96, 6, {"groups": 8, "top_groups": 3}),
