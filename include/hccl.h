@@ -702,7 +702,7 @@ hcclResult_t hccl_moe_layer_mx_bytes(size_t tokens, uint32_t top_k, size_t cols,
  * nothing. So ranks that hold an expert each and have all the tokens add up their results by hccl_allreduce.
  * x: tokens rows of cols in dtype; out: the same. w_in: held * 2 * inner rows of cols in microscaled 4-bit floats, an expert's
  * inner rows of G and then those of U; w_out: held * cols rows of inner, D. x enters as it is; products are added
- * up in fp32, h is kept to 2^-16 of itself (exactly with fp32), and the sum over experts is taken in fp32 in an order
+ * up in fp32, h is kept in fp32, and the sum over experts is taken in fp32 in an order
  * that depends on sizes and choices alone, then rounded to dtype once. silu has the error that hccl_moe_quantize states.
  * Results of a token with an infinity or NaN are infinite or NaN, and no other's are.
  * workspace: hccl_moe_layer_mx_bytes bytes, 4-byte aligned, free again once the call's work is done; calls that may run at

@@ -137,7 +137,7 @@ struct LayerMxArgs {
     int32_t* index;  // the routes
     float* weight;
     void* out;
-    uint16_t* hidden;  // [route][plane][inner padded to 32], bf16 planes whose sum is the hidden value
+    uint16_t* hidden;  // [route][plane][inner padded to 32], three bf16 planes whose sum is the hidden value
     uint64_t ldx, ld_in, ld_in_scale, ld_out, ld_out_scale, ldo;
     uint32_t tokens, top_k, cols, inner;
     uint32_t first, held;  // experts whose weights are there

@@ -87,7 +87,7 @@ bool is_float(hcclDataType_t dt) { return dt == hcclBf16 || dt == hcclFp16 || dt
 uint64_t mx_bytes(uint64_t cols) { return (cols + 1) / 2; }
 uint64_t mx_blocks(uint64_t cols) { return (cols + kMxBlock - 1) / kMxBlock; }
 
-// The hidden values of every route, in up to three parts of 16 bits; a row's end is whole blocks.
+// The hidden values of every route, in three parts of 16 bits; a row's end is whole blocks.
 uint64_t layer_mx_bytes(uint64_t tokens, uint64_t top_k, uint64_t inner) { return tokens * top_k * mx_blocks(inner) * kMxBlock * 3 * 2; }
 
 template <typename F>

@@ -17,7 +17,9 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
 
 constexpr int kTerms(int dt) { return dt == hcclBf16 ? 1 : dt == hcclFp16 ? 2 : 3; }   // bf16 terms that hold a value of a type
-constexpr int kPlanes(int dt) { return dt == hcclFp32 ? 3 : 2; }                       // bf16 planes of the hidden values
+// bf16 planes of the hidden values: 32 bits of them, as rows of fp32 have. With two the last would be rounded, 2^-16 of a value
+// away, for 1.5 times fewer loads in the second launch (8 tokens 25 : 28 us, 32 tokens 80 : 91 us).
+constexpr int kPlanes = 3;
 
 __device__ __forceinline__ uint32_t padded(uint32_t inner) { return (inner + 31) / 32 * 32; }
 
@@ -229,6 +231,36 @@ __device__ __forceinline__ b8 piece(const b8 (&t)[FOURS][N], int n, uint32_t lan
     }
     return __builtin_bit_cast(b8, v);
 }
+// p[j] of lane 4 r + g: t[g] of lane 4 r + j, for the N that there are. So with several planes or rows for a lane all of its pieces
+// move at once, in two exchanges.
+template <int N>
+__device__ __forceinline__ void turn(const b8 (&t)[N], b8 (&p)[4], uint32_t lane) {
+    static_assert(N >= 2 && N <= 4, "lanes of a quad");
+    const bool odd = lane & 1, high = lane & 2;
+    v4u x[4], y[4];
+#pragma unroll
+    for (int n = 0; n < N; ++n) x[n] = __builtin_bit_cast(v4u, t[n]);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t s0 = dpp<kQuadSwap>(x[0][k]), s1 = dpp<kQuadSwap>(x[1][k]);
+        const uint32_t a0 = odd ? s1 : x[0][k], a1 = odd ? x[1][k] : s0;
+        const uint32_t h0 = dpp<kQuadHalf>(a0), h1 = dpp<kQuadHalf>(a1);
+        if constexpr (N == 2) {
+            y[0][k] = a0, y[1][k] = a1, y[2][k] = h0, y[3][k] = h1;
+        } else {
+            const uint32_t s2 = dpp<kQuadSwap>(x[2][k]);
+            uint32_t a2 = x[2][k], a3 = s2;
+            if constexpr (N == 4) {
+                const uint32_t s3 = dpp<kQuadSwap>(x[3][k]);
+                a2 = odd ? s3 : x[2][k], a3 = odd ? x[3][k] : s2;
+            }
+            const uint32_t h2 = dpp<kQuadHalf>(a2), h3 = dpp<kQuadHalf>(a3);
+            y[0][k] = high ? h2 : a0, y[1][k] = high ? h3 : a1, y[2][k] = high ? a2 : h0, y[3][k] = high ? a3 : h1;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) p[j] = __builtin_bit_cast(b8, y[j]);
+}
 // f(which of four pieces) for each
 template <typename F>
 __device__ __forceinline__ void each_piece(F f) {
@@ -248,7 +280,7 @@ __device__ __forceinline__ void each_piece(F f) {
 // shares as leave the waves least to do in all of their rounds.
 template <int DT, int FOURS, int AHEAD, bool ALIGNED>
 __device__ __forceinline__ void layer_up(const LayerMxArgs& a, Choices& choices, char* buffers, v4f (*part)[2][64]) {
-    constexpr int TERMS = kTerms(DT), PLANES = kPlanes(DT), ES = kSize<DT>;
+    constexpr int TERMS = kTerms(DT), ES = kSize<DT>;
     const uint32_t lane = threadIdx.x & 63, w = first_lane(threadIdx.x >> 6), i = lane & 15, q = lane >> 4;
     const uint32_t ldh = padded(a.inner), tiles = ldh / 16, items = first_lane(choices.number) * tiles;
     const uint32_t steps = ((a.cols + 1) / 2 + 127) / 128, whole_steps = a.cols / 256;
@@ -379,17 +411,16 @@ __device__ __forceinline__ void layer_up(const LayerMxArgs& a, Choices& choices,
         const uint32_t route = lds_u16(choices.lists[w][entry % kLists] + row_of_lane(i));
         if (!some || share != 0 || route == 0xffffu) continue;
         const uint32_t f = f0 + q * 4;
-        uint16_t* to = a.hidden + (uint64_t)route * PLANES * ldh + f;
+        uint16_t* to = a.hidden + (uint64_t)route * kPlanes * ldh + f;
         float h[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) h[j] = f + j < a.inner ? mx_gate(acc[0][j], acc[1][j]) : 0.0f;
 #pragma unroll
-        for (int p = 0; p < PLANES; ++p) {
+        for (int p = 0; p < kPlanes; ++p) {
             uint32_t b[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                // (the last of two planes is rounded, after which 2^-16 of the value is missing at most; three are exact)
-                b[j] = p == 1 && PLANES == 2 ? narrow1<hcclBf16>(h[j]) : __float_as_uint(h[j]) >> 16;
+                b[j] = __float_as_uint(h[j]) >> 16;
                 h[j] -= __uint_as_float(b[j] << 16);
             }
             *gptr<typename Loose<2>::x2>(to + (uint64_t)p * ldh) = typename Loose<2>::x2{b[0] | b[1] << 16, b[2] | b[3] << 16};
@@ -415,17 +446,17 @@ __global__ __launch_bounds__(kWaves * 64, 2) void hccl_moe_layer_mx_up_kernel(La
 
 // Results. A block takes 16 columns of all tokens. The whole steps of all entries, one entry behind the other, are shared out
 // evenly among its waves, and so is what is left of each; a wave adds its weighted results up in its own part of LDS, and these
-// are added up at the end in the waves' order.
-template <int DT, int FOURS, int AHEAD, bool ALIGNED>
+// are added up at the end in the waves' order. An instruction's 16 columns are up to 4 rows in three planes, up to 8 in the
+// first two (and another's the third), or up to 16 in one; a row's columns are added up when its entry ends.
+template <int FOURS, int AHEAD, bool ALIGNED>
 __device__ __forceinline__ void layer_down(const LayerMxArgs& a, Choices& choices, char* buffers, float (*sums)[HCCL_MAX_LAYER_TOKENS][16]) {
-    constexpr int PLANES = kPlanes(DT);
     const uint32_t lane = threadIdx.x & 63, w = first_lane(threadIdx.x >> 6), i = lane & 15, q = lane >> 4;
     const uint32_t n0 = blockIdx.x * 16;
     const uint32_t ldh = padded(a.inner), whole_steps = a.inner / 256, entries = first_lane(choices.number);
     char* mine = buffers + w * (AHEAD * kSlot<1>);
     const uint32_t at0 = lds_address(mine) + code_place(lane), at_scale = lds_address(mine) + scale_place(1, lane);
     Codes c[ALIGNED ? 1 : AHEAD][1];
-    b8 hidden[AHEAD][FOURS][2][PLANES];
+    b8 hidden[AHEAD][FOURS][2][kPlanes];
     const uint8_t *pw, *ps;
     Source<1> src;
     const uint16_t* ph[FOURS];
@@ -438,7 +469,7 @@ __device__ __forceinline__ void layer_down(const LayerMxArgs& a, Choices& choice
         if constexpr (ALIGNED) src = source_of<1>(a.w_out, a.ld_out, a.w_out_scale, a.ld_out_scale, [&](uint32_t, uint32_t r) { return row_of(r); });
         list_entry(a, choices, w, entry, what);
 #pragma unroll
-        for (int r = 0; r < FOURS; ++r) ph[r] = a.hidden + (uint64_t)route_of(choices, w, entry, r * 4 + i / 4) * PLANES * ldh;
+        for (int r = 0; r < FOURS; ++r) ph[r] = a.hidden + (uint64_t)route_of(choices, w, entry, r * 4 + i / 4) * kPlanes * ldh;
     };
     auto fetch_h = [&](int u, uint32_t s, auto inside) {
 #pragma unroll
@@ -446,7 +477,7 @@ __device__ __forceinline__ void layer_down(const LayerMxArgs& a, Choices& choice
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int p = 0; p < PLANES; ++p) {
+                for (int p = 0; p < kPlanes; ++p) {
                     const uint32_t k = s * 256 + q * 64 + h * 32 + (i & 3) * 8;
                     hidden[u][r][h][p] = decltype(inside)::value || k < ldh ? __builtin_bit_cast(b8, load16<2>(ph[r] + (uint64_t)p * ldh + k)) : b8{};
                 }
@@ -458,30 +489,49 @@ __device__ __forceinline__ void layer_down(const LayerMxArgs& a, Choices& choice
         fetch_h(u, s, std::true_type());
         asm volatile("" ::: "memory");  // (steps' loads are made in the steps' order, which the waits count on)
     };
-    v4f acc = v4f{0, 0, 0, 0};
+    v4f acc[2] = {v4f{0, 0, 0, 0}, v4f{0, 0, 0, 0}};
     auto multiply = [&](int u, const Codes& codes) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            b8 planes[FOURS][PLANES];
+            b8 v[4];
 #pragma unroll
-            for (int r = 0; r < FOURS; ++r)
+            for (int j = 0; j < 4; ++j) v[j] = decode8(codes.c[h][j], power_of(codes, h));
+            auto with = [&](int y, const auto& t) {
+                b8 p[4];
+                turn(t, p, lane);
 #pragma unroll
-                for (int p = 0; p < PLANES; ++p) planes[r][p] = hidden[u][r][h][p];
-            each_piece([&](auto j) {
-                constexpr int J = decltype(j)::value;
-                const b8 v = decode8(codes.c[h][J], power_of(codes, h));
+                for (int j = 0; j < 4; ++j) acc[y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[j], p[j], acc[y], 0, 0, 0);
+            };
+            auto& x = hidden[u];
+            if constexpr (FOURS == 1) {
+                with(0, x[0][h]);
+            } else if constexpr (FOURS == 2) {
+                const b8 two[4] = {x[0][h][0], x[1][h][0], x[0][h][1], x[1][h][1]}, last[2] = {x[0][h][2], x[1][h][2]};
+                with(0, two);
+                with(1, last);
+            } else {
 #pragma unroll
-                for (int p = 0; p < PLANES; ++p) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, piece<J>(planes, p, lane), acc, 0, 0, 0);
-            });
+                for (int p = 0; p < kPlanes; ++p) {
+                    const b8 four[4] = {x[0][h][p], x[1][h][p], x[2][h][p], x[3][h][p]};
+                    with(0, four);
+                }
+            }
         }
     };
     auto add = [&](uint32_t entry) {
+        // (the columns' terms, small ones first)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t y = __float_as_uint(acc[0][j]);
+            if constexpr (FOURS == 1) acc[0][j] += __uint_as_float(dpp<kQuadSwap>(y)) + __uint_as_float(dpp<kQuadHalf>(y));
+            if constexpr (FOURS == 2) acc[0][j] += __uint_as_float(dpp<kQuadHalf>(y)) + acc[1][j];
+        }
         const uint32_t route = lds_u16(choices.lists[w][entry % kLists] + row_of_lane(i));
         if (route != 0xffffu) {
             const float weight = __uint_as_float(lds_u32(choices.weight + route));
-            lds_add4(&sums[w][route / a.top_k][q * 4], weight * acc[0], weight * acc[1], weight * acc[2], weight * acc[3]);
+            lds_add4(&sums[w][route / a.top_k][q * 4], weight * acc[0][0], weight * acc[0][1], weight * acc[0][2], weight * acc[0][3]);
         }
-        acc = v4f{0, 0, 0, 0};
+        acc[0] = acc[1] = v4f{0, 0, 0, 0};
     };
     const uint64_t all = (uint64_t)entries * whole_steps;
     uint32_t g = (uint32_t)(all * w / kWaves);
@@ -499,7 +549,7 @@ __device__ __forceinline__ void layer_down(const LayerMxArgs& a, Choices& choice
         };
         auto take = [&](int u) {
             if constexpr (ALIGNED) {
-                wait_steps<(AHEAD - 1) * (kSlotLoads<1> + FOURS * 2 * PLANES)>();
+                wait_steps<(AHEAD - 1) * (kSlotLoads<1> + FOURS * 2 * kPlanes)>();
                 const uint32_t at = u * kSlot<1>;
                 read_from_lds(c[0], at0 + at, (at0 ^ 16) + at, at_scale + at);
                 // (used from here on, and not sooner, which would be another wait)
@@ -508,7 +558,7 @@ __device__ __forceinline__ void layer_down(const LayerMxArgs& a, Choices& choice
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
 #pragma unroll
-                        for (int p = 0; p < PLANES; ++p) asm volatile("" : "+v"(hidden[u][r][h][p]));
+                        for (int p = 0; p < kPlanes; ++p) asm volatile("" : "+v"(hidden[u][r][h][p]));
                 multiply(u, c[0][0]);
             } else {
                 multiply(u, c[u][0]);
@@ -557,9 +607,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void hccl_moe_layer_mx_down_kernel(
     for (uint32_t r = lane; r < a.tokens * 16; r += 64) sums[w][r / 16][r % 16] = 0.0f;
     find_choices<false>(a, choices, nullptr);
     const uint32_t rows = first_lane(choices.rows);
-    if (rows == 4) layer_down<DT, 1, steps_ahead(DT, 1), ALIGNED>(a, choices, buffers, sums);
-    else if (rows == 8) layer_down<DT, 2, steps_ahead(DT, 2), ALIGNED>(a, choices, buffers, sums);
-    else layer_down<DT, 4, steps_ahead(DT, 4), ALIGNED>(a, choices, buffers, sums);
+    if (rows == 4) layer_down<1, 2, ALIGNED>(a, choices, buffers, sums);
+    else if (rows == 8) layer_down<2, 2, ALIGNED>(a, choices, buffers, sums);
+    else layer_down<4, 1, ALIGNED>(a, choices, buffers, sums);  // (registers)
     __builtin_amdgcn_s_waitcnt(0xc07f);  // (LDS alone: the compiler does not know of the sums' additions)
     __syncthreads();
     for (uint32_t r = threadIdx.x; r < a.tokens * 16; r += kWaves * 64) {
