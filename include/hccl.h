@@ -704,6 +704,8 @@ hcclResult_t hccl_moe_layer_mx_bytes(size_t tokens, uint32_t top_k, size_t cols,
  * inner rows of G and then those of U; w_out: held * cols rows of inner, D. x enters as it is; products are added
  * up in fp32, h is kept in fp32, and the sum over experts is taken in fp32 in an order
  * that depends on sizes and choices alone, then rounded to dtype once. silu has the error that hccl_moe_quantize states.
+ * Magnitudes that 16-bit floats do not reach: an element of the weights of 2^128 or more (scales 253 and 254 have some) counts
+ * as infinite, as hccl_moe_dequantize_mx has it, and of an fp32 element of x and of h what is below 2^-133 is lost.
  * Results of a token with an infinity or NaN are infinite or NaN, and no other's are.
  * workspace: hccl_moe_layer_mx_bytes bytes, 4-byte aligned, free again once the call's work is done; calls that may run at
  * a time, and graphs that may, need one each.

@@ -1,7 +1,7 @@
 // moe_mx_layer.hip -- a whole mixture-of-experts layer for few tokens, with weights in microscaled 4-bit floats:
 //   h_tk = silu(G_e x_t) * (U_e x_t),   y_t = sum_k w_tk D_e h_tk,   e = the token's choice k
 // in two launches, the first of which makes the choice too. Tokens keep their own type: codes become 16-bit floats exactly (an e2m1 code times
-// a power of two has two bits), rows that 16-bit floats do not hold are split into two or three that add up to them, and
+// a power of two has two bits; from 2^128 on it is infinite), rows that 16-bit floats do not hold are split into two or three that add up to them (down to 2^-133, the least 16-bit float), and
 // the matrix instructions add up the products in 32 bits. Bound by latency up to some MB of weights (one token, 4 experts of
 // 2048 x 1024, 14.3 us for 13 MB), then by their bytes: 8 tokens, 8 of 128 experts of 4096 x 1024, 79-87 us for 355 MB; 32
 // tokens, 4 of 64 experts of 4096 x 2048, 176-190 us for 766 MB.
@@ -23,7 +23,7 @@ constexpr int kPlanes = 3;
 
 __device__ __forceinline__ uint32_t padded(uint32_t inner) { return (inner + 31) / 32 * 32; }
 
-// Eight codes times 2^(b - 127) as 16-bit floats.
+// Eight codes times 2^(b - 127) as 16-bit floats: subnormal ones from the least scales, infinite ones from the greatest two.
 __device__ __forceinline__ b8 decode8(uint32_t c, float power) {
     const b2 p = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, power, 0), q = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, power, 1);
     const b2 r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, power, 2), s = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, power, 3);
