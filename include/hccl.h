@@ -706,7 +706,8 @@ hcclResult_t hccl_moe_layer_mx_bytes(size_t tokens, uint32_t top_k, size_t cols,
  * that depends on sizes and choices alone, then rounded to dtype once. silu has the error that hccl_moe_quantize states.
  * Magnitudes that 16-bit floats do not reach: an element of the weights of 2^128 or more (scales 253 and 254 have some) counts
  * as infinite, as hccl_moe_dequantize_mx has it, and of an fp32 element of x and of h what is below 2^-133 is lost.
- * Results of a token with an infinity or NaN are infinite or NaN, and no other's are.
+ * An infinity or NaN in x makes all results of its token infinite or NaN where an expert of its is held, and no other
+ * token's; a masked token and one whose experts are all elsewhere have zeros whatever x holds.
  * workspace: hccl_moe_layer_mx_bytes bytes, 4-byte aligned, free again once the call's work is done; calls that may run at
  * a time, and graphs that may, need one each.
  */

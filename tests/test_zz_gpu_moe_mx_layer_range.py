@@ -112,3 +112,20 @@ def test_elements_beyond_32_bits_are_infinite(comm, dt):
         got = run(comm, x, w_in, w_out)
         others = [n for n in range(96) if n != 11]
         assert not bool(torch.isfinite(got[:, 11]).any()) and torch.equal(got[:, others], finite[:, others]) and bool(torch.isfinite(finite).all())
+
+
+@pytest.mark.parametrize("dt", TYPES)
+def test_tokens_that_are_no_numbers_and_have_no_expert_here(comm, dt):
+    """Masked, or none of whose experts is held: zeros, whatever their rows hold."""
+    rng = np.random.default_rng(2)
+    x = torch.from_numpy(rng.normal(size=(6, 70))).to(TYPES[dt]).to(DEV)
+    logits = torch.zeros(6, 4, device=DEV)
+    logits[[0, 3], 1], logits[[1, 2, 4, 5], 2] = 5.0, 5.0
+    x[1, 4], x[2, 69], x[3, 0], x[4, 33] = INF, float("nan"), -INF, float("nan")
+    mask = torch.tensor([1, 1, 0, 1, 1, 1], dtype=U8, device=DEV)
+    w_in, w_out = random_weights(rng, 80, 70, 122), random_weights(rng, 70, 40, 122)
+    both = lambda w: [np.repeat(t, 2, 0) for t in w]  # noqa: E731
+    got = run(comm, x, both(w_in), both(w_out), 4, logits, mask=mask, first=0)  # experts 0 and 1: tokens 0 and 3
+    assert bool((got[[1, 2, 4, 5]] == 0).all()) and bool(torch.isfinite(got[0]).all()) and not bool(torch.isfinite(got[3]).any())
+    got = run(comm, x, both(w_in), both(w_out), 4, logits, mask=mask, first=2)  # experts 2 and 3: tokens 1, 4 and 5; 2 is masked
+    assert bool((got[[0, 2, 3]] == 0).all()) and bool(torch.isfinite(got[5]).all()) and not bool(torch.isfinite(got[[1, 4]]).any())
