@@ -62,11 +62,15 @@ __device__ __forceinline__ void encode(float (&x)[8], const float (&up)[8], uint
 // lane stores 16 bytes of them and not 4, and its scales are one store. (8 192 x 4 096 bf16 to 4 rows each, 139 MB: 35.5 us; by 4 bytes, with the
 // places looked up before each store, 43 us. 16 384 x 4 096 to one row 32 us for 170 MB.)
 constexpr uint32_t kWide = 4;  // units
+struct WideRow {               // of a wave, aligned for what it reads back
+    v4u codes[kWide * 16];
+    uint32_t scales[kWide * 4];
+};
+static_assert(alignof(WideRow) == 16 && sizeof(WideRow) % 16 == 0, "16 bytes a lane");
 template <int DT, bool GATED>
 __global__ __launch_bounds__(kThreads) void hccl_moe_quantize_mx_wide_kernel(QuantizeMxArgs a) {
     constexpr int ES = kSize<DT>;
-    __shared__ uint32_t all_codes[kWaves][kWide * 64];
-    __shared__ uint8_t all_scales[kWaves][kWide * 16];
+    __shared__ WideRow own[kWaves];
     const uint32_t lane = threadIdx.x & 63, w = first_lane(threadIdx.x >> 6), pieces = a.blocks / (kWide * 16);
     const uint32_t id = blockIdx.x * kWaves + w, t = id / pieces, b0 = id % pieces * (kWide * 16);
     const uint64_t rows = a.limit && *a.limit < (int64_t)a.rows ? (*a.limit < 0 ? 0 : (uint64_t)*a.limit) : a.rows;
@@ -84,12 +88,14 @@ __global__ __launch_bounds__(kThreads) void hccl_moe_quantize_mx_wide_kernel(Qua
     for (uint32_t u = 0; u < kWide; ++u) {
         uint32_t b, codes;
         encode<DT, GATED>(x[u], up[u], b, codes);
-        all_codes[w][u * 64 + lane] = codes;
-        if (lane % 4 == 0) all_scales[w][u * 16 + lane / 4] = (uint8_t)b;
+        ((uint32_t*)own[w].codes)[u * 64 + lane] = codes;
+        if (lane % 4 == 0) ((uint8_t*)own[w].scales)[u * 16 + lane / 4] = (uint8_t)b;
     }
-    // (a wave's own part of LDS, which it reads in the order of its writes)
-    const v4u codes = *(const v4u*)&all_codes[w][lane * 4];
-    const uint32_t scales = *(const uint32_t*)&all_scales[w][lane % 16 * 4];
+    // (a wave's own part of LDS, which it reads in the order of its writes; the fence keeps the compiler to that)
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    const v4u codes = own[w].codes[lane];
+    const uint32_t scales = own[w].scales[lane % 16];
     const uint32_t copies = a.row ? a.top_k : 1u;
     for (uint32_t k = 0; k < copies; ++k) {
         const uint32_t r = a.row ? at_lane(mine, k) : t;
