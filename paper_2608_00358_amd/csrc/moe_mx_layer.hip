@@ -1,10 +1,12 @@
 // moe_mx_layer.hip -- a whole mixture-of-experts layer for few tokens, with weights in microscaled 4-bit floats:
 //   h_tk = silu(G_e x_t) * (U_e x_t),   y_t = sum_k w_tk D_e h_tk,   e = the token's choice k
-// in two launches, the first of which makes the choice too. Tokens keep their own type: codes become 16-bit floats exactly (an e2m1 code times
-// a power of two has two bits; from 2^128 on it is infinite), rows that 16-bit floats do not hold are split into two or three that add up to them (down to 2^-133, the least 16-bit float), and
-// the matrix instructions add up the products in 32 bits. Bound by latency up to some MB of weights (one token, 4 experts of
-// 2048 x 1024, 14.3 us for 13 MB), then by their bytes: 8 tokens, 8 of 128 experts of 4096 x 1024, 79-87 us for 355 MB; 32
-// tokens, 4 of 64 experts of 4096 x 2048, 176-190 us for 766 MB.
+// in two launches, the first of which makes the choice too. Tokens keep their own type: codes become 16-bit floats exactly (an e2m1
+// code times a power of two has two bits; from 2^128 on it is infinite), rows and hidden values that 16-bit floats do not hold are
+// split into two or three that add up to them (down to 2^-133, the least 16-bit float), and the matrix instructions add up
+// the products in 32 bits. Bound by latency up to some MB of weights (one token, 4 experts of 2048 x 1024, 15.1 us for 13 MB),
+// then by their bytes and by what rows and hidden values take to reach the matrix instructions: 8 tokens, 8 of 128 experts of
+// 4096 x 1024, 74-92 us for 355 MB; 32 tokens, 4 of 64 experts of 4096 x 2048, 183-217 us for 766 MB, and 262 where an expert has
+// more than 8 of them. (Ranges are those of eight batches.)
 #include <type_traits>
 
 #include "moe_mx_device.h"
@@ -108,9 +110,10 @@ struct Choices {
     uint16_t lists[kWaves][kLists][16];
 };
 // ROUTES: and makes them, where the launch found that it may (LayerMxArgs::routes), for rounds that every block does over again
-// while it would wait for the routes; block 0 stores them. A launch less: 24 tokens 32 -> 27 us, one token by itself 28.1 ->
-// 27.1 us, and 14.3 us as before in a row of calls, whose launches overlap. 16 lanes a token keep it at one pass for 32 tokens;
-// more experts than 128, 17 choices or groups would not fit those, and are a launch of their own.
+// while it would wait for the routes; block 0 stores them. A launch less: one token 15.6 -> 15.1 us in a row of calls, whose
+// launches overlap, and 27.7 -> 26.9 us by itself; 5 tokens by themselves 38.7 -> 37.2 us; 24 and more within a percent. 16 lanes a
+// token keep it at one pass for 32 tokens; more experts than 128, 17 choices or groups would not fit those, and are a launch of
+// their own.
 constexpr int kRouteLanes = 16, kRouteEach = 8;  // a token's lanes, experts of each
 constexpr uint32_t kRouteValues = kWaves * 64 * kRouteEach;
 template <bool ROUTES>

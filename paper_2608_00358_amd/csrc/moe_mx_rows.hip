@@ -59,7 +59,7 @@ __device__ __forceinline__ void encode(float (&x)[8], const float (&up)[8], uint
 }
 
 // Rows that are whole units: a wave is at one row, whose places are on their way with it. Its codes go through LDS, so that a
-// lane stores 16 bytes of them and not 4, and its scales are one store. (8 192 x 4 096 bf16 to 4 rows each, 139 MB: 35.5 us; by 4 bytes, with the
+// lane stores 16 bytes of them and not 4, and its scales are one store. (8 192 x 4 096 bf16 to 4 rows each, 139 MB: 36 us; by 4 bytes, with the
 // places looked up before each store, 43 us. 16 384 x 4 096 to one row 32 us for 170 MB.)
 constexpr uint32_t kWide = 4;  // units
 struct WideRow {               // of a wave, aligned for what it reads back
